@@ -170,7 +170,8 @@ const char* wq4_status_string(int status);
  * another CTA's activations gave up; wq4_attn.h calls add bit 3 = a sequence
  * length beyond its page table (clamped), bit 4 = a page id outside the pool
  * (zeros read in its place), bit 5 = an append with a bad position or page
- * id (nothing written); bit 6 = wq4_gemm met a scale beyond
+ * id (nothing written), bit 7 = a page pool call that could not be done in
+ * full; bit 6 = wq4_gemm met a scale beyond
  * WQ4_MAX_FP16_SCALE (its outputs are not valid).  Returns WQ4_ERR_TIMEOUT if
  * any bit was set, WQ4_OK otherwise, WQ4_ERR_CUDA on a CUDA failure.
  */

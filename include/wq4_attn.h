@@ -93,6 +93,22 @@ int wq4_paged_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_stri
                         size_t workspace_bytes, void* stream);
 
 /*
+ * wq4_paged_attention under a sliding window with a few first tokens that stay
+ * visible (sinks): the new token of sequence b, at position T - 1, sees
+ *   t < T  with  t >= T - window  or  t < n_sinks.
+ *   window  : tokens of the window, the new one included, >= 1; 0: no window
+ *             (n_sinks is then without effect).
+ *   n_sinks : >= 0.
+ * Everything else is as for wq4_paged_attention, its workspace included.  Only
+ * pages that hold a visible token are looked up and read: the others may have
+ * been freed (wq4_kv_trim) and their page-table entries may be anything.
+ * What masked rows of a visible page hold (NaN included) does not matter.
+ */
+int wq4_window_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_stride, const int32_t* seq_lens,
+                         uint16_t* out, int out_stride, int batch, int n_q_heads, float scale, int window,
+                         int n_sinks, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Append step of a decode iteration: writes the new token's key and value of
  * every key/value head into the cache,
  *   cache.k[page_table[b][pos / page_size]][h][pos % page_size][:] = new_k[b][h][:]
@@ -106,6 +122,150 @@ int wq4_paged_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_stri
  */
 int wq4_kv_append(const wq4_kv_cache* cache, const uint16_t* new_k, const uint16_t* new_v, int new_stride,
                   const int32_t* positions, int batch, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Prompts                                                                    */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * The new tokens of a batch of prompts (or of chunks of them) are rows laid end
+ * to end: sequence b owns rows [row_starts[b], row_starts[b + 1]), n of them (0
+ * allowed), and they are the last n of its seq_lens[b] tokens: the row r stands
+ * at position seq_lens[b] - n + (r - row_starts[b]).
+ *   row_starts : int32 [batch + 1] device array, not decreasing, within [0, rows].
+ *   seq_lens   : int32 [batch] device array, tokens of each sequence, the new
+ *                ones included.
+ *   rows       : rows that the buffers hold (>= row_starts[batch]).  Rows that
+ *                no sequence owns are neither read nor written.
+ *
+ * wq4_prompt_append: for each row of the fused QKV projection's output, the
+ * rotation of q and k as in wq4_decode_attn (pairs (x_2i, x_2i+1) by
+ * pos * rope_theta^(-2i / 128)) and the append of k and v at the row's position:
+ *   q_out[r] = rope(qkv[r][: n_q_heads]),  cache.k <- rope(the next n_kv_heads),
+ *   cache.v <- the last n_kv_heads.
+ *   qkv   : fp16 rows of qkv_stride elements holding [n_q_heads + 2 *
+ *           n_kv_heads][head_dim]; 16-byte aligned, qkv_stride % 8 == 0.
+ *   q_out : fp16 rows of q_out_stride elements, [n_q_heads][head_dim] each; 16-byte
+ *           aligned, q_out_stride % 8 == 0.  It may be qkv itself (the same
+ *           pointer and stride: rotated in place); otherwise it must not overlap it.
+ *   rope_theta : > 1, or 0 for no rotation (q is then copied, and left out with
+ *           a null q_out).
+ * Each rotated element is within half an fp16 ulp, plus 2^-22 of the pair's
+ * larger element, of the exact rotation; values are copied bit for bit.  A
+ * sequence whose rows have a position below 0, beyond the page table or on a
+ * page id outside the pool: those rows' keys and values are not written, and
+ * bit 5 is flagged (q is rotated by max(position, 0)).
+ * Sequences must not map new positions to the same cache row.
+ */
+int wq4_prompt_append(const wq4_kv_cache* cache, const uint16_t* qkv, int qkv_stride, uint16_t* q_out,
+                      int q_out_stride, const int32_t* row_starts, const int32_t* seq_lens, int batch, int rows,
+                      int n_q_heads, double rope_theta, void* stream);
+
+/*
+ * Workspace wq4_prompt_attention needs on the current device for calls of at
+ * most this batch and this many rows.  0 on bad arguments.
+ */
+size_t wq4_prompt_attention_workspace_bytes(int batch, int rows, int n_q_heads, int n_kv_heads, int head_dim);
+
+/*
+ * Attention of a prompt's rows over the cache, their own keys and values
+ * (appended before) included: the row at position i sees
+ *   t <= i  with  window == 0  or  t > i - window  or  t < n_sinks
+ * and o is as for wq4_paged_attention over those tokens; a row that sees none
+ * (position below 0) gets zeros.  Grouping, scale and the accuracy contract are
+ * those of wq4_paged_attention.
+ *   q, out : fp16 rows of q_stride, out_stride elements, [n_q_heads][head_dim]
+ *            each; 16-byte aligned, strides % 8 == 0; out must not overlap the
+ *            inputs or the workspace.
+ *   workspace : device memory of wq4_prompt_attention_workspace_bytes(), 256-byte
+ *            aligned, of any contents, not shared by calls that may overlap.
+ * Pages of which no row of the call sees a token are not read: their entries may
+ * be anything.  What a row does not see (NaN included) does not reach it.
+ * Positions at or beyond the page table's end: the length is clamped there for
+ * keys and values and bit 3 flagged; a page id outside the pool among the seen
+ * ones reads as zeros and flags bit 4.  Deterministic on one device.
+ */
+int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_stride, const int32_t* row_starts,
+                         const int32_t* seq_lens, uint16_t* out, int out_stride, int batch, int rows, int n_q_heads,
+                         float scale, int window, int n_sinks, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Pages                                                                      */
+/* ------------------------------------------------------------------------ */
+
+#define WQ4_KV_MAX_SEQS 1024
+#define WQ4_KV_MAX_LAYERS 128
+
+/*
+ * A pool of pages and the sequences that hold them, kept on the device.  Every
+ * layer has its own cache of the same geometry; one page table serves them all.
+ * What the calls below keep true, and need:
+ *   - page_table[s][j] for j < ceil(seq_lens[s] / page_size) is a page id, or -1
+ *     where wq4_kv_trim freed the page; every further entry is -1;
+ *   - page_refs[p] is the number of entries that name page p; 0: free.
+ * (All -1, 0 and 0 is an empty pool.)  A call that takes pages takes the
+ * lowest-numbered free ones in order, so its result depends on the state alone.
+ *   layers     : HOST array of num_layers caches, each with this page_table;
+ *                at most WQ4_KV_MAX_LAYERS.
+ *   page_table : device int32 [max_seqs][layers[0].page_table_stride].
+ *   seq_lens   : device int32 [max_seqs];  max_seqs <= WQ4_KV_MAX_SEQS.
+ *   page_refs  : device int32 [num_pages].
+ *   workspace  : device memory of wq4_kv_pool_workspace_bytes(), 16-byte aligned,
+ *                of any contents.
+ * The calls are asynchronous on `stream`, allocate nothing and can be captured;
+ * calls on one pool must not overlap on the GPU.  Lists are device int32 [n], n
+ * from 0 to WQ4_KV_MAX_SEQS.  What cannot be done is left undone as said at each
+ * call and flagged in the status word (bit 7).
+ */
+typedef struct {
+    const wq4_kv_cache* layers;
+    int num_layers;
+    int max_seqs;
+    int32_t* page_table;
+    int32_t* seq_lens;
+    int32_t* page_refs;
+    void* workspace;
+    size_t workspace_bytes;
+} wq4_kv_pool;
+
+/* 0 on bad arguments. */
+size_t wq4_kv_pool_workspace_bytes(int num_pages, int max_seqs);
+
+/* Grows sequence seqs[i] to new_lens[i] tokens: takes the pages it lacks and sets
+ * its length (the new tokens' rows hold whatever the pages held).  Refused:
+ * an index out of range or listed before, a length below the present one or
+ * beyond the page table.  Where the free pages run out, that sequence and all
+ * later ones that need any stay as they were. */
+int wq4_kv_reserve(const wq4_kv_pool* pool, const int32_t* seqs, const int32_t* new_lens, int n, void* stream);
+
+/* Sequence children[i] becomes a copy of parents[i]: full pages are shared, a
+ * last page that is not full is copied (its rows in use, in every layer) to a page
+ * of the child's own, so that both can append.  What the child held is freed
+ * first.  A parent may have many children.  Refused: an index out of range, a
+ * child listed before, a child that is a parent in the list.  A child for whose
+ * last page no free one is left stays empty (length 0). */
+int wq4_kv_fork(const wq4_kv_pool* pool, const int32_t* parents, const int32_t* children, int n, void* stream);
+
+/* Frees all pages of the listed sequences; their lengths become 0.  An index out
+ * of range is refused; one listed twice is freed once. */
+int wq4_kv_free(const wq4_kv_pool* pool, const int32_t* seqs, int n, void* stream);
+
+/* Frees the pages of the listed sequences that their coming tokens do not see
+ * under a window (>= 1) with n_sinks (>= 0) first tokens: those without a token t
+ * < n_sinks or t > seq_lens - window.  Their entries become -1; lengths stay.
+ * Refusals as for wq4_kv_free. */
+int wq4_kv_trim(const wq4_kv_pool* pool, const int32_t* seqs, int n, int window, int n_sinks, void* stream);
+
+/* Moves the pages in use to the front of the pool: with m in use, the k-th one at
+ * or behind page m moves to the k-th free one before it, in every layer, and
+ * every table entry follows.  An entry that names a page without reference or
+ * outside the pool becomes -1 and is flagged if it is at or behind m. */
+int wq4_kv_compact(const wq4_kv_pool* pool, void* stream);
+
+/* Copies page src[i] to page dst[i] in every layer (n up to num_pages; table and
+ * references stay as they are).  Refused: an id outside the pool, a page that is
+ * the destination of two pairs or both a source and a destination. */
+int wq4_kv_copy_pages(const wq4_kv_pool* pool, const int32_t* src, const int32_t* dst, int n, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Decode step with attention                                               */

@@ -27,6 +27,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <mutex>
@@ -76,6 +77,7 @@ struct AttnParams {
     uint32_t* err;
     int q_stride, out_stride, pt_stride;
     int batch, Hkv, G, page_size, num_pages;
+    int window, sinks;           // paged_attn_kernel<true>: tokens of the window, first tokens that stay visible
     float sl2;                   // scale * log2(e)
     int stall;                   // test hook: no tile is copied
     float* sq;                   // per (row, head) sums of squares of the outputs, [batch][sq_ld]; null: none
@@ -134,6 +136,22 @@ __device__ __forceinline__ float2 unpack_half2(uint32_t v)
 __device__ __forceinline__ uint32_t sw128(int r, int c)
 {
     return static_cast<uint32_t>(r * 128 + ((c ^ (r & 7)) << 4));
+}
+
+// Tiles that a sequence's new token sees under a window: the last `window`
+// tokens and the first `sinks`.  Tiles of the list from `front` on are `gap`
+// tiles further along the sequence (the tiles between hold no visible token: their
+// pages may be gone, and are neither looked up nor read).
+struct SeenTiles {
+    int tiles, front, gap;
+};
+
+__device__ __forceinline__ SeenTiles seen_tiles(int T, int window, int sinks)
+{
+    const int all = (T + kTile - 1) / kTile;
+    const int front = (min(sinks, T) + kTile - 1) / kTile, first = max(0, T - window) / kTile;
+    const int gap = max(0, first - front);
+    return {all - gap, front, gap};
 }
 
 // One piece: tiles [t0, t1) of kv head h of sequence b (a contiguous run of
@@ -200,6 +218,8 @@ __device__ __forceinline__ Piece whole_piece(const int* pre, const int* parts, i
     return p;
 }
 
+// kWin: under a window, the tile list holds the visible tiles only.
+template <bool kWin>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attn_kernel(const __grid_constant__ AttnParams P)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -230,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attn_kernel(const 
                     atomicOr(P.err, kErrSeqLen);
                     T = max_tok;
                 }
-                tiles = T > 0 ? (T + kTile - 1) / kTile : 0;
+                tiles = T > 0 ? (kWin ? seen_tiles(T, P.window, P.sinks).tiles : (T + kTile - 1) / kTile) : 0;
             }
             longest = max(longest, tiles);
             live += __popc(__ballot_sync(0xffffffffu, tiles > 0));
@@ -314,12 +334,14 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attn_kernel(const 
         for (int g = g_begin; g < g_end && ok;) {
             const Piece pc = piece(g);
             const int32_t* pt = P.page_table + static_cast<size_t>(pc.b) * P.pt_stride;
+            SeenTiles seen = {};
+            if (kWin) seen = seen_tiles(min(P.seq_lens[pc.b], max_tok), P.window, P.sinks);
             for (int t = pc.t0; t < pc.t1 && ok; t += 32) {
                 // page ids of up to 32 tiles, one per lane
                 int mypage = -1, myrow = 0;
                 const int tt = t + lane;
                 if (tt < pc.t1) {
-                    const int tok = tt * kTile;
+                    const int tok = (kWin && tt >= seen.front ? tt + seen.gap : tt) * kTile;
                     mypage = pt[tok / P.page_size];
                     myrow = tok % P.page_size;
                 }
@@ -391,6 +413,13 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attn_kernel(const 
         const int ntile = pc.t1 - pc.t0;
         int T = P.seq_lens[pc.b];
         T = T > max_tok ? max_tok : T;
+        SeenTiles seen = {};
+        int sink_end = 0, win_begin = 0;
+        if (kWin) {
+            seen = seen_tiles(T, P.window, P.sinks);
+            sink_end = min(P.sinks, T);
+            win_begin = max(0, T - P.window);
+        }
 
         // query fragments: rows = query heads of the group (rows >= G are 0)
         uint32_t qa[8][2];
@@ -418,8 +447,13 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attn_kernel(const 
             const int i = ibase + k;
             const int slot = i % kSlots;
             if (ok) ok = mbar_wait(&full[slot], (i / kSlots) & 1, P.err);
-            const int tok0 = (pc.t0 + k) * kTile;
+            const int tt = pc.t0 + k;
+            const int tok0 = (kWin && tt >= seen.front ? tt + seen.gap : tt) * kTile;
             const int valid = min(kTile, T - tok0);
+            auto sees = [&](int i) {
+                return i < valid && (!kWin || tok0 + i < sink_end || tok0 + i >= win_begin);
+            };
+            const bool see0 = sees(qc), see1 = sees(qc + 1), see2 = sees(qc + 8), see3 = sees(qc + 9);
             const uint32_t kb = ring + slot * kSlotBytes;
             const uint32_t vb = kb + 2 * kBoxBytes;
 
@@ -438,10 +472,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attn_kernel(const 
                 }
             }
             // online softmax of row gq over this tile's tokens
-            float x0 = qc < valid ? s[0][0] * P.sl2 : -INFINITY;
-            float x1 = qc + 1 < valid ? s[0][1] * P.sl2 : -INFINITY;
-            float x2 = qc + 8 < valid ? s[1][0] * P.sl2 : -INFINITY;
-            float x3 = qc + 9 < valid ? s[1][1] * P.sl2 : -INFINITY;
+            float x0 = see0 ? s[0][0] * P.sl2 : -INFINITY;
+            float x1 = see1 ? s[0][1] * P.sl2 : -INFINITY;
+            float x2 = see2 ? s[1][0] * P.sl2 : -INFINITY;
+            float x3 = see3 ? s[1][1] * P.sl2 : -INFINITY;
             float mx = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3));
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
@@ -461,9 +495,9 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attn_kernel(const 
             // ldmatrix.  Output columns = heads 2(lane&3), +1: fetch their factors.
             const float al0 = __shfl_sync(0xffffffffu, alpha, 8 * (lane & 3));
             const float al1 = __shfl_sync(0xffffffffu, alpha, 8 * (lane & 3) + 4);
-            // masks of the value rows past the sequence end (their contents may be anything)
-            const uint32_t mlo = (qc < valid ? 0x0000FFFFu : 0u) | (qc + 1 < valid ? 0xFFFF0000u : 0u);
-            const uint32_t mhi = (qc + 8 < valid ? 0x0000FFFFu : 0u) | (qc + 9 < valid ? 0xFFFF0000u : 0u);
+            // masks of the value rows that are not seen (their contents may be anything)
+            const uint32_t mlo = (see0 ? 0x0000FFFFu : 0u) | (see1 ? 0xFFFF0000u : 0u);
+            const uint32_t mhi = (see2 ? 0x0000FFFFu : 0u) | (see3 ? 0xFFFF0000u : 0u);
             {
                 const int mi = lane >> 3;
                 const int r = ((mi >> 1) << 3) + (lane & 7);
@@ -650,19 +684,27 @@ __global__ void kv_append_kernel(const uint16_t* __restrict__ new_k, const uint1
     }
 }
 
+// Blocks of one kernel that fit an SM (0: a CUDA failure).
+template <bool kWin>
+int attn_per_sm()
+{
+    int per_sm = 0;
+    if (cudaFuncSetAttribute(paged_attn_kernel<kWin>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(attn_smem_bytes(WQ4_ATTN_MAX_BATCH))) != cudaSuccess)
+        return 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, paged_attn_kernel<kWin>, kThreads,
+                                                      attn_smem_bytes(WQ4_ATTN_MAX_BATCH)) != cudaSuccess)
+        return 0;
+    return per_sm;
+}
+
 int attn_grid(int dev, int sms)
 {
     static std::mutex mu;
     static int cached[64] = {0};
     std::lock_guard<std::mutex> lock(mu);
     if (dev >= 0 && dev < 64 && cached[dev]) return cached[dev];
-    int per_sm = 0;
-    if (cudaFuncSetAttribute(paged_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             static_cast<int>(attn_smem_bytes(WQ4_ATTN_MAX_BATCH))) != cudaSuccess)
-        return 0;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, paged_attn_kernel, kThreads,
-                                                      attn_smem_bytes(WQ4_ATTN_MAX_BATCH)) != cudaSuccess)
-        return 0;
+    int per_sm = std::min(attn_per_sm<false>(), attn_per_sm<true>());
     if (per_sm < 1) return 0;
     if (per_sm > kCtasPerSm) per_sm = kCtasPerSm;
     int g = sms * per_sm;
@@ -702,7 +744,7 @@ namespace wq4 {
 
 int launch_paged_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_stride, const int32_t* seq_lens,
                            uint16_t* out, int out_stride, int batch, int n_q_heads, float scale, void* workspace,
-                           size_t workspace_bytes, float* sq, int sq_ld, cudaStream_t stream)
+                           size_t workspace_bytes, float* sq, int sq_ld, cudaStream_t stream, int window, int sinks)
 {
     if (!check_cache(cache) || !q || !seq_lens || !out || !workspace) return WQ4_ERR_INVALID;
     if (batch < 1 || batch > WQ4_ATTN_MAX_BATCH) return WQ4_ERR_INVALID;
@@ -710,7 +752,7 @@ int launch_paged_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_s
     if (n_q_heads < Hkv || n_q_heads % Hkv) return WQ4_ERR_INVALID;
     if (cache->head_dim != kD || n_q_heads / Hkv > kMaxGroup) return WQ4_ERR_UNSUPPORTED;
     if (q_stride < n_q_heads * kD || out_stride < n_q_heads * kD) return WQ4_ERR_INVALID;
-    if (!(scale == scale) || std::isinf(scale)) return WQ4_ERR_INVALID;
+    if (!(scale == scale) || std::isinf(scale) || window < 0 || sinks < 0) return WQ4_ERR_INVALID;
     if (!aligned(q, 16) || q_stride % 8 || !aligned(cache->k, 16) || !aligned(cache->v, 16) ||
         !aligned(out, 4) || out_stride % 2 || !aligned(workspace, 16) || !aligned(seq_lens, 4) ||
         !aligned(cache->page_table, 4))
@@ -759,6 +801,10 @@ int launch_paged_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_s
     p.batch = batch;
     p.Hkv = Hkv;
     p.G = n_q_heads / Hkv;
+    // a window that no sequence of this page table can outgrow hides nothing
+    const bool windowed = window > 0 && window < cache->page_table_stride * cache->page_size;
+    p.window = window;
+    p.sinks = sinks;
     p.page_size = cache->page_size;
     p.num_pages = cache->num_pages;
     p.sl2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
@@ -776,7 +822,9 @@ int launch_paged_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_s
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, paged_attn_kernel, p) == cudaSuccess ? WQ4_OK : WQ4_ERR_CUDA;
+    const cudaError_t e = windowed ? cudaLaunchKernelEx(&cfg, paged_attn_kernel<true>, p)
+                                   : cudaLaunchKernelEx(&cfg, paged_attn_kernel<false>, p);
+    return e == cudaSuccess ? WQ4_OK : WQ4_ERR_CUDA;
 }
 
 }  // namespace wq4
@@ -787,6 +835,15 @@ extern "C" int wq4_paged_attention(const wq4_kv_cache* cache, const uint16_t* q,
 {
     return launch_paged_attention(cache, q, q_stride, seq_lens, out, out_stride, batch, n_q_heads, scale, workspace,
                                   workspace_bytes, nullptr, 0, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int wq4_window_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_stride,
+                                    const int32_t* seq_lens, uint16_t* out, int out_stride, int batch, int n_q_heads,
+                                    float scale, int window, int n_sinks, void* workspace, size_t workspace_bytes,
+                                    void* stream)
+{
+    return launch_paged_attention(cache, q, q_stride, seq_lens, out, out_stride, batch, n_q_heads, scale, workspace,
+                                  workspace_bytes, nullptr, 0, static_cast<cudaStream_t>(stream), window, n_sinks);
 }
 
 extern "C" int wq4_kv_append(const wq4_kv_cache* cache, const uint16_t* new_k, const uint16_t* new_v, int new_stride,

@@ -55,6 +55,11 @@ class wq4_kv_cache(ctypes.Structure):
                 ("head_dim", _I), ("page_table", _P), ("page_table_stride", _I)]
 
 
+class wq4_kv_pool(ctypes.Structure):
+    _fields_ = [("layers", ctypes.POINTER(wq4_kv_cache)), ("num_layers", _I), ("max_seqs", _I), ("page_table", _P),
+                ("seq_lens", _P), ("page_refs", _P), ("workspace", _P), ("workspace_bytes", _SZ)]
+
+
 class wq4_chain_trace(ctypes.Structure):
     _fields_ = [(n, _SZ) for n in ("x_in", "qkv", "o", "x_mid", "gate_up", "act", "down", "x_out",
                                    "q_rot", "k_rot", "attn")]
@@ -113,7 +118,23 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     L.wq4_paged_attention_workspace_bytes.restype = _SZ
     L.wq4_paged_attention.argtypes = [ctypes.POINTER(wq4_kv_cache), _P, _I, _P, _P, _I, _I, _I, ctypes.c_float,
                                       _P, _SZ, _P]
+    L.wq4_window_attention.argtypes = [ctypes.POINTER(wq4_kv_cache), _P, _I, _P, _P, _I, _I, _I, ctypes.c_float, _I, _I,
+                                       _P, _SZ, _P]
     L.wq4_kv_append.argtypes = [ctypes.POINTER(wq4_kv_cache), _P, _P, _I, _P, _I, _P]
+    L.wq4_prompt_append.argtypes = [ctypes.POINTER(wq4_kv_cache), _P, _I, _P, _I, _P, _P, _I, _I, _I, ctypes.c_double, _P]
+    L.wq4_prompt_attention_workspace_bytes.argtypes = [_I, _I, _I, _I, _I]
+    L.wq4_prompt_attention_workspace_bytes.restype = _SZ
+    L.wq4_prompt_attention.argtypes = [ctypes.POINTER(wq4_kv_cache), _P, _I, _P, _P, _P, _I, _I, _I, _I, ctypes.c_float,
+                                       _I, _I, _P, _SZ, _P]
+    pool = ctypes.POINTER(wq4_kv_pool)
+    L.wq4_kv_pool_workspace_bytes.argtypes = [_I, _I]
+    L.wq4_kv_pool_workspace_bytes.restype = _SZ
+    L.wq4_kv_reserve.argtypes = [pool, _P, _P, _I, _P]
+    L.wq4_kv_fork.argtypes = [pool, _P, _P, _I, _P]
+    L.wq4_kv_free.argtypes = [pool, _P, _I, _P]
+    L.wq4_kv_trim.argtypes = [pool, _P, _I, _I, _I, _P]
+    L.wq4_kv_compact.argtypes = [pool, _P]
+    L.wq4_kv_copy_pages.argtypes = [pool, _P, _P, _I, _P]
     _lib = L
     return L
 
@@ -126,7 +147,10 @@ EXPORTED = ["wq4_gemv", "wq4_gemm", "wq4_unpack_debug", "wq4_pack_host", "wq4_st
             "wq4_test_chain_waits", "wq4_test_gemv_path", "wq4_test_copy_stall",
             "wq4_decode_step_workspace_bytes", "wq4_decode_step", "wq4_decode_step_host",
             "wq4_synth_codes", "wq4_synth_scales", "wq4_synth_sum4",
-            "wq4_paged_attention_workspace_bytes", "wq4_paged_attention", "wq4_kv_append"]
+            "wq4_paged_attention_workspace_bytes", "wq4_paged_attention", "wq4_window_attention", "wq4_kv_append",
+            "wq4_prompt_append", "wq4_prompt_attention_workspace_bytes", "wq4_prompt_attention",
+            "wq4_kv_pool_workspace_bytes", "wq4_kv_reserve", "wq4_kv_fork", "wq4_kv_free", "wq4_kv_trim",
+            "wq4_kv_compact", "wq4_kv_copy_pages"]
 
 
 def _ptr(t) -> int | None:
@@ -303,8 +327,82 @@ def wq4_paged_attention(cache: wq4_kv_cache, q, q_stride: int, seq_lens, out, ou
     return _check("wq4_paged_attention", rc) if check else rc
 
 
+def wq4_window_attention(cache: wq4_kv_cache, q, q_stride: int, seq_lens, out, out_stride: int, batch: int,
+                         n_q_heads: int, scale: float, window: int, n_sinks: int, workspace, workspace_bytes: int,
+                         stream=None, check: bool = True) -> int:
+    rc = load().wq4_window_attention(ctypes.byref(cache), _ptr(q), q_stride, _ptr(seq_lens), _ptr(out), out_stride,
+                                     batch, n_q_heads, scale, window, n_sinks, _ptr(workspace), workspace_bytes,
+                                     _stream(stream))
+    return _check("wq4_window_attention", rc) if check else rc
+
+
 def wq4_kv_append(cache: wq4_kv_cache, new_k, new_v, new_stride: int, positions, batch: int, stream=None,
                   check: bool = True) -> int:
     rc = load().wq4_kv_append(ctypes.byref(cache), _ptr(new_k), _ptr(new_v), new_stride, _ptr(positions), batch,
                               _stream(stream))
     return _check("wq4_kv_append", rc) if check else rc
+
+
+def wq4_prompt_append(cache: wq4_kv_cache, qkv, qkv_stride: int, q_out, q_out_stride: int, row_starts, seq_lens,
+                      batch: int, rows: int, n_q_heads: int, rope_theta: float, stream=None, check: bool = True) -> int:
+    rc = load().wq4_prompt_append(ctypes.byref(cache), _ptr(qkv), qkv_stride, _ptr(q_out), q_out_stride,
+                                  _ptr(row_starts), _ptr(seq_lens), batch, rows, n_q_heads, rope_theta, _stream(stream))
+    return _check("wq4_prompt_append", rc) if check else rc
+
+
+def wq4_prompt_attention_workspace_bytes(batch: int, rows: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return load().wq4_prompt_attention_workspace_bytes(batch, rows, n_q_heads, n_kv_heads, head_dim)
+
+
+def wq4_prompt_attention(cache: wq4_kv_cache, q, q_stride: int, row_starts, seq_lens, out, out_stride: int, batch: int,
+                         rows: int, n_q_heads: int, scale: float, window: int, n_sinks: int, workspace,
+                         workspace_bytes: int, stream=None, check: bool = True) -> int:
+    rc = load().wq4_prompt_attention(ctypes.byref(cache), _ptr(q), q_stride, _ptr(row_starts), _ptr(seq_lens), _ptr(out),
+                                     out_stride, batch, rows, n_q_heads, scale, window, n_sinks, _ptr(workspace),
+                                     workspace_bytes, _stream(stream))
+    return _check("wq4_prompt_attention", rc) if check else rc
+
+
+def kv_pool_desc(layers, page_table, seq_lens, page_refs, workspace) -> wq4_kv_pool:
+    """wq4_kv_pool of a list of wq4_kv_cache (one a layer, all with this page_table), page_table int32
+    [max_seqs][stride], seq_lens int32 [max_seqs], page_refs int32 [num_pages] and a workspace of
+    wq4_kv_pool_workspace_bytes(num_pages, max_seqs) bytes."""
+    descs = (wq4_kv_cache * len(layers))(*layers)
+    pool = wq4_kv_pool(descs, len(layers), page_table.shape[0], _ptr(page_table), _ptr(seq_lens), _ptr(page_refs),
+                       _ptr(workspace), workspace.numel() * workspace.element_size())
+    pool._keep = descs
+    return pool
+
+
+def wq4_kv_pool_workspace_bytes(num_pages: int, max_seqs: int) -> int:
+    return load().wq4_kv_pool_workspace_bytes(num_pages, max_seqs)
+
+
+def wq4_kv_reserve(pool: wq4_kv_pool, seqs, new_lens, n: int, stream=None, check: bool = True) -> int:
+    rc = load().wq4_kv_reserve(ctypes.byref(pool), _ptr(seqs), _ptr(new_lens), n, _stream(stream))
+    return _check("wq4_kv_reserve", rc) if check else rc
+
+
+def wq4_kv_fork(pool: wq4_kv_pool, parents, children, n: int, stream=None, check: bool = True) -> int:
+    rc = load().wq4_kv_fork(ctypes.byref(pool), _ptr(parents), _ptr(children), n, _stream(stream))
+    return _check("wq4_kv_fork", rc) if check else rc
+
+
+def wq4_kv_free(pool: wq4_kv_pool, seqs, n: int, stream=None, check: bool = True) -> int:
+    rc = load().wq4_kv_free(ctypes.byref(pool), _ptr(seqs), n, _stream(stream))
+    return _check("wq4_kv_free", rc) if check else rc
+
+
+def wq4_kv_trim(pool: wq4_kv_pool, seqs, n: int, window: int, n_sinks: int, stream=None, check: bool = True) -> int:
+    rc = load().wq4_kv_trim(ctypes.byref(pool), _ptr(seqs), n, window, n_sinks, _stream(stream))
+    return _check("wq4_kv_trim", rc) if check else rc
+
+
+def wq4_kv_compact(pool: wq4_kv_pool, stream=None, check: bool = True) -> int:
+    rc = load().wq4_kv_compact(ctypes.byref(pool), _stream(stream))
+    return _check("wq4_kv_compact", rc) if check else rc
+
+
+def wq4_kv_copy_pages(pool: wq4_kv_pool, src, dst, n: int, stream=None, check: bool = True) -> int:
+    rc = load().wq4_kv_copy_pages(ctypes.byref(pool), _ptr(src), _ptr(dst), n, _stream(stream))
+    return _check("wq4_kv_copy_pages", rc) if check else rc
