@@ -5,10 +5,16 @@
 #include "wq4_attn.h"
 #include "wq4_device.cuh"
 #include "wq4_host.h"
+#include "wq4_tc.cuh"
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
+#include <atomic>
+#include <cfloat>
 #include <cmath>
+#include <cstring>
 
 namespace wq4 {
 namespace {
@@ -144,6 +150,55 @@ __global__ void __launch_bounds__(kAppThreads) prompt_append_kernel(const __grid
 }
 
 // -------------------------------------------------------------- attention --
+//
+// An item is the rows of one key/value head's G query heads over 2 * (128 / G)
+// consecutive new tokens of one sequence: two tiles of up to 128 (token, head)
+// rows, row = token * G + head, so that a key tile is read once for the group.  It
+// walks the tiles of 128 keys that any of its rows sees.  The items' key tiles,
+// laid end to end, are cut into equal shares, one a block of the persistent
+// grid; an item cut by a share's end leaves partial results (maximum, sum,
+// unnormalised output in fp32) that a second kernel joins in their order.
+//
+// Warps: 0-3 and 4-7 the softmax of row tiles 0 and 1 (a thread a row), 8 the MMA
+// issuer, 9 the copies, 10 and 11 what masks do to values (below).  Scores S =
+// Q K^T of 128 x 128 go to tensor memory, one thread reads its row's 128, takes
+// the maximum and writes the weights as fp16 over the scores; O += P V reads
+// them there.  While one row tile's softmax runs, the tensor cores work for the
+// other.  An item of at most one row tile gives both softmax groups that tile,
+// one the even and one the odd key tiles, and adds the two results at its end.
+//
+// The maximum that weights refer to follows the true one only when that is more
+// than 2^kLazy above it, so that O in tensor memory is rarely rescaled; weights
+// carry a factor 2^kLift and so lie within [0, 2^(kLift + kLazy)] of fp16's range,
+// those of 2^-(24 + kLift) of the largest still above zero.
+//
+// Values of masked tokens: a weight of 0 times a NaN or an infinity would reach
+// rows that do not see the token.  In a tile that is not seen whole by all of the
+// item's rows, tokens that no row sees are set to zero in shared memory; if
+// another holds a value that is not finite, the item's rows are computed again
+// one by one, without the tokens they do not see (attend_row).
+
+constexpr int kThreads = 384;
+constexpr int kMmaWarp = 8, kCopyWarp = 9, kValueWarp = 10;
+constexpr int kKeys = 128;                         // keys of a tile
+constexpr int kTileBytes = kKeys * kD * 2;         // Q, K and V tiles: two slabs of 64 dims, 128-byte swizzle
+constexpr int kSlab = kTileBytes / 2;
+constexpr int kStages = 4;
+constexpr float kLift = 8.f, kLazy = 6.f;
+constexpr int kMinShare = 4;                       // key tiles of a block's share, at least
+
+constexpr int kSlotRows = 256;
+constexpr size_t kSlotBytes = static_cast<size_t>(kSlotRows) * (kD + 2) * 4 + 256;   // O, m, l, flag
+constexpr int kDescInts = 8;
+
+constexpr int kOffQ = 0;
+constexpr int kOffRing = 2 * kTileBytes;
+constexpr int kOffBars = kOffRing + kStages * kTileBytes;
+constexpr int kOffMl = kOffBars + 256;             // float [2][128]: m, l of group 1 for group 0
+constexpr int kOffMisc = kOffMl + 2 * 128 * 4;     // ints
+constexpr int kOffSeq = kOffMisc + 128;            // int [4][batch] + 1: first tile, new tokens, length, first row
+
+size_t prompt_smem_bytes(int batch) { return 1024 + kOffSeq + (4 * static_cast<size_t>(batch) + 1) * 4; }
 
 struct PromptArgs {
     Rows rows;
@@ -152,12 +207,21 @@ struct PromptArgs {
     uint16_t* out;
     int q_stride, out_stride, G;
     int window, sinks;               // window 0: none
-    float sl2;                       // scale * log2(e)
+    float sl2;                       // |scale| * log2(e), not 0
+    uint32_t neg;                    // kIdescNegA for a negative scale
+    int box;                         // cache rows of one copy: a page's, or the part of it that divides a tile
+    int stall;                       // test hook: no key or value is copied
+    int32_t* desc;                   // [grid][kDescInts] items to join
+    uint8_t* slots;                  // [2 * grid] partial results
     uint32_t* err;
 };
 
+struct PromptMaps {
+    CUtensorMap q, k, v;
+};
+
 // One row and query head by one warp, a token at a time, four dimensions a lane.
-__device__ void attend_row(const PromptArgs& a, int b, int pos, int row, int head)
+__device__ __noinline__ void attend_row(const PromptArgs& a, int b, int pos, int row, int head)
 {
     const int lane = threadIdx.x & 31, h = head / a.G;
     const int cap = a.c.stride * a.c.page_size;
@@ -203,17 +267,734 @@ __device__ void attend_row(const PromptArgs& a, int b, int pos, int row, int hea
     *reinterpret_cast<uint2*>(a.out + static_cast<size_t>(row) * a.out_stride + head * kD + 4 * lane) = w;
 }
 
-__global__ void __launch_bounds__(256) prompt_attn_kernel(const PromptArgs a)
+// What the rows at positions [pf, pl] of one item see, in tiles of 128 keys: tile
+// i of its list is tile i of the sequence, or i + gap from `front` on.
+struct Seen {
+    int pf, pl, tiles, front, gap;
+    __device__ __forceinline__ int token0(int i) const { return (i < front ? i : i + gap) * kKeys; }
+};
+
+__device__ __forceinline__ Seen seen_by(int pf, int pl, int cap, int window, int sinks)
 {
+    Seen s;
+    s.pf = pf;
+    s.pl = min(pl, cap - 1);
+    const int all = s.pl >= 0 ? s.pl / kKeys + 1 : 0;
+    s.front = s.gap = 0;
+    if (window) {
+        s.front = min((min(sinks, max(s.pl, -1) + 1) + kKeys - 1) / kKeys, all);
+        s.gap = max(0, min(max(0, pf - window + 1) / kKeys, all) - s.front);
+    }
+    s.tiles = max(1, all - s.gap);               // an item without keys still writes its zeros
+    return s;
+}
+
+// The batch as every block sees it, in shared memory.
+struct Seqs {
+    const int* pre;          // [batch + 1] key tiles of one head before sequence b
+    const int* n;            // new tokens
+    const int* len;
+    const int* row0;
+};
+
+// A block's walk over its share [g, end) of the flattened list.
+struct Walk {
+    int g, end, b, h, qt, is;      // is: where the present item begins
+};
+
+struct Piece {
+    Seen seen;
+    int t0, t1;                    // its tiles
+    int b, h, row0, ntok;          // first row of the batch, tokens
+    bool first, dual;              // the share's first piece; both groups on one row tile
+    __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == seen.tiles; }
+};
+
+__device__ __forceinline__ Seen item_seen(const PromptArgs& a, const Seqs& s, int b, int qt, int tt)
+{
+    const int pf = s.len[b] - s.n[b] + qt * tt;
+    return seen_by(pf, pf + min(tt, s.n[b] - qt * tt) - 1, a.c.stride * a.c.page_size, a.window, a.sinks);
+}
+
+__device__ __forceinline__ bool next_piece(const PromptArgs& a, const Seqs& s, int g_begin, Walk& w, Piece& p)
+{
+    if (w.g >= w.end) return false;
+    const int tok = kKeys / a.G, tt = 2 * tok;
+    p.seen = item_seen(a, s, w.b, w.qt, tt);
+    p.b = w.b;
+    p.h = w.h;
+    p.row0 = s.row0[w.b] + w.qt * tt;
+    p.ntok = min(tt, s.n[w.b] - w.qt * tt);
+    p.dual = p.ntok <= tok;
+    p.first = w.g == g_begin;
+    p.t0 = w.g - w.is;
+    p.t1 = min(p.seen.tiles, w.end - w.is);
+    w.g = w.is + p.t1;
+    if (p.t1 == p.seen.tiles) {
+        w.is = w.g;
+        if (++w.qt * tt >= s.n[w.b]) {
+            w.qt = 0;
+            if (++w.h == a.c.Hkv) {
+                w.h = 0;
+                do ++w.b;
+                while (w.b < a.rows.batch && s.n[w.b] == 0);
+            }
+        }
+    }
+    return true;
+}
+
+// Where piece-local key tile i of the group's k-th turn lies: group w of a dual
+// item takes every other tile.
+__device__ __forceinline__ int turns(const Piece& p, int w)
+{
+    const int nt = p.t1 - p.t0;
+    return p.dual ? (nt + 1 - w) / 2 : nt;
+}
+
+__device__ __forceinline__ int turn_tile(const Piece& p, int w, int k) { return p.t0 + (p.dual ? 2 * k + w : k); }
+
+// Whether the rows at [pf, pl] see every key of the tile at t0; end: the last token of the cache.
+__device__ __forceinline__ bool sees_all(int t0, int pf, int pl, int end, int window, int sinks)
+{
+    return t0 + kKeys - 1 <= min(pf, end) && (!window || t0 > pl - window || t0 + kKeys <= sinks);
+}
+
+struct Ring {
+    int slot = 0;
+    uint32_t par = 0;
+    __device__ __forceinline__ void next(int by = 1)
+    {
+        slot += by;
+        if (slot >= kStages) {
+            slot -= kStages;
+            par ^= 1u;
+        }
+    }
+};
+
+// Values read from tensor memory are used from here on, not before: the wait names
+// no registers, so the uses would not be ordered behind it.
+template <int N>
+__device__ __forceinline__ void pin(uint32_t* v)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+r"(v[i]));
+}
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
+__device__ __forceinline__ uint64_t pair(float lo, float hi)
+{
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+    return d;
+}
+
+__device__ __forceinline__ void unpair(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+__device__ __forceinline__ uint32_t half2_bits(float lo, float hi)
+{
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Whether any of the eight fp16 values is an infinity or a NaN (exponent all ones).
+__device__ __forceinline__ bool not_finite(uint4 v)
+{
+    auto f = [](uint32_t x) { return ((x & 0x7C007C00u) + 0x04000400u) & 0x80008000u; };
+    return (f(v.x) | f(v.y) | f(v.z) | f(v.w)) != 0u;
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+    prompt_attn_kernel(const __grid_constant__ PromptMaps maps, const __grid_constant__ PromptArgs a)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + kOffBars);   // key or value tile landed
+    uint64_t* empty = full + kStages;                                // ... read by its MMAs
+    uint64_t* fixed = empty + kStages;                               // value tile looked over
+    uint64_t* qfull = fixed + kStages;
+    uint64_t* qempty = qfull + 2;
+    uint64_t* sfull = qempty + 2;                                    // scores of a row tile written
+    uint64_t* pfull = sfull + 2;                                     // ... weights
+    uint64_t* ofull = pfull + 2;                                     // ... output of a piece
+    uint64_t* drain = ofull + 2;
+    float* ml = reinterpret_cast<float*>(smem + kOffMl);
+    volatile int* misc = reinterpret_cast<volatile int*>(smem + kOffMisc);   // [0..5] walk, [6] tmem, [8..11] pieces with a value that is not finite
+    int* seq = reinterpret_cast<int*>(smem + kOffSeq);
+    const int batch = a.rows.batch;
+    int* pre = seq;
+    int* sn = pre + batch + 1;
+    int* slen = sn + batch;
+    int* srow = slen + batch;
+    const Seqs S = {pre, sn, slen, srow};
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int cap = a.c.stride * a.c.page_size;
+    const int tok = kKeys / a.G, tt = 2 * tok;
+    uint32_t* err = a.err;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+            mbar_init(&fixed[i], 2);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&qfull[i], 1);
+            mbar_init(&qempty[i], 1);
+            mbar_init(&sfull[i], 1);
+            mbar_init(&pfull[i], 4);
+            mbar_init(&ofull[i], 1);
+        }
+        mbar_init(drain, 1);
+        mbar_fence_init();
+        for (int i = 8; i < 12; ++i) misc[i] = 0;
+    }
+    if (warp == kCopyWarp && lane == 0) {
+        tc::prefetch_map(&maps.q);
+        tc::prefetch_map(&maps.k);
+        tc::prefetch_map(&maps.v);
+    }
+    grid_dependency_wait();              // every input may come from the previous kernel
+    grid_dependents_launch();
+
+    // the sequences' rows, lengths and key tiles; their prefix
+    for (int b = warp; b < batch; b += kThreads / 32) {
+        const int s = min(max(__ldg(a.rows.starts + b), 0), a.rows.rows);
+        const int n = min(max(__ldg(a.rows.starts + b + 1), s), a.rows.rows) - s;
+        const int L = max(__ldg(a.rows.lens + b), 0);
+        if (lane == 0) {
+            sn[b] = n;
+            slen[b] = L;
+            srow[b] = s;
+            if (n > 0 && L > cap && blockIdx.x == 0) atomicOr(err, kErrSeqLen);
+        }
+        __syncwarp();
+        int tiles = 0;
+        for (int qt = lane; qt * tt < n; qt += 32) tiles += item_seen(a, S, b, qt, tt).tiles;
+        tiles = __reduce_add_sync(0xffffffffu, tiles);
+        if (lane == 0) pre[b] = tiles;
+    }
+    __syncthreads();
+    if (warp == 0) {
+        int carry = 0;
+        for (int b0 = 0; b0 < batch; b0 += 32) {
+            const int v = b0 + lane < batch ? pre[b0 + lane] : 0;
+            int incl = v;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int u = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += u;
+            }
+            if (b0 + lane < batch) pre[b0 + lane] = carry + incl - v;
+            carry += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        if (lane == 0) pre[batch] = carry;
+        __syncwarp();
+        const int total = a.c.Hkv * carry, grid = static_cast<int>(gridDim.x);
+        const int R = max((total + grid - 1) / grid, kMinShare);
+        const int g = min(static_cast<int64_t>(total), static_cast<int64_t>(blockIdx.x) * R);
+        if (g < total) {
+            int lo = 0, hi = batch - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (a.c.Hkv * pre[mid] <= g) lo = mid;
+                else hi = mid - 1;
+            }
+            const int of_head = pre[lo + 1] - pre[lo];
+            const int h = (g - a.c.Hkv * pre[lo]) / of_head;
+            int at = a.c.Hkv * pre[lo] + h * of_head, qt = 0;
+            for (int q0 = 0;; q0 += 32) {       // ends: g lies within this head's tiles
+                const int v = (q0 + lane) * tt < sn[lo] ? item_seen(a, S, lo, q0 + lane, tt).tiles : 0;
+                int incl = v;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int u = __shfl_up_sync(0xffffffffu, incl, o);
+                    if (lane >= o) incl += u;
+                }
+                const uint32_t past = __ballot_sync(0xffffffffu, at + incl > g);
+                if (past || (q0 + 32) * tt >= sn[lo]) {
+                    const int l = past ? __ffs(past) - 1 : 31;
+                    qt = q0 + l;
+                    at += __shfl_sync(0xffffffffu, incl - v, l);
+                    break;
+                }
+                at += __shfl_sync(0xffffffffu, incl, 31);
+            }
+            if (lane == 0) {
+                misc[2] = lo;
+                misc[3] = h;
+                misc[4] = qt;
+                misc[5] = at;
+            }
+        }
+        if (lane == 0) {
+            misc[0] = g;
+            misc[1] = min(static_cast<int64_t>(total), static_cast<int64_t>(g) + R);
+            misc[7] = R;
+        }
+    }
+    __syncthreads();
+    const int g_begin = misc[0];
+    Walk walk = {g_begin, misc[1], misc[2], misc[3], misc[4], misc[5]};
+    const int R = misc[7];
+    int32_t* desc = a.desc + static_cast<size_t>(blockIdx.x) * kDescInts;
+    if (walk.g >= walk.end) {            // more blocks than shares
+        if (threadIdx.x == 0) desc[0] = 0;
+        return;
+    }
+    if (warp == kMmaWarp) tc::tmem_alloc(const_cast<uint32_t*>(reinterpret_cast<volatile uint32_t*>(misc + 6)), 512);
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    const uint32_t tbase = static_cast<uint32_t>(misc[6]);
+    // tensor memory: scores (and weights over them) of row tile w at 128 w, output at 256 + 128 w
+
+    // After a wait gave up (bounded, flagged) a role waits no more but goes on
+    // through every tile with every arrival, so that no other is left behind; the
+    // copies stop and are waited for.
+    Piece p;
+    if (warp == kCopyWarp) {
+        // ------------------------------------------------------------ copies
+        Ring ring;
+        int issued = 0, nq[2] = {0, 0};
+        bool ok = true;
+        const int boxes = kKeys / a.box;
+        const uint32_t qbytes = static_cast<uint32_t>(a.G * tok) * 128u * 2u;
+        auto tile = [&](const Piece& pc, const int32_t* table, int i, bool value) {
+            if (issued >= kStages && ok) ok = mbar_wait(&empty[ring.slot], ring.par ^ 1u, err);
+            if (!ok) return;
+            uint8_t* dst = smem + kOffRing + ring.slot * kTileBytes;
+            if (lane == 0) mbar_arrive_expect_tx(&full[ring.slot], kTileBytes);
+            __syncwarp();
+            if (lane < 2 * boxes) {
+                // a lane a box and half; boxes without a visible token, or on a page outside the
+                // pool, lie wholly outside the tensor: the copy reads zeros
+                const int t = pc.seen.token0(i) + (lane >> 1) * a.box;
+                const bool needed = t <= pc.seen.pl && (!a.window || t < a.sinks || t + a.box - 1 > pc.seen.pf - a.window);
+                int y = -a.box;
+                if (needed) {
+                    const int page = __ldg(table + t / a.c.page_size);
+                    if (page >= 0 && page < a.c.num_pages) y = (page * a.c.Hkv + pc.h) * a.c.page_size + t % a.c.page_size;
+                    else atomicOr(err, kErrPageId);
+                }
+                tc::tma_load_2d(dst + (lane & 1) * kSlab + (lane >> 1) * a.box * 128, value ? &maps.v : &maps.k, 64 * (lane & 1), y,
+                                &full[ring.slot]);
+            }
+            ++issued;
+            ring.next();
+        };
+        while (ok && a.stall == 0) {
+            if (!next_piece(a, S, g_begin, walk, p)) break;
+            const int32_t* table = a.c.table + static_cast<size_t>(p.b) * a.c.stride;
+            for (int i = p.t0; i < p.t1 && ok; ++i) {
+                tile(p, table, i, false);
+                if (i == p.t0)
+                    for (int w = 0; w < (p.dual ? 1 : 2) && ok; ++w) {
+                        if (nq[w] >= 1) ok = mbar_wait(&qempty[w], (nq[w] - 1) & 1, err);
+                        if (!ok) break;
+                        if (lane == 0) {
+                            mbar_arrive_expect_tx(&qfull[w], qbytes);
+                            for (int s = 0; s < 2; ++s)
+                                tc::tma_load_3d(smem + kOffQ + w * kTileBytes + s * kSlab, &maps.q, 64 * s, p.h * a.G, p.row0 + w * tok,
+                                                &qfull[w]);
+                        }
+                        ++nq[w];
+                    }
+                tile(p, table, i, true);
+            }
+        }
+        // every copy issued has landed before the block's memory goes away
+        for (int i = max(0, issued - kStages); i < issued; ++i) mbar_wait(&full[i % kStages], (i / kStages) & 1, err);
+        for (int w = 0; w < 2; ++w)
+            if (nq[w]) mbar_wait(&qfull[w], (nq[w] - 1) & 1, err);
+    } else if (warp == kMmaWarp) {
+        // -------------------------------------------------------- MMA issuer
+        // Units alternate between the groups; the scores of the unit after next are
+        // issued behind the weights x values of the present one, whose weights they
+        // overwrite (MMAs run in the order of issue).
+        const uint32_t idesc_s = tc::idesc_f16_f32(128, kKeys) | a.neg;
+        const uint32_t idesc_o = tc::idesc_f16_f32(128, kD) | tc::kIdescTransB;
+        const bool leader = tc::elect_one();
+        const uint64_t qdesc = tc::sw128_kmajor_desc(smem_addr(smem + kOffQ));
+        const uint64_t kdesc = tc::sw128_kmajor_desc(smem_addr(smem + kOffRing));
+        const uint64_t vdesc = tc::sw128_mnmajor_desc(smem_addr(smem + kOffRing), kSlab);
+        Ring kr, vr;                     // the next key tile, the next value tile
+        vr.slot = 1;
+        uint32_t qpar[2] = {0, 0}, ppar[2] = {0, 0};
+        bool ok = true;
+        while (next_piece(a, S, g_begin, walk, p)) {
+            const int nt = p.t1 - p.t0, units = p.dual ? nt : 2 * nt;
+            auto scores = [&](int u) {
+                const int w = u & 1;
+                const bool news = p.dual || w == 0, last = p.dual || w == 1;     // first / last to read the key tile
+                if (u < 2 && (w == 0 || !p.dual)) {
+                    if (ok) ok = mbar_wait(&qfull[w], qpar[w], err);
+                    qpar[w] ^= 1u;
+                }
+                if (news && ok) ok = mbar_wait(&full[kr.slot], kr.par, err);
+                tc::fence_after_sync();
+                if (leader) {
+                    const uint64_t qd = qdesc + static_cast<uint64_t>(p.dual ? 0 : w) * (kTileBytes >> 4);
+                    const uint64_t kd = kdesc + static_cast<uint64_t>(kr.slot) * (kTileBytes >> 4);
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) {
+                        const uint64_t step = (s >> 2) * (kSlab >> 4) + (s & 3) * 2;
+                        tc::mma_f16_ss(tbase + 128 * w, qd + step, kd + step, idesc_s, s > 0 ? 1u : 0u);
+                    }
+                    if (last) tc::commit(&empty[kr.slot]);
+                    if (p.dual ? u == units - 1 : u >= units - 2) tc::commit(&qempty[p.dual ? 0 : w]);
+                    tc::commit(&sfull[w]);
+                }
+                if (last) kr.next(2);
+            };
+            scores(0);
+            if (units > 1) scores(1);
+            for (int u = 0; u < units; ++u) {
+                const int w = u & 1;
+                if (ok) ok = mbar_wait(&fixed[vr.slot], vr.par, err);
+                if (ok) ok = mbar_wait(&pfull[w], ppar[w], err);
+                ppar[w] ^= 1u;
+                tc::fence_after_sync();
+                if (leader) {
+                    const uint64_t vd = vdesc + static_cast<uint64_t>(vr.slot) * (kTileBytes >> 4);
+#pragma unroll
+                    for (int s = 0; s < 8; ++s)
+                        tc::mma_f16_ts(tbase + 256 + 128 * w, tbase + 128 * w + 8 * s, vd + s * (2048 >> 4), idesc_o, u > 1 || s > 0 ? 1u : 0u);
+                    if (p.dual || w == 1) tc::commit(&empty[vr.slot]);
+                    if (u >= units - 2) tc::commit(&ofull[w]);
+                }
+                if (p.dual || w == 1) vr.next(2);
+                if (u + 2 < units) scores(u + 2);
+            }
+        }
+        if (leader) tc::commit(drain);   // all MMAs have completed before tensor memory is released
+        mbar_wait(drain, 0, err);
+    } else if (warp >= kValueWarp) {
+        // ---------------------------------------------------- masked values
+        Ring vr;
+        vr.slot = 1;
+        bool ok = true;
+        for (int seqno = 1; next_piece(a, S, g_begin, walk, p); ++seqno) {
+            for (int i = p.t0; i < p.t1; ++i) {
+                if (ok) ok = mbar_wait(&full[vr.slot], vr.par, err);
+                __syncwarp();
+                const int t0 = p.seen.token0(i);
+                if (!sees_all(t0, p.seen.pf, p.seen.pl, p.seen.pl, a.window, a.sinks)) {
+                    uint8_t* base = smem + kOffRing + vr.slot * kTileBytes;
+                    bool bad = false;
+                    // 8 lanes a row of a slab, 64 rows a warp
+                    for (int e = lane; e < 64 * 16; e += 32) {
+                        const int row = (warp - kValueWarp) * 64 + (e >> 4), t = t0 + row;
+                        uint4* at = reinterpret_cast<uint4*>(base + ((e >> 3) & 1) * kSlab + row * 128) + (e & 7);
+                        if (t > p.seen.pl || (a.window && t <= p.seen.pf - a.window && t >= a.sinks)) *at = make_uint4(0, 0, 0, 0);
+                        else bad |= not_finite(*at);
+                    }
+                    if (__any_sync(0xffffffffu, bad) && lane == 0) misc[8 + (seqno & 3)] = seqno;
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                }
+                if (lane == 0) mbar_arrive(&fixed[vr.slot]);
+                vr.next(2);
+            }
+        }
+        // the item that this share's end cuts, and does not begin in an earlier one: who joins it finds it here
+        if (warp == kValueWarp && lane == 0) {
+            const bool head = p.t0 == 0 && !p.whole();
+            desc[0] = head ? (walk.is + p.seen.tiles - 1) / R - static_cast<int>(blockIdx.x) + 1 : 0;
+            desc[1] = p.b;
+            desc[2] = p.h;
+            desc[3] = p.row0;
+            desc[4] = p.ntok;
+            desc[5] = p.seen.pf;
+            desc[6] = 2 * static_cast<int>(blockIdx.x) + (p.first ? 0 : 1);
+        }
+    } else {
+        // ------------------------------------------------------------ softmax
+        const int w = warp >> 2, row = 32 * (warp & 3) + lane;
+        const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16;
+        const uint32_t ts = tbase + 128 * w + lanes, to = tbase + 256 + 128 * w + lanes;
+        const int rtok = row / a.G, rhead = row - rtok * a.G;
+        uint32_t spar = 0, opar = 0;
+        bool ok = true;
+        for (int seqno = 1; next_piece(a, S, g_begin, walk, p); ++seqno) {
+            const int base = p.dual ? 0 : w * tok;            // first token of the group's row tile
+            const int pos = p.seen.pf + base + rtok;
+            const int pf = p.seen.pf + base, pl = min(pf + tok, p.seen.pf + p.ntok) - 1;
+            const int nk = turns(p, w);
+            float m = -INFINITY;
+            uint64_t l2 = pair(0.f, 0.f);
+            for (int k = 0; k < nk; ++k) {
+                if (ok) ok = mbar_wait(&sfull[w], spar, err);
+                spar ^= 1u;
+                __syncwarp();
+                tc::fence_after_sync();
+                uint32_t s[128];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tc::ld32(ts + 32 * c, s + 32 * c);
+                tc::ld_wait();
+                pin<128>(s);
+                const int t0 = p.seen.token0(turn_tile(p, w, k));
+                if (!sees_all(t0, pf, pl, p.seen.pl, a.window, a.sinks)) {
+                    const int hi = min(pos, p.seen.pl) - t0, lo = a.window ? pos - a.window - t0 : -1, sk = a.window ? a.sinks - t0 : 0;
+#pragma unroll
+                    for (int c = 0; c < 128; ++c)
+                        if (c > hi || (c <= lo && c >= sk)) s[c] = 0xFF800000u;      // -infinity
+                }
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int c = 0; c < 128; c += 8)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], __uint_as_float(s[c + 2 * i]), __uint_as_float(s[c + 2 * i + 1]));
+                const float mnew = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * a.sl2;
+                const bool up = mnew > m + kLazy;
+                const float mref = up ? mnew : m;
+                const float ms = mref == -INFINITY ? 0.f : mref;
+                const float alpha = up ? ex2(m - ms) : 1.f;
+                m = mref;
+                const uint64_t sl = pair(a.sl2, a.sl2), off = pair(kLift - ms, kLift - ms);
+                l2 = fma2(l2, pair(alpha, alpha), pair(0.f, 0.f));
+                uint32_t pk[64];
+                uint64_t sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
+#pragma unroll
+                for (int c = 0; c < 64; ++c) {
+                    const uint64_t x = fma2(pair(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), sl, off);
+                    float x0, x1;
+                    unpair(x, x0, x1);
+                    x0 = ex2(x0);
+                    x1 = ex2(x1);
+                    sum[c & 1] = add2(sum[c & 1], pair(x0, x1));
+                    pk[c] = half2_bits(x0, x1);
+                }
+                l2 = add2(l2, add2(sum[0], sum[1]));
+                tc::st32(ts, pk);
+                tc::st32(ts + 32, pk + 32);
+                if (k > 0 && __any_sync(0xffffffffu, up)) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t o[32];
+                        tc::ld32(to + 32 * c, o);
+                        tc::ld_wait();
+                        pin<32>(o);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                        tc::st32(to + 32 * c, o);
+                    }
+                }
+                tc::st_wait();
+                tc::fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&pfull[w]);
+            }
+            float l, lh;
+            unpair(l2, l, lh);
+            l += lh;
+            if (nk > 0) {
+                if (ok) ok = mbar_wait(&ofull[w], opar, err);
+                opar ^= 1u;
+                __syncwarp();
+                tc::fence_after_sync();
+            }
+            // factors of this group's output and, in a dual item, of the other's (same lanes)
+            float f0 = 1.f, f1 = 0.f;
+            const bool joined = p.dual && turns(p, 1) > 0;
+            if (joined) {
+                if (w == 1) {
+                    ml[row] = m;
+                    ml[128 + row] = l;
+                }
+                named_barrier_sync(1, 256);
+                if (w == 0) {
+                    const float m1 = ml[row], M = fmaxf(m, m1), Ms = M == -INFINITY ? 0.f : M;
+                    f0 = ex2(m - Ms);
+                    f1 = ex2(m1 - Ms);
+                    l = l * f0 + ml[128 + row] * f1;
+                    m = M;
+                }
+            }
+            if (!p.dual || w == 0) {
+                const bool slow = misc[8 + (seqno & 3)] == seqno;
+                const bool valid = rtok < tok && base + rtok < p.ntok;
+                if (p.whole() && slow) {
+                    for (int i = 0; i < 32; ++i) {
+                        const int r = 32 * (warp & 3) + i, rt = r / a.G;
+                        if (rt < tok && base + rt < p.ntok)
+                            attend_row(a, p.b, p.seen.pf + base + rt, p.row0 + base + rt, p.h * a.G + r - rt * a.G);
+                    }
+                } else {
+                    const float inv = l == 0.f ? 0.f : 1.f / l;
+                    if (p.whole()) {
+                        f0 *= inv;
+                        f1 *= inv;
+                    }
+                    const int slot = 2 * static_cast<int>(blockIdx.x) + (p.first ? 0 : 1);
+                    uint8_t* part = a.slots + static_cast<size_t>(slot) * kSlotBytes;
+                    uint16_t* orow = a.out + static_cast<size_t>(p.row0 + base + (valid ? rtok : 0)) * a.out_stride +
+                                     static_cast<size_t>(p.h * a.G + rhead) * kD;
+                    const int prow = w * 128 + row;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t o[32];
+                        tc::ld32(to + 32 * c, o);
+                        if (joined) {
+                            uint32_t o1[32];
+                            tc::ld32(to + 128 + 32 * c, o1);
+                            tc::ld_wait();
+                            pin<32>(o);
+                            pin<32>(o1);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                o[i] = __float_as_uint(__uint_as_float(o[i]) * f0 + __uint_as_float(o1[i]) * f1);
+                        } else {
+                            tc::ld_wait();
+                            pin<32>(o);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f0);
+                        }
+                        if (p.whole()) {
+                            if (valid)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    uint4 v;
+                                    v.x = half2_bits(__uint_as_float(o[8 * i]), __uint_as_float(o[8 * i + 1]));
+                                    v.y = half2_bits(__uint_as_float(o[8 * i + 2]), __uint_as_float(o[8 * i + 3]));
+                                    v.z = half2_bits(__uint_as_float(o[8 * i + 4]), __uint_as_float(o[8 * i + 5]));
+                                    v.w = half2_bits(__uint_as_float(o[8 * i + 6]), __uint_as_float(o[8 * i + 7]));
+                                    reinterpret_cast<uint4*>(orow)[4 * c + i] = v;
+                                }
+                        } else if (valid) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                reinterpret_cast<uint4*>(part)[(8 * c + i) * kSlotRows + prow] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                        }
+                    }
+                    if (!p.whole()) {
+                        float* mlp = reinterpret_cast<float*>(part + static_cast<size_t>(kSlotRows) * kD * 4);
+                        mlp[prow] = m;
+                        mlp[kSlotRows + prow] = l;
+                        if (warp == 0 && lane == 0) reinterpret_cast<int*>(mlp + 2 * kSlotRows)[0] = slow ? 1 : 0;
+                    }
+                }
+            }
+            if (joined) named_barrier_sync(1, 256);      // group 1's output and m, l are read
+            tc::fence_before_sync();
+        }
+    }
+
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    if (warp == kMmaWarp) tc::tmem_dealloc(tbase, 512);
+}
+
+// Joins the parts of the items that shares cut, in their order: a block 32 rows
+// of one item, a lane a row, a warp 16 of the 128 dimensions.
+constexpr int kMaxGrid = 256;
+
+__global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs a)
+{
+    __shared__ float sm[8][32], sl[8][32];
+    __shared__ __align__(16) uint16_t tile[32][kD + 8];
     grid_dependency_wait();
     grid_dependents_launch();
-    const int Hq = a.G * a.c.Hkv;
-    const int64_t item = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-    if (item >= static_cast<int64_t>(a.rows.rows) * Hq) return;
-    const int row = static_cast<int>(item / Hq), head = static_cast<int>(item % Hq);
-    int pos;
-    const int b = row_owner(a.rows, row, &pos);
-    if (b >= 0) attend_row(a, b, pos, row, head);
+    const int32_t* desc = a.desc + static_cast<size_t>(blockIdx.x) * kDescInts;
+    const int parts = __ldcg(desc);
+    if (parts < 2) return;
+    const int b = __ldcg(desc + 1), h = __ldcg(desc + 2), row0 = __ldcg(desc + 3), ntok = __ldcg(desc + 4), pf = __ldcg(desc + 5);
+    const int slot0 = __ldcg(desc + 6), slot1 = 2 * static_cast<int>(blockIdx.x) + 2;    // the following ones: 2 apart
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int tok = kKeys / a.G;
+    auto place = [&](int r, int& token) {          // row of the item -> its token; whether there is one
+        const int rt = (r & 127) / a.G;
+        token = (r >> 7) * tok + rt;
+        return rt < tok && token < ntok;
+    };
+    const int r0 = 32 * blockIdx.y;
+    int token;
+    const bool valid = place(r0 + lane, token);
+    if (!__syncthreads_or(valid)) return;
+    auto part = [&](int i) { return a.slots + static_cast<size_t>(i == 0 ? slot0 : slot1 + 2 * (i - 1)) * kSlotBytes; };
+    auto stats = [&](int i) { return reinterpret_cast<const float*>(part(i) + static_cast<size_t>(kSlotRows) * kD * 4); };
+    int slow = 0;
+    float M = -INFINITY, L = 0.f;
+    for (int i = warp; i < parts; i += 8) {
+        const float m = valid ? __ldcg(stats(i) + r0 + lane) : 0.f, l = valid ? __ldcg(stats(i) + kSlotRows + r0 + lane) : 0.f;
+        slow |= __ldcg(reinterpret_cast<const int*>(stats(i) + 2 * kSlotRows));
+        const float Mn = fmaxf(M, m), Ms = Mn == -INFINITY ? 0.f : Mn;
+        L = L * ex2(M - Ms) + l * ex2(m - Ms);
+        M = Mn;
+    }
+    sm[warp][lane] = M;
+    sl[warp][lane] = L;
+    if (__syncthreads_or(slow)) {
+        for (int i = 4 * warp; i < 4 * warp + 4; ++i) {
+            const int r = r0 + i;
+            int t;
+            if (place(r, t)) attend_row(a, b, pf + t, row0 + t, h * a.G + (r & 127) % a.G);
+        }
+        return;
+    }
+    M = -INFINITY;
+    L = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) M = fmaxf(M, sm[w][lane]);
+    const float Ms = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) L = fmaf(sl[w][lane], ex2(sm[w][lane] - Ms), L);
+    float4 acc[4] = {};
+#pragma unroll 4
+    for (int i = 0; i < parts; ++i) {
+        const float f = valid ? ex2(__ldcg(stats(i) + r0 + lane) - Ms) : 0.f;
+        const float4* o = reinterpret_cast<const float4*>(part(i)) + (4 * warp) * kSlotRows + r0 + lane;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const float4 v = valid ? __ldcg(o + c * kSlotRows) : make_float4(0.f, 0.f, 0.f, 0.f);
+            acc[c].x = fmaf(v.x, f, acc[c].x);
+            acc[c].y = fmaf(v.y, f, acc[c].y);
+            acc[c].z = fmaf(v.z, f, acc[c].z);
+            acc[c].w = fmaf(v.w, f, acc[c].w);
+        }
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<uint2*>(&tile[lane][16 * warp + 4 * c]) =
+            make_uint2(half2_bits(acc[c].x * inv, acc[c].y * inv), half2_bits(acc[c].z * inv, acc[c].w * inv));
+    __syncthreads();
+    for (int e = threadIdx.x; e < 32 * 16; e += 256) {
+        const int r = r0 + (e >> 4);
+        int t;
+        if (place(r, t))
+            reinterpret_cast<uint4*>(a.out + static_cast<size_t>(row0 + t) * a.out_stride + (h * a.G + (r & 127) % a.G) * kD)[e & 15] =
+                reinterpret_cast<const uint4*>(tile[e >> 4])[e & 15];
+    }
 }
 
 // ------------------------------------------------------------------- host --
@@ -250,8 +1031,8 @@ size_t rows_bytes(int rows, int stride, int width)
     return (static_cast<size_t>(rows - 1) * stride + width) * 2;
 }
 
-template <typename Args>
-int launch(void (*kernel)(Args), dim3 grid, int threads, void* stream, const Args& args)
+template <typename... Params, typename... Args>
+int launch(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, void* stream, const Args&... args)
 {
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -259,11 +1040,28 @@ int launch(void (*kernel)(Args), dim3 grid, int threads, void* stream, const Arg
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = static_cast<cudaStream_t>(stream);
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args) == cudaSuccess ? WQ4_OK : WQ4_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? WQ4_OK : WQ4_ERR_CUDA;
 }
+
+// The attention kernel's limit of shared memory, set once on each device (twice is harmless).
+bool prompt_ready(int dev)
+{
+    static std::atomic<bool> ready[kMaxDevices];
+    if (dev < kMaxDevices && ready[dev].load()) return true;
+    if (cudaFuncSetAttribute(prompt_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(prompt_smem_bytes(WQ4_ATTN_MAX_BATCH))) != cudaSuccess)
+        return false;
+    if (dev < kMaxDevices) ready[dev].store(true);
+    return true;
+}
+
+size_t prompt_desc_bytes(int grid) { return align_up(static_cast<size_t>(grid) * kDescInts * 4, 256); }
+
+int prompt_grid(const DeviceInfo* di) { return std::min(di->sm_count, kMaxGrid); }
 
 }  // namespace
 }  // namespace wq4
@@ -302,7 +1100,7 @@ extern "C" int wq4_prompt_append(const wq4_kv_cache* cache, const uint16_t* qkv,
     a.err = status_word();
     if (!a.err) return WQ4_ERR_CUDA;
     for (int i = 0; i < kD / 2; ++i) a.inv_freq[i] = rotate ? std::pow(rope_theta, -2.0 * i / kD) : 0.0;
-    return launch(prompt_append_kernel, dim3((rows + kAppRows - 1) / kAppRows), kAppThreads, stream, a);
+    return launch(prompt_append_kernel, dim3((rows + kAppRows - 1) / kAppRows), kAppThreads, 0, stream, a);
 }
 
 extern "C" size_t wq4_prompt_attention_workspace_bytes(int batch, int rows, int n_q_heads, int n_kv_heads, int head_dim)
@@ -310,7 +1108,11 @@ extern "C" size_t wq4_prompt_attention_workspace_bytes(int batch, int rows, int 
     if (batch < 1 || batch > WQ4_ATTN_MAX_BATCH || rows < 1 || n_kv_heads < 1 || n_q_heads < n_kv_heads ||
         n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > kMaxGroup || head_dim != kD)
         return 0;
-    return 256;
+    int dev = 0;
+    const DeviceInfo* di = current_device_info(&dev);
+    if (!di) return 0;
+    const int grid = prompt_grid(di);
+    return prompt_desc_bytes(grid) + 2 * static_cast<size_t>(grid) * kSlotBytes;
 }
 
 extern "C" int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_stride, const int32_t* row_starts,
@@ -332,17 +1134,45 @@ extern "C" int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q
     if (overlaps(out, ob, cache->k, cb) || overlaps(out, ob, cache->v, cb) || overlaps(out, ob, workspace, need) ||
         overlaps(out, ob, q, rows_bytes(rows, q_stride, width)))
         return WQ4_ERR_INVALID;
+    const int Hkv = cache->n_kv_heads, G = n_q_heads / Hkv, tok = kKeys / G;
+    const int cap = cache->page_table_stride * cache->page_size;
+    // the list of key tiles is indexed in int
+    const int64_t items = static_cast<int64_t>(Hkv) * ((rows + 2 * tok - 1) / (2 * tok) + batch);
+    const int64_t most = items * (cap / kKeys + 1);
+    if (most >= (int64_t(1) << 31)) return WQ4_ERR_UNSUPPORTED;
+    int dev = 0;
+    const DeviceInfo* di = current_device_info(&dev);
+    if (!di || !prompt_ready(dev)) return WQ4_ERR_CUDA;
+    const int grid = static_cast<int>(std::min<int64_t>(prompt_grid(di), (most + kMinShare - 1) / kMinShare));
     a.q = q;
     a.out = out;
     a.q_stride = q_stride;
     a.out_stride = out_stride;
-    a.G = n_q_heads / cache->n_kv_heads;
-    a.window = window;
-    a.sinks = n_sinks;
-    a.sl2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
+    a.G = G;
+    a.window = window < cap ? window : 0;        // a window that no sequence can outgrow hides nothing
+    a.sinks = std::min(n_sinks, cap);
+    a.sl2 = static_cast<float>(std::fabs(static_cast<double>(scale)) * 1.4426950408889634);
+    if (a.sl2 < FLT_MIN) a.sl2 = FLT_MIN;        // every weight alike, and masked scores still -infinity
+    a.neg = scale < 0.f ? tc::kIdescNegA : 0u;
+    a.box = 16;
+    while (a.box < kKeys && cache->page_size % (2 * a.box) == 0) a.box *= 2;
+    a.stall = test_copy_stall() == WQ4_STALL_PROMPT ? 1 : 0;
+    a.desc = static_cast<int32_t*>(workspace);
+    a.slots = static_cast<uint8_t*>(workspace) + prompt_desc_bytes(prompt_grid(di));
     a.err = status_word();
     if (!a.err) return WQ4_ERR_CUDA;
-    const int64_t items = static_cast<int64_t>(rows) * n_q_heads;
-    if (items >= (int64_t(1) << 33)) return WQ4_ERR_UNSUPPORTED;
-    return launch(prompt_attn_kernel, dim3(static_cast<unsigned>((items + 7) / 8)), 256, stream, a);
+    PromptMaps maps;
+    const uint64_t crows = static_cast<uint64_t>(cache->num_pages) * Hkv * cache->page_size;
+    if (!encode_tensor_map_2d(&maps.k, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, cache->k, kD, crows, kD * 2, 64, a.box,
+                              CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !encode_tensor_map_2d(&maps.v, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, cache->v, kD, crows, kD * 2, 64, a.box,
+                              CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !encode_tensor_map_3d(&maps.q, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, q,
+                              {kD, static_cast<uint64_t>(n_q_heads), static_cast<uint64_t>(rows)},
+                              {kD * 2, static_cast<uint64_t>(q_stride) * 2},
+                              {64, static_cast<uint32_t>(G), static_cast<uint32_t>(tok)}, CU_TENSOR_MAP_SWIZZLE_128B))
+        return WQ4_ERR_CUDA;
+    const int r = launch(prompt_attn_kernel, dim3(grid), kThreads, prompt_smem_bytes(batch), stream, maps, a);
+    if (r != WQ4_OK || grid == 1) return r;      // one block cuts nothing
+    return launch(prompt_join_kernel, dim3(grid - 1, kSlotRows / 32), 256, 0, stream, a);
 }
