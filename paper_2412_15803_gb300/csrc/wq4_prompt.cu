@@ -13,8 +13,10 @@
 #include <algorithm>
 #include <atomic>
 #include <cfloat>
+#include <climits>
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 
 namespace wq4 {
 namespace {
@@ -160,7 +162,8 @@ __global__ void __launch_bounds__(kAppThreads) prompt_append_kernel(const __grid
 // unnormalised output in fp32) that a second kernel joins in their order.
 //
 // Warps: 0-3 and 4-7 the softmax of row tiles 0 and 1 (a thread a row), 8 the MMA
-// issuer, 9 the copies, 10 and 11 what masks do to values (below).  Scores S =
+// issuer, 9 and 10 the copies of queries and keys and of values, 11 what masks do
+// to values (below).  Scores S =
 // Q K^T of 128 x 128 go to tensor memory, one thread reads its row's 128, takes
 // the maximum and writes the weights as fp16 over the scores; O += P V reads
 // them there.  While one row tile's softmax runs, the tensor cores work for the
@@ -179,13 +182,18 @@ __global__ void __launch_bounds__(kAppThreads) prompt_append_kernel(const __grid
 // one by one, without the tokens they do not see (attend_row).
 
 constexpr int kThreads = 384;
-constexpr int kMmaWarp = 8, kCopyWarp = 9, kValueWarp = 10;
+constexpr int kMmaWarp = 8, kKeyWarp = 9, kValueWarp = 10, kMaskWarp = 11;
+// Registers a thread: the softmax groups take over what the other four warps leave
+// of the launch's 384 x 168.
+constexpr int kRegsLaunch = 168, kRegsSoftmax = 208, kRegsOther = 80;
+static_assert(256 * kRegsSoftmax + 128 * kRegsOther <= kThreads * kRegsLaunch, "registers");
 constexpr int kKeys = 128;                         // keys of a tile
 constexpr int kTileBytes = kKeys * kD * 2;         // Q, K and V tiles: two slabs of 64 dims, 128-byte swizzle
 constexpr int kSlab = kTileBytes / 2;
-constexpr int kStages = 4;
+constexpr int kStages = 2;                         // of keys, and of values
 constexpr float kLift = 8.f, kLazy = 6.f;
-constexpr int kMinShare = 4;                       // key tiles of a block's share, at least
+constexpr int kItem = 2;                           // an item's own cost, in key tiles
+constexpr int kMinShare = 4;                       // places of a block's share, at least: more than kItem
 
 constexpr int kSlotRows = 256;
 constexpr size_t kSlotBytes = static_cast<size_t>(kSlotRows) * (kD + 2) * 4 + 256;   // O, m, l, flag
@@ -193,10 +201,10 @@ constexpr int kDescInts = 8;
 
 constexpr int kOffQ = 0;
 constexpr int kOffRing = 2 * kTileBytes;
-constexpr int kOffBars = kOffRing + kStages * kTileBytes;
+constexpr int kOffBars = kOffRing + 2 * kStages * kTileBytes;
 constexpr int kOffMl = kOffBars + 256;             // float [2][128]: m, l of group 1 for group 0
 constexpr int kOffMisc = kOffMl + 2 * 128 * 4;     // ints
-constexpr int kOffSeq = kOffMisc + 128;            // int [4][batch] + 1: first tile, new tokens, length, first row
+constexpr int kOffSeq = kOffMisc + 160;            // int [4][batch] + 1: first tile, new tokens, length, first row
 
 size_t prompt_smem_bytes(int batch) { return 1024 + kOffSeq + (4 * static_cast<size_t>(batch) + 1) * 4; }
 
@@ -210,6 +218,7 @@ struct PromptArgs {
     float sl2;                       // |scale| * log2(e), not 0
     uint32_t neg;                    // kIdescNegA for a negative scale
     int box;                         // cache rows of one copy: a page's, or the part of it that divides a tile
+    int wide;                        // output rows are 32-byte aligned
     int stall;                       // test hook: no key or value is copied
     int32_t* desc;                   // [grid][kDescInts] items to join
     uint8_t* slots;                  // [2 * grid] partial results
@@ -297,7 +306,9 @@ struct Seqs {
     const int* row0;
 };
 
-// A block's walk over its share [g, end) of the flattened list.
+// A block's walk over its share [g, end) of the flattened list.  An item takes
+// kItem places before its tiles' (what beginning and ending one costs), so that
+// shares with many short items are no longer than others.
 struct Walk {
     int g, end, b, h, qt, is;      // is: where the present item begins
 };
@@ -320,16 +331,22 @@ __device__ __forceinline__ bool next_piece(const PromptArgs& a, const Seqs& s, i
 {
     if (w.g >= w.end) return false;
     const int tok = kKeys / a.G, tt = 2 * tok;
-    p.seen = item_seen(a, s, w.b, w.qt, tt);
+    const Seen seen = item_seen(a, s, w.b, w.qt, tt);
+    const int t0 = max(0, w.g - w.is - kItem), t1 = min(seen.tiles, w.end - w.is - kItem);
+    if (t1 <= t0) {                      // the share ends before the item's first tile; p stays the last piece
+        w.g = w.end;
+        return false;
+    }
+    p.seen = seen;
+    p.t0 = t0;
+    p.t1 = t1;
     p.b = w.b;
     p.h = w.h;
     p.row0 = s.row0[w.b] + w.qt * tt;
     p.ntok = min(tt, s.n[w.b] - w.qt * tt);
     p.dual = p.ntok <= tok;
     p.first = w.g == g_begin;
-    p.t0 = w.g - w.is;
-    p.t1 = min(p.seen.tiles, w.end - w.is);
-    w.g = w.is + p.t1;
+    w.g = w.is + kItem + p.t1;
     if (p.t1 == p.seen.tiles) {
         w.is = w.g;
         if (++w.qt * tt >= s.n[w.b]) {
@@ -363,11 +380,10 @@ __device__ __forceinline__ bool sees_all(int t0, int pf, int pl, int end, int wi
 struct Ring {
     int slot = 0;
     uint32_t par = 0;
-    __device__ __forceinline__ void next(int by = 1)
+    __device__ __forceinline__ void next()
     {
-        slot += by;
-        if (slot >= kStages) {
-            slot -= kStages;
+        if (++slot == kStages) {
+            slot = 0;
             par ^= 1u;
         }
     }
@@ -425,11 +441,29 @@ __device__ __forceinline__ uint32_t half2_bits(float lo, float hi)
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Whether any of the eight fp16 values is an infinity or a NaN (exponent all ones).
-__device__ __forceinline__ bool not_finite(uint4 v)
+// The lowest n bits (none for n <= 0, all for n >= 32).
+__device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? 0xFFFFFFFFu : (1u << max(n, 0)) - 1u; }
+
+__device__ __forceinline__ __half2 as_half2(uint32_t v) { return *reinterpret_cast<const __half2*>(&v); }
+
+// Whether either of the two is an infinity or a NaN (exponent all ones).
+__device__ __forceinline__ bool not_finite(__half2 v)
 {
-    auto f = [](uint32_t x) { return ((x & 0x7C007C00u) + 0x04000400u) & 0x80008000u; };
-    return (f(v.x) | f(v.y) | f(v.z) | f(v.w)) != 0u;
+    const uint32_t x = *reinterpret_cast<const uint32_t*>(&v);
+    return (x & 0x7C00u) == 0x7C00u || (x & 0x7C000000u) == 0x7C000000u;
+}
+
+// 32 bytes by one thread (p 32-byte aligned).
+__device__ __forceinline__ void store32(void* p, const uint32_t v[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+
+__device__ __forceinline__ int* slot_flag(const PromptArgs& a, int slot)
+{
+    return reinterpret_cast<int*>(a.slots + static_cast<size_t>(slot) * kSlotBytes + static_cast<size_t>(kSlotRows) * (kD + 2) * 4);
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
@@ -437,9 +471,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + kOffBars);   // key or value tile landed
-    uint64_t* empty = full + kStages;                                // ... read by its MMAs
-    uint64_t* fixed = empty + kStages;                               // value tile looked over
+    uint64_t* kfull = reinterpret_cast<uint64_t*>(smem + kOffBars);  // key tile landed
+    uint64_t* kempty = kfull + kStages;                              // ... read by its MMAs
+    uint64_t* vfull = kempty + kStages;
+    uint64_t* vempty = vfull + kStages;
+    uint64_t* fixed = vempty + kStages;                              // value tile looked over
     uint64_t* qfull = fixed + kStages;
     uint64_t* qempty = qfull + 2;
     uint64_t* sfull = qempty + 2;                                    // scores of a row tile written
@@ -447,7 +483,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint64_t* ofull = pfull + 2;                                     // ... output of a piece
     uint64_t* drain = ofull + 2;
     float* ml = reinterpret_cast<float*>(smem + kOffMl);
-    volatile int* misc = reinterpret_cast<volatile int*>(smem + kOffMisc);   // [0..5] walk, [6] tmem, [8..11] pieces with a value that is not finite
+    volatile int* misc = reinterpret_cast<volatile int*>(smem + kOffMisc);   // [0..5] walk, [6] tmem, [7] share
+    uint32_t* again = reinterpret_cast<uint32_t*>(smem + kOffMisc + 32);     // a bit a piece (modulo 1024) whose rows are computed again
     int* seq = reinterpret_cast<int*>(smem + kOffSeq);
     const int batch = a.rows.batch;
     int* pre = seq;
@@ -462,9 +499,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
-            mbar_init(&full[i], 1);
-            mbar_init(&empty[i], 1);
-            mbar_init(&fixed[i], 2);
+            mbar_init(&kfull[i], 1);
+            mbar_init(&kempty[i], 1);
+            mbar_init(&vfull[i], 1);
+            mbar_init(&vempty[i], 1);
+            mbar_init(&fixed[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&qfull[i], 1);
@@ -475,9 +514,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         mbar_init(drain, 1);
         mbar_fence_init();
-        for (int i = 8; i < 12; ++i) misc[i] = 0;
     }
-    if (warp == kCopyWarp && lane == 0) {
+    if (threadIdx.x < 32) again[threadIdx.x] = 0;
+    if (warp == kKeyWarp && lane == 0) {
         tc::prefetch_map(&maps.q);
         tc::prefetch_map(&maps.k);
         tc::prefetch_map(&maps.v);
@@ -498,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         __syncwarp();
         int tiles = 0;
-        for (int qt = lane; qt * tt < n; qt += 32) tiles += item_seen(a, S, b, qt, tt).tiles;
+        for (int qt = lane; qt * tt < n; qt += 32) tiles += item_seen(a, S, b, qt, tt).tiles + kItem;
         tiles = __reduce_add_sync(0xffffffffu, tiles);
         if (lane == 0) pre[b] = tiles;
     }
@@ -532,7 +571,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int h = (g - a.c.Hkv * pre[lo]) / of_head;
             int at = a.c.Hkv * pre[lo] + h * of_head, qt = 0;
             for (int q0 = 0;; q0 += 32) {       // ends: g lies within this head's tiles
-                const int v = (q0 + lane) * tt < sn[lo] ? item_seen(a, S, lo, q0 + lane, tt).tiles : 0;
+                const int v = (q0 + lane) * tt < sn[lo] ? item_seen(a, S, lo, q0 + lane, tt).tiles + kItem : 0;
                 int incl = v;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
@@ -581,42 +620,54 @@ __global__ void __launch_bounds__(kThreads, 1)
     // through every tile with every arrival, so that no other is left behind; the
     // copies stop and are waited for.
     Piece p;
-    if (warp == kCopyWarp) {
+    if (warp >= kMmaWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
+    if (warp == kKeyWarp || warp == kValueWarp) {
         // ------------------------------------------------------------ copies
+        const bool keys = warp == kKeyWarp;
+        uint64_t* const full = keys ? kfull : vfull;
+        uint64_t* const empty = keys ? kempty : vempty;
+        uint8_t* const tiles = smem + kOffRing + (keys ? 0 : kStages * kTileBytes);
+        const CUtensorMap* const map = keys ? &maps.k : &maps.v;
         Ring ring;
         int issued = 0, nq[2] = {0, 0};
         bool ok = true;
         const int boxes = kKeys / a.box;
         const uint32_t qbytes = static_cast<uint32_t>(a.G * tok) * 128u * 2u;
-        auto tile = [&](const Piece& pc, const int32_t* table, int i, bool value) {
+        // A lane a box and half.  Boxes without a visible token, or on a page outside the
+        // pool, lie wholly outside the tensor: the copy reads zeros.  The next tile's
+        // page ids are under way while this one's copies are issued.
+        constexpr int kHidden = INT_MIN;
+        auto lookup = [&](const int32_t* table, int i) {
+            const int t = p.seen.token0(i) + (lane >> 1) * a.box;
+            const bool needed = lane < 2 * boxes && t <= p.seen.pl && (!a.window || t < a.sinks || t + a.box - 1 > p.seen.pf - a.window);
+            return needed ? __ldg(table + t / a.c.page_size) : kHidden;
+        };
+        auto tile = [&](int y) {
             if (issued >= kStages && ok) ok = mbar_wait(&empty[ring.slot], ring.par ^ 1u, err);
             if (!ok) return;
-            uint8_t* dst = smem + kOffRing + ring.slot * kTileBytes;
+            uint8_t* dst = tiles + ring.slot * kTileBytes;
             if (lane == 0) mbar_arrive_expect_tx(&full[ring.slot], kTileBytes);
             __syncwarp();
-            if (lane < 2 * boxes) {
-                // a lane a box and half; boxes without a visible token, or on a page outside the
-                // pool, lie wholly outside the tensor: the copy reads zeros
-                const int t = pc.seen.token0(i) + (lane >> 1) * a.box;
-                const bool needed = t <= pc.seen.pl && (!a.window || t < a.sinks || t + a.box - 1 > pc.seen.pf - a.window);
-                int y = -a.box;
-                if (needed) {
-                    const int page = __ldg(table + t / a.c.page_size);
-                    if (page >= 0 && page < a.c.num_pages) y = (page * a.c.Hkv + pc.h) * a.c.page_size + t % a.c.page_size;
-                    else atomicOr(err, kErrPageId);
-                }
-                tc::tma_load_2d(dst + (lane & 1) * kSlab + (lane >> 1) * a.box * 128, value ? &maps.v : &maps.k, 64 * (lane & 1), y,
-                                &full[ring.slot]);
-            }
+            if (lane < 2 * boxes)
+                tc::tma_load_2d(dst + (lane & 1) * kSlab + (lane >> 1) * a.box * 128, map, 64 * (lane & 1), y, &full[ring.slot]);
             ++issued;
             ring.next();
         };
         while (ok && a.stall == 0) {
             if (!next_piece(a, S, g_begin, walk, p)) break;
             const int32_t* table = a.c.table + static_cast<size_t>(p.b) * a.c.stride;
+            int page = lookup(table, p.t0);
             for (int i = p.t0; i < p.t1 && ok; ++i) {
-                tile(p, table, i, false);
-                if (i == p.t0)
+                const int next = i + 1 < p.t1 ? lookup(table, i + 1) : kHidden;
+                int y = -a.box;
+                if (page >= 0 && page < a.c.num_pages)
+                    y = (page * a.c.Hkv + p.h) * a.c.page_size + (p.seen.token0(i) + (lane >> 1) * a.box) % a.c.page_size;
+                else if (page != kHidden)
+                    atomicOr(err, kErrPageId);
+                page = next;
+                tile(y);
+                if (keys && i == p.t0)
                     for (int w = 0; w < (p.dual ? 1 : 2) && ok; ++w) {
                         if (nq[w] >= 1) ok = mbar_wait(&qempty[w], (nq[w] - 1) & 1, err);
                         if (!ok) break;
@@ -628,7 +679,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         ++nq[w];
                     }
-                tile(p, table, i, true);
             }
         }
         // every copy issued has landed before the block's memory goes away
@@ -640,103 +690,171 @@ __global__ void __launch_bounds__(kThreads, 1)
         // Units alternate between the groups; the scores of the unit after next are
         // issued behind the weights x values of the present one, whose weights they
         // overwrite (MMAs run in the order of issue).
+        // The loop's numbers come through a shuffle: warp-uniform for the compiler too,
+        // without which each MMA's operands pass through vector registers.
         const uint32_t idesc_s = tc::idesc_f16_f32(128, kKeys) | a.neg;
         const uint32_t idesc_o = tc::idesc_f16_f32(128, kD) | tc::kIdescTransB;
+        const uint32_t tb = __shfl_sync(0xffffffffu, tbase, 0);
         const bool leader = tc::elect_one();
         const uint64_t qdesc = tc::sw128_kmajor_desc(smem_addr(smem + kOffQ));
         const uint64_t kdesc = tc::sw128_kmajor_desc(smem_addr(smem + kOffRing));
-        const uint64_t vdesc = tc::sw128_mnmajor_desc(smem_addr(smem + kOffRing), kSlab);
+        const uint64_t vdesc = tc::sw128_mnmajor_desc(smem_addr(smem + kOffRing + kStages * kTileBytes), kSlab);
         Ring kr, vr;                     // the next key tile, the next value tile
-        vr.slot = 1;
         uint32_t qpar[2] = {0, 0}, ppar[2] = {0, 0};
         bool ok = true;
-        while (next_piece(a, S, g_begin, walk, p)) {
-            const int nt = p.t1 - p.t0, units = p.dual ? nt : 2 * nt;
-            auto scores = [&](int u) {
-                const int w = u & 1;
-                const bool news = p.dual || w == 0, last = p.dual || w == 1;     // first / last to read the key tile
-                if (u < 2 && (w == 0 || !p.dual)) {
-                    if (ok) ok = mbar_wait(&qfull[w], qpar[w], err);
-                    qpar[w] ^= 1u;
-                }
-                if (news && ok) ok = mbar_wait(&full[kr.slot], kr.par, err);
-                tc::fence_after_sync();
-                if (leader) {
-                    const uint64_t qd = qdesc + static_cast<uint64_t>(p.dual ? 0 : w) * (kTileBytes >> 4);
-                    const uint64_t kd = kdesc + static_cast<uint64_t>(kr.slot) * (kTileBytes >> 4);
-#pragma unroll
-                    for (int s = 0; s < 8; ++s) {
-                        const uint64_t step = (s >> 2) * (kSlab >> 4) + (s & 3) * 2;
-                        tc::mma_f16_ss(tbase + 128 * w, qd + step, kd + step, idesc_s, s > 0 ? 1u : 0u);
-                    }
-                    if (last) tc::commit(&empty[kr.slot]);
-                    if (p.dual ? u == units - 1 : u >= units - 2) tc::commit(&qempty[p.dual ? 0 : w]);
-                    tc::commit(&sfull[w]);
-                }
-                if (last) kr.next(2);
-            };
-            scores(0);
-            if (units > 1) scores(1);
-            for (int u = 0; u < units; ++u) {
-                const int w = u & 1;
-                if (ok) ok = mbar_wait(&fixed[vr.slot], vr.par, err);
-                if (ok) ok = mbar_wait(&pfull[w], ppar[w], err);
-                ppar[w] ^= 1u;
-                tc::fence_after_sync();
-                if (leader) {
-                    const uint64_t vd = vdesc + static_cast<uint64_t>(vr.slot) * (kTileBytes >> 4);
-#pragma unroll
-                    for (int s = 0; s < 8; ++s)
-                        tc::mma_f16_ts(tbase + 256 + 128 * w, tbase + 128 * w + 8 * s, vd + s * (2048 >> 4), idesc_o, u > 1 || s > 0 ? 1u : 0u);
-                    if (p.dual || w == 1) tc::commit(&empty[vr.slot]);
-                    if (u >= units - 2) tc::commit(&ofull[w]);
-                }
-                if (p.dual || w == 1) vr.next(2);
-                if (u + 2 < units) scores(u + 2);
+        auto scores = [&](auto group, bool dual, bool first, bool last) {      // first, last: of this piece for its Q tile
+            constexpr int w = decltype(group)::value;
+            if (first && (w == 0 || !dual)) {
+                if (ok) ok = mbar_wait(&qfull[w], qpar[w], err);
+                qpar[w] ^= 1u;
             }
+            if ((w == 0 || dual) && ok) ok = mbar_wait(&kfull[kr.slot], kr.par, err);
+            tc::fence_after_sync();
+            if (leader) {
+                const uint64_t qd = qdesc + (w == 0 || dual ? 0u : kTileBytes >> 4);
+                const uint64_t kd = kdesc + kr.slot * (kTileBytes >> 4);
+#pragma unroll
+                for (int s = 0; s < 8; ++s) {
+                    const uint64_t step = (s >> 2) * (kSlab >> 4) + (s & 3) * 2;
+                    tc::mma_f16_ss(tb + 128 * w, qd + step, kd + step, idesc_s, s > 0 ? 1u : 0u);
+                }
+                tc::commit(&sfull[w]);
+                if (w == 1 || dual) tc::commit(&kempty[kr.slot]);
+                if (last) tc::commit(&qempty[dual ? 0 : w]);
+            }
+            if (w == 1 || dual) kr.next();
+        };
+        auto values = [&](auto group, bool dual, bool first, bool last) {
+            constexpr int w = decltype(group)::value;
+            if ((w == 0 || dual) && ok) ok = mbar_wait(&fixed[vr.slot], vr.par, err);
+            if (ok) ok = mbar_wait(&pfull[w], ppar[w], err);
+            ppar[w] ^= 1u;
+            tc::fence_after_sync();
+            if (leader) {
+                const uint64_t vd = vdesc + vr.slot * (kTileBytes >> 4);
+#pragma unroll
+                for (int s = 0; s < 8; ++s)
+                    tc::mma_f16_ts(tb + 256 + 128 * w, tb + 128 * w + 8 * s, vd + s * (2048 >> 4), idesc_o, s > 0 || !first ? 1u : 0u);
+                if (last) tc::commit(&ofull[w]);
+                if (w == 1 || dual) tc::commit(&vempty[vr.slot]);
+            }
+            if (w == 1 || dual) vr.next();
+        };
+        using G0 = std::integral_constant<int, 0>;
+        using G1 = std::integral_constant<int, 1>;
+        struct Turns {
+            int nt, n0, n1;              // tiles of the piece, turns of the groups
+            bool dual;
+        };
+        auto fetch = [&](Turns& x) {
+            const int more = next_piece(a, S, g_begin, walk, p) ? 1 : 0;
+            if (!__shfl_sync(0xffffffffu, more, 0)) return false;
+            x.nt = __shfl_sync(0xffffffffu, p.t1 - p.t0, 0);
+            x.dual = __shfl_sync(0xffffffffu, p.dual ? 1 : 0, 0) != 0;
+            x.n0 = x.dual ? (x.nt + 1) / 2 : x.nt;
+            x.n1 = x.dual ? x.nt / 2 : x.nt;
+            return true;
+        };
+        auto first0 = [&](const Turns& x) { scores(G0{}, x.dual, true, x.nt == 1); };
+        auto first1 = [&](const Turns& x) {
+            if (x.n1 > 0) scores(G1{}, x.dual, true, x.dual ? x.nt == 2 : x.nt == 1);
+        };
+        // The next piece's first scores are issued behind a group's last values, where
+        // the groups end in their order; so its softmax finds them when its output is stored.
+        Turns x, next;
+        bool have = fetch(x);
+        if (have) {
+            first0(x);
+            first1(x);
+        }
+        while (have) {
+            const bool hn = fetch(next), even = x.n0 == x.n1;
+            for (int k = 0; k < x.n0; ++k) {
+                values(G0{}, x.dual, k == 0, k == x.n0 - 1);
+                if (k + 1 < x.n0) scores(G0{}, x.dual, false, x.dual ? 2 * k + 3 == x.nt : k + 2 == x.nt);
+                else if (hn && even) first0(next);
+                if (k < x.n1) {
+                    values(G1{}, x.dual, k == 0, k == x.n1 - 1);
+                    if (k + 1 < x.n1) scores(G1{}, x.dual, false, x.dual ? 2 * k + 4 == x.nt : k + 2 == x.nt);
+                    else if (hn && even) first1(next);
+                }
+            }
+            if (hn && !even) {
+                first0(next);
+                first1(next);
+            }
+            x = next;
+            have = hn;
         }
         if (leader) tc::commit(drain);   // all MMAs have completed before tensor memory is released
         mbar_wait(drain, 0, err);
-    } else if (warp >= kValueWarp) {
+    } else if (warp == kMaskWarp) {
         // ---------------------------------------------------- masked values
         Ring vr;
-        vr.slot = 1;
         bool ok = true;
-        for (int seqno = 1; next_piece(a, S, g_begin, walk, p); ++seqno) {
+        for (int piece = 0; next_piece(a, S, g_begin, walk, p); ++piece) {
             for (int i = p.t0; i < p.t1; ++i) {
-                if (ok) ok = mbar_wait(&full[vr.slot], vr.par, err);
+                if (ok) ok = mbar_wait(&vfull[vr.slot], vr.par, err);
                 __syncwarp();
-                const int t0 = p.seen.token0(i);
-                if (!sees_all(t0, p.seen.pf, p.seen.pl, p.seen.pl, a.window, a.sinks)) {
-                    uint8_t* base = smem + kOffRing + vr.slot * kTileBytes;
-                    bool bad = false;
-                    // 8 lanes a row of a slab, 64 rows a warp
-                    for (int e = lane; e < 64 * 16; e += 32) {
-                        const int row = (warp - kValueWarp) * 64 + (e >> 4), t = t0 + row;
-                        uint4* at = reinterpret_cast<uint4*>(base + ((e >> 3) & 1) * kSlab + row * 128) + (e & 7);
-                        if (t > p.seen.pl || (a.window && t <= p.seen.pf - a.window && t >= a.sinks)) *at = make_uint4(0, 0, 0, 0);
-                        else bad |= not_finite(*at);
+                const int t0 = p.seen.token0(i), pf = p.seen.pf, pl = p.seen.pl;
+                if (!sees_all(t0, pf, pl, pl, a.window, a.sinks)) {
+                    uint8_t* base = smem + kOffRing + (kStages + vr.slot) * kTileBytes + ((lane >> 3) & 1) * kSlab + (lane & 7) * 16;
+                    __half2 big = __float2half2_rn(0.f);
+                    auto clip = [&](int tkn) { return min(max(tkn - t0, 0), kKeys); };
+                    // [from, to) of the tile's rows: 16 lanes a row
+                    auto zero = [&](int from, int to) {
+                        for (int r = clip(from) + (lane >> 4); r < clip(to); r += 2)
+                            *reinterpret_cast<uint4*>(base + r * 128) = make_uint4(0, 0, 0, 0);
+                    };
+                    auto look = [&](int from, int to) {        // the largest size, NaN above all
+                        const int f = clip(from), e = clip(to);
+                        for (int r = f + (lane >> 4); r - (lane >> 4) < e; r += 16) {
+                            uint4 x[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const uint4*>(base + min(r + 2 * j, e - 1) * 128);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                big = __hmax2_nan(big, __hmax2_nan(__habs2(as_half2(x[j].x)), __habs2(as_half2(x[j].y))));
+                                big = __hmax2_nan(big, __hmax2_nan(__habs2(as_half2(x[j].z)), __habs2(as_half2(x[j].w))));
+                            }
+                        }
+                    };
+                    // Seen by no row: behind pl, and between the sinks and pf - window (whole boxes
+                    // there were copied as zeros).  Seen by some: from pf on, and up to pl - window.
+                    zero(pl + 1, (pl / a.box + 1) * a.box);
+                    look(max(pf, -1) + 1, pl + 1);
+                    if (a.window) {
+                        const int gone = pf - a.window + 1;    // the first token that the window shows
+                        if (gone > a.sinks) {
+                            zero(a.sinks, min(gone, (a.sinks + a.box - 1) / a.box * a.box));
+                            zero(max(a.sinks, gone / a.box * a.box), gone);
+                        }
+                        look(max(a.sinks, gone), min(pl - a.window, pf) + 1);
                     }
-                    if (__any_sync(0xffffffffu, bad) && lane == 0) misc[8 + (seqno & 3)] = seqno;
+                    if (__any_sync(0xffffffffu, not_finite(big)) && lane == 0) atomicOr(&again[(piece >> 5) & 31], 1u << (piece & 31));
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                 }
                 if (lane == 0) mbar_arrive(&fixed[vr.slot]);
-                vr.next(2);
+                vr.next();
             }
         }
         // the item that this share's end cuts, and does not begin in an earlier one: who joins it finds it here
-        if (warp == kValueWarp && lane == 0) {
+        if (lane == 0) {
             const bool head = p.t0 == 0 && !p.whole();
-            desc[0] = head ? (walk.is + p.seen.tiles - 1) / R - static_cast<int>(blockIdx.x) + 1 : 0;
+            desc[0] = head ? (walk.is + kItem + p.seen.tiles - 1) / R - static_cast<int>(blockIdx.x) + 1 : 0;
             desc[1] = p.b;
             desc[2] = p.h;
             desc[3] = p.row0;
             desc[4] = p.ntok;
             desc[5] = p.seen.pf;
             desc[6] = 2 * static_cast<int>(blockIdx.x) + (p.first ? 0 : 1);
+            for (int i = 0; i < 2; ++i) *slot_flag(a, 2 * blockIdx.x + i) = 0;
         }
+    }
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsLaunch));
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
         // ------------------------------------------------------------ softmax
         const int w = warp >> 2, row = 32 * (warp & 3) + lane;
         const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16;
@@ -744,7 +862,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int rtok = row / a.G, rhead = row - rtok * a.G;
         uint32_t spar = 0, opar = 0;
         bool ok = true;
-        for (int seqno = 1; next_piece(a, S, g_begin, walk, p); ++seqno) {
+        while (next_piece(a, S, g_begin, walk, p)) {
             const int base = p.dual ? 0 : w * tok;            // first token of the group's row tile
             const int pos = p.seen.pf + base + rtok;
             const int pf = p.seen.pf + base, pl = min(pf + tok, p.seen.pf + p.ntok) - 1;
@@ -763,10 +881,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                 pin<128>(s);
                 const int t0 = p.seen.token0(turn_tile(p, w, k));
                 if (!sees_all(t0, pf, pl, p.seen.pl, a.window, a.sinks)) {
-                    const int hi = min(pos, p.seen.pl) - t0, lo = a.window ? pos - a.window - t0 : -1, sk = a.window ? a.sinks - t0 : 0;
+                    // a bit a key: those up to hi, less those from sk to lo
+                    const int hi = min(pos, p.seen.pl) - t0 + 1, lo = a.window ? pos - a.window - t0 + 1 : 0, sk = a.window ? a.sinks - t0 : 0;
 #pragma unroll
-                    for (int c = 0; c < 128; ++c)
-                        if (c > hi || (c <= lo && c >= sk)) s[c] = 0xFF800000u;      // -infinity
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t see = first_bits(hi - 32 * c) & (~first_bits(lo - 32 * c) | first_bits(sk - 32 * c));
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) s[32 * c + i] = see & (1u << i) ? s[32 * c + i] : 0xFF800000u;   // -infinity
+                    }
                 }
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -780,7 +902,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float alpha = up ? ex2(m - ms) : 1.f;
                 m = mref;
                 const uint64_t sl = pair(a.sl2, a.sl2), off = pair(kLift - ms, kLift - ms);
-                l2 = fma2(l2, pair(alpha, alpha), pair(0.f, 0.f));
                 uint32_t pk[64];
                 uint64_t sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
 #pragma unroll
@@ -793,7 +914,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     sum[c & 1] = add2(sum[c & 1], pair(x0, x1));
                     pk[c] = half2_bits(x0, x1);
                 }
-                l2 = add2(l2, add2(sum[0], sum[1]));
+                l2 = fma2(l2, pair(alpha, alpha), add2(sum[0], sum[1]));
                 tc::st32(ts, pk);
                 tc::st32(ts + 32, pk + 32);
                 if (k > 0 && __any_sync(0xffffffffu, up)) {
@@ -840,78 +961,88 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
             if (!p.dual || w == 0) {
-                const bool slow = misc[8 + (seqno & 3)] == seqno;
                 const bool valid = rtok < tok && base + rtok < p.ntok;
-                if (p.whole() && slow) {
-                    for (int i = 0; i < 32; ++i) {
-                        const int r = 32 * (warp & 3) + i, rt = r / a.G;
-                        if (rt < tok && base + rt < p.ntok)
-                            attend_row(a, p.b, p.seen.pf + base + rt, p.row0 + base + rt, p.h * a.G + r - rt * a.G);
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                if (p.whole()) {
+                    f0 *= inv;
+                    f1 *= inv;
+                }
+                const int slot = 2 * static_cast<int>(blockIdx.x) + (p.first ? 0 : 1);
+                uint8_t* part = a.slots + static_cast<size_t>(slot) * kSlotBytes;
+                uint16_t* orow = a.out + static_cast<size_t>(p.row0 + base + (valid ? rtok : 0)) * a.out_stride +
+                                 static_cast<size_t>(p.h * a.G + rhead) * kD;
+                const int prow = w * 128 + row;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t o[32];
+                    tc::ld32(to + 32 * c, o);
+                    if (joined) {
+                        uint32_t o1[32];
+                        tc::ld32(to + 128 + 32 * c, o1);
+                        tc::ld_wait();
+                        pin<32>(o);
+                        pin<32>(o1);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            o[i] = __float_as_uint(__uint_as_float(o[i]) * f0 + __uint_as_float(o1[i]) * f1);
+                    } else {
+                        tc::ld_wait();
+                        pin<32>(o);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f0);
                     }
-                } else {
-                    const float inv = l == 0.f ? 0.f : 1.f / l;
                     if (p.whole()) {
-                        f0 *= inv;
-                        f1 *= inv;
-                    }
-                    const int slot = 2 * static_cast<int>(blockIdx.x) + (p.first ? 0 : 1);
-                    uint8_t* part = a.slots + static_cast<size_t>(slot) * kSlotBytes;
-                    uint16_t* orow = a.out + static_cast<size_t>(p.row0 + base + (valid ? rtok : 0)) * a.out_stride +
-                                     static_cast<size_t>(p.h * a.G + rhead) * kD;
-                    const int prow = w * 128 + row;
+                        uint32_t v[16];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t o[32];
-                        tc::ld32(to + 32 * c, o);
-                        if (joined) {
-                            uint32_t o1[32];
-                            tc::ld32(to + 128 + 32 * c, o1);
-                            tc::ld_wait();
-                            pin<32>(o);
-                            pin<32>(o1);
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                o[i] = __float_as_uint(__uint_as_float(o[i]) * f0 + __uint_as_float(o1[i]) * f1);
-                        } else {
-                            tc::ld_wait();
-                            pin<32>(o);
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f0);
-                        }
-                        if (p.whole()) {
-                            if (valid)
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    uint4 v;
-                                    v.x = half2_bits(__uint_as_float(o[8 * i]), __uint_as_float(o[8 * i + 1]));
-                                    v.y = half2_bits(__uint_as_float(o[8 * i + 2]), __uint_as_float(o[8 * i + 3]));
-                                    v.z = half2_bits(__uint_as_float(o[8 * i + 4]), __uint_as_float(o[8 * i + 5]));
-                                    v.w = half2_bits(__uint_as_float(o[8 * i + 6]), __uint_as_float(o[8 * i + 7]));
-                                    reinterpret_cast<uint4*>(orow)[4 * c + i] = v;
-                                }
+                        for (int i = 0; i < 16; ++i) v[i] = half2_bits(__uint_as_float(o[2 * i]), __uint_as_float(o[2 * i + 1]));
+                        if (valid && a.wide) {
+                            store32(orow + 32 * c, v);
+                            store32(orow + 32 * c + 16, v + 8);
                         } else if (valid) {
 #pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                reinterpret_cast<uint4*>(part)[(8 * c + i) * kSlotRows + prow] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                            for (int i = 0; i < 4; ++i)
+                                reinterpret_cast<uint4*>(orow)[4 * c + i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                         }
+                    } else if (valid) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            reinterpret_cast<uint4*>(part)[(8 * c + i) * kSlotRows + prow] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                     }
-                    if (!p.whole()) {
-                        float* mlp = reinterpret_cast<float*>(part + static_cast<size_t>(kSlotRows) * kD * 4);
-                        mlp[prow] = m;
-                        mlp[kSlotRows + prow] = l;
-                        if (warp == 0 && lane == 0) reinterpret_cast<int*>(mlp + 2 * kSlotRows)[0] = slow ? 1 : 0;
-                    }
+                }
+                if (!p.whole()) {
+                    float* mlp = reinterpret_cast<float*>(part + static_cast<size_t>(kSlotRows) * kD * 4);
+                    mlp[prow] = m;
+                    mlp[kSlotRows + prow] = l;
                 }
             }
             if (joined) named_barrier_sync(1, 256);      // group 1's output and m, l are read
             tc::fence_before_sync();
         }
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsLaunch));
     }
 
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
     if (warp == kMmaWarp) tc::tmem_dealloc(tbase, 512);
+
+    // Rows beside masked values that are not finite, once more: not inside the
+    // pipeline, whose waits are bounded.  (A piece that shares its bit with such a
+    // one is computed again as well, to the same effect.)
+    uint32_t some = again[lane];
+    if (!__any_sync(0xffffffffu, some != 0u)) return;
+    walk = {g_begin, misc[1], misc[2], misc[3], misc[4], misc[5]};
+    for (int piece = 0; next_piece(a, S, g_begin, walk, p); ++piece) {
+        if (!(again[(piece >> 5) & 31] >> (piece & 31) & 1u)) continue;
+        if (!p.whole()) {
+            if (threadIdx.x == 0) *slot_flag(a, 2 * static_cast<int>(blockIdx.x) + (p.first ? 0 : 1)) = 1;   // left to who joins it
+            continue;
+        }
+        for (int i = warp; i < p.ntok * a.G; i += kThreads / 32) {
+            const int t = i / a.G;
+            attend_row(a, p.b, p.seen.pf + t, p.row0 + t, p.h * a.G + i - t * a.G);
+        }
+    }
 }
 
 // Joins the parts of the items that shares cut, in their order: a block 32 rows
@@ -946,7 +1077,7 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs a)
     float M = -INFINITY, L = 0.f;
     for (int i = warp; i < parts; i += 8) {
         const float m = valid ? __ldcg(stats(i) + r0 + lane) : 0.f, l = valid ? __ldcg(stats(i) + kSlotRows + r0 + lane) : 0.f;
-        slow |= __ldcg(reinterpret_cast<const int*>(stats(i) + 2 * kSlotRows));
+        slow |= __ldcg(slot_flag(a, i == 0 ? slot0 : slot1 + 2 * (i - 1)));
         const float Mn = fmaxf(M, m), Ms = Mn == -INFINITY ? 0.f : Mn;
         L = L * ex2(M - Ms) + l * ex2(m - Ms);
         M = Mn;
@@ -1138,7 +1269,7 @@ extern "C" int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q
     const int cap = cache->page_table_stride * cache->page_size;
     // the list of key tiles is indexed in int
     const int64_t items = static_cast<int64_t>(Hkv) * ((rows + 2 * tok - 1) / (2 * tok) + batch);
-    const int64_t most = items * (cap / kKeys + 1);
+    const int64_t most = items * (cap / kKeys + 1 + kItem);
     if (most >= (int64_t(1) << 31)) return WQ4_ERR_UNSUPPORTED;
     int dev = 0;
     const DeviceInfo* di = current_device_info(&dev);
@@ -1156,6 +1287,7 @@ extern "C" int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q
     a.neg = scale < 0.f ? tc::kIdescNegA : 0u;
     a.box = 16;
     while (a.box < kKeys && cache->page_size % (2 * a.box) == 0) a.box *= 2;
+    a.wide = aligned(out, 32) && out_stride % 16 == 0 ? 1 : 0;
     a.stall = test_copy_stall() == WQ4_STALL_PROMPT ? 1 : 0;
     a.desc = static_cast<int32_t*>(workspace);
     a.slots = static_cast<uint8_t*>(workspace) + prompt_desc_bytes(prompt_grid(di));
