@@ -136,7 +136,7 @@ int wq4_kv_append(const wq4_kv_cache* cache, const uint16_t* new_k, const uint16
  *   seq_lens   : int32 [batch] device array, tokens of each sequence, the new
  *                ones included.
  *   rows       : rows that the buffers hold (>= row_starts[batch]).  Rows that
- *                no sequence owns are neither read nor written.
+ *                no sequence owns are left as they are.
  *
  * wq4_prompt_append: for each row of the fused QKV projection's output, the
  * rotation of q and k as in wq4_decode_attn (pairs (x_2i, x_2i+1) by

@@ -133,8 +133,8 @@ __global__ void __launch_bounds__(256) pool_drop_kernel(const PoolArgs a, const 
         if (blockIdx.y == 0 && threadIdx.x == 0) flag(a);
         return;
     }
-    const int T = a.lens[s];
-    for (int j = blockIdx.y * 256 + threadIdx.x; j < a.stride; j += gridDim.y * 256) {
+    const int T = a.lens[s], held = pages_of(a, T);
+    for (int j = blockIdx.y * 256 + threadIdx.x; j < held; j += gridDim.y * 256) {
         const int64_t first = static_cast<int64_t>(j) * a.page_size;
         const bool keep = !whole && (first < sinks || first + a.page_size > static_cast<int64_t>(T) + 1 - window);
         if (!keep) {
@@ -240,16 +240,16 @@ __global__ void __launch_bounds__(kPlan) pool_fork_kernel(const PoolArgs a, cons
     par[i] = p;
     chi[i] = c;
     __syncthreads();
-    // what the children held goes back first
+    // what the children held goes back first; four entries a lane at a time
     for (int k = warp; k < n; k += kPlanWarps) {
         if (chi[k] < 0) continue;
         int32_t* row = a.table + static_cast<size_t>(chi[k]) * a.stride;
-        for (int j = lane; j < a.stride; j += 32) {
+        const int np = pages_of(a, a.lens[chi[k]]);
+#pragma unroll 4
+        for (int j = lane; j < np; j += 32) {
             const int e = row[j];
-            if (e >= 0) {
-                row[j] = -1;
-                drop(a, e);
-            }
+            row[j] = -1;
+            if (e >= 0) drop(a, e);
         }
     }
     __syncthreads();
@@ -490,8 +490,8 @@ int check_pool(const wq4_kv_pool* pool, PoolArgs* a)
     a->page_size = c0.page_size;
     a->num_pages = c0.num_pages;
     a->max_seqs = pool->max_seqs;
-    a->err = status_word();
-    return a->err ? WQ4_OK : WQ4_ERR_CUDA;
+    a->err = nullptr;                // found once the lists are checked too
+    return WQ4_OK;
 }
 
 // Launch with programmatic dependent launch, as every kernel of the library.
@@ -548,6 +548,7 @@ extern "C" int wq4_kv_free(const wq4_kv_pool* pool, const int32_t* seqs, int n, 
     if (bad_list(seqs, n, WQ4_KV_MAX_SEQS)) return WQ4_ERR_INVALID;
     if (!aligned(seqs, 4)) return WQ4_ERR_ALIGN;
     if (n == 0) return WQ4_OK;
+    if (!(a.err = status_word())) return WQ4_ERR_CUDA;
     const int r = launch(pool_drop_kernel, dim3(n, std::min((a.stride + 255) / 256, 1024)), 256, stream, a, seqs, 1, 0, 0);
     return r != WQ4_OK ? r : launch(pool_empty_kernel, dim3((n + 255) / 256), 256, stream, a, seqs, n);
 }
@@ -560,6 +561,7 @@ extern "C" int wq4_kv_trim(const wq4_kv_pool* pool, const int32_t* seqs, int n, 
     if (bad_list(seqs, n, WQ4_KV_MAX_SEQS) || window < 1 || n_sinks < 0) return WQ4_ERR_INVALID;
     if (!aligned(seqs, 4)) return WQ4_ERR_ALIGN;
     if (n == 0) return WQ4_OK;
+    if (!(a.err = status_word())) return WQ4_ERR_CUDA;
     return launch(pool_drop_kernel, dim3(n, std::min((a.stride + 255) / 256, 1024)), 256, stream, a, seqs, 0, window, n_sinks);
 }
 
@@ -571,6 +573,7 @@ extern "C" int wq4_kv_reserve(const wq4_kv_pool* pool, const int32_t* seqs, cons
     if (bad_list(seqs, n, WQ4_KV_MAX_SEQS) || bad_list(new_lens, n, WQ4_KV_MAX_SEQS)) return WQ4_ERR_INVALID;
     if (!aligned(seqs, 4) || !aligned(new_lens, 4)) return WQ4_ERR_ALIGN;
     if (n == 0) return WQ4_OK;
+    if (!(a.err = status_word())) return WQ4_ERR_CUDA;
     return launch(pool_reserve_kernel, dim3(1), kPlan, stream, a, seqs, new_lens, n);
 }
 
@@ -582,6 +585,7 @@ extern "C" int wq4_kv_fork(const wq4_kv_pool* pool, const int32_t* parents, cons
     if (bad_list(parents, n, WQ4_KV_MAX_SEQS) || bad_list(children, n, WQ4_KV_MAX_SEQS)) return WQ4_ERR_INVALID;
     if (!aligned(parents, 4) || !aligned(children, 4)) return WQ4_ERR_ALIGN;
     if (n == 0) return WQ4_OK;
+    if (!(a.err = status_word())) return WQ4_ERR_CUDA;
     const int r = launch(pool_fork_kernel, dim3(1), kPlan, stream, a, parents, children, n);
     return r != WQ4_OK ? r : launch_copies(pool, a, n, false, stream);
 }
@@ -591,6 +595,7 @@ extern "C" int wq4_kv_compact(const wq4_kv_pool* pool, void* stream)
     PoolArgs a;
     const int rc = check_pool(pool, &a);
     if (rc != WQ4_OK) return rc;
+    if (!(a.err = status_word())) return WQ4_ERR_CUDA;
     const int r = launch(pool_compact_kernel, dim3(1), kPlan, stream, a);
     return r != WQ4_OK ? r : launch_copies(pool, a, a.num_pages, true, stream);
 }
@@ -603,6 +608,7 @@ extern "C" int wq4_kv_copy_pages(const wq4_kv_pool* pool, const int32_t* src, co
     if (bad_list(src, n, a.num_pages) || bad_list(dst, n, a.num_pages)) return WQ4_ERR_INVALID;
     if (!aligned(src, 4) || !aligned(dst, 4)) return WQ4_ERR_ALIGN;
     if (n == 0) return WQ4_OK;
+    if (!(a.err = status_word())) return WQ4_ERR_CUDA;
     const int r = launch(pool_copy_plan_kernel, dim3(1), kPlan, stream, a, src, dst, n);
     return r != WQ4_OK ? r : launch_copies(pool, a, n, false, stream);
 }

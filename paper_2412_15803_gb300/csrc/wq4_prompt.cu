@@ -54,7 +54,7 @@ __device__ __forceinline__ int row_owner(const Rows& R, int r, int* pos)
 
 // ----------------------------------------------------------------- append --
 
-constexpr int kAppRows = 8;
+constexpr int kAppRows = 4;
 constexpr int kAppThreads = 256;
 
 struct AppendArgs {
@@ -64,14 +64,50 @@ struct AppendArgs {
     uint16_t* q_out;                 // null: q is left alone
     int qkv_stride, q_out_stride, Hq, rotate;
     uint32_t* err;
-    double inv_freq[kD / 2];
+    uint64_t turns[kD / 2];          // angle of position 1 in turns, times 2^64
 };
+
+// Cosine and sine as sums of a value of 12 significant bits and a remainder
+// (x + y, z + w), each to about 2^-26, of pos times the angle in turns.  The
+// product modulo a turn is exact in 64-bit integers (fp64, which GB300 has at 1.25
+// TFLOP/s, made the angles cost more than the copy that they are for: 8192 rows of
+// 48 heads 68 us); a quarter of a turn is split off and the rest, |x| <= pi / 4,
+// goes through the Taylor series, with what rounding x to fp32 leaves over.
+__device__ __forceinline__ float4 rotation(int pos, uint64_t turns)
+{
+    const uint64_t t = static_cast<uint64_t>(pos) * turns;
+    const uint32_t quarter = static_cast<uint32_t>((t + (1ull << 61)) >> 62);
+    const int r = static_cast<int>(static_cast<int64_t>(t - (static_cast<uint64_t>(quarter) << 62)) >> 31);   // turns * 2^33
+    const float rh = static_cast<float>(r), rl = static_cast<float>(r - static_cast<int>(rh));
+    constexpr double kTurn = 6.283185307179586476925 / 8589934592.0;          // 2 pi / 2^33
+    constexpr float kHi = static_cast<float>(kTurn), kLo = static_cast<float>(kTurn - static_cast<double>(kHi));
+    const float x = rh * kHi, xl = fmaf(rh, kHi, -x) + fmaf(rh, kLo, rl * kHi);
+    const float z = x * x, zl = fmaf(x, x, -z);
+    const float S = fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f);
+    const float C = fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f);
+    float sh = x, sl = fmaf(x * z, S, fmaf(-0.5f * z, xl, xl));
+    float ch = fmaf(-0.5f, z, 1.f), cl = fmaf(z * z, C, fmaf(-0.5f, z, 1.f - ch) - fmaf(0.5f, zl, x * xl));
+    if (quarter & 1) {               // (c, s) -> (-s, c)
+        const float h = sh, l = sl;
+        sh = ch;
+        sl = cl;
+        ch = -h;
+        cl = -l;
+    }
+    if (quarter & 2) {
+        ch = -ch;
+        cl = -cl;
+        sh = -sh;
+        sl = -sl;
+    }
+    const float c12 = __uint_as_float(__float_as_uint(ch) & 0xFFFFF000u), s12 = __uint_as_float(__float_as_uint(sh) & 0xFFFFF000u);
+    return make_float4(c12, (ch - c12) + cl, s12, (sh - s12) + sl);
+}
 
 // (x0, x1) turned by the angle whose cosine and sine are t.x + t.y and t.z + t.w.
 // t.x and t.z have 12 significant bits, an fp16 value 11: their products are exact
 // in fp32, so the difference of the two large products is rounded once and the
-// remainders (2^-12 of them) add what they lack.  The fp64 rotation costs more
-// than the copy that it rides on (GB300 has 1.25 TFLOP/s of fp64).
+// remainders (2^-12 of them) add what they lack.
 __device__ __forceinline__ uint32_t turn(uint32_t x, float4 t)
 {
     const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&x));
@@ -81,64 +117,60 @@ __device__ __forceinline__ uint32_t turn(uint32_t x, float4 t)
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-__device__ __forceinline__ float2 split12(double v)
-{
-    const float hi = __uint_as_float(__float_as_uint(static_cast<float>(v)) & 0xFFFFF000u);
-    return make_float2(hi, static_cast<float>(v - hi));
-}
-
 // A block takes kAppRows rows: their owners and cache rows, the 64 rotations of
-// each, then 16 bytes a thread and step.
+// each (one a thread), and 16 bytes of every row a thread and step, all rows'
+// loads ahead of their stores.
 __global__ void __launch_bounds__(kAppThreads) prompt_append_kernel(const __grid_constant__ AppendArgs a)
 {
     __shared__ float4 rope[kAppRows][kD / 2];
     __shared__ int64_t dst[kAppRows];       // (page, row) as a row of head 0; -1: not written
-    __shared__ int pos_of[kAppRows], owner[kAppRows];
+    __shared__ int owner[kAppRows];
+    static_assert(kAppRows * (kD / 2) == kAppThreads, "a rotation a thread");
     grid_dependency_wait();
     grid_dependents_launch();
     const int r0 = blockIdx.x * kAppRows, tid = threadIdx.x;
-    if (tid < kAppRows) {
+    const int words = (a.Hq + 2 * a.c.Hkv) * (kD / 8);
+    uint4 x[kAppRows];
+    // (a row that no sequence owns is in the buffer, if the batch has it)
+    auto load = [&](int e) {
+#pragma unroll
+        for (int r = 0; r < kAppRows; ++r)
+            if (e < words && r0 + r < a.rows.rows)
+                x[r] = __ldcs(reinterpret_cast<const uint4*>(a.qkv + static_cast<size_t>(r0 + r) * a.qkv_stride) + e);
+    };
+    load(tid);                       // under way while the rows' places and rotations are found
+    {
+        const int r = tid / (kD / 2), i = tid % (kD / 2);
         int pos = 0;
-        const int b = r0 + tid < a.rows.rows ? row_owner(a.rows, r0 + tid, &pos) : -1;
-        int64_t d = -1;
-        if (b >= 0) {
-            const int page = pos >= 0 && pos < a.c.stride * a.c.page_size
-                                 ? __ldg(a.c.table + static_cast<size_t>(b) * a.c.stride + pos / a.c.page_size) : -1;
-            if (page >= 0 && page < a.c.num_pages)
-                d = static_cast<int64_t>(page) * a.c.Hkv * a.c.page_size + pos % a.c.page_size;
-            else
-                atomicOr(a.err, kErrAppend);
+        const int b = r0 + r < a.rows.rows ? row_owner(a.rows, r0 + r, &pos) : -1;
+        if (i == 0) {
+            int64_t d = -1;
+            if (b >= 0) {
+                const int page = pos >= 0 && pos < a.c.stride * a.c.page_size
+                                     ? __ldg(a.c.table + static_cast<size_t>(b) * a.c.stride + pos / a.c.page_size) : -1;
+                if (page >= 0 && page < a.c.num_pages)
+                    d = static_cast<int64_t>(page) * a.c.Hkv * a.c.page_size + pos % a.c.page_size;
+                else
+                    atomicOr(a.err, kErrAppend);
+            }
+            owner[r] = b;
+            dst[r] = d;
         }
-        owner[tid] = b;
-        pos_of[tid] = pos < 0 ? 0 : pos;
-        dst[tid] = d;
+        if (a.rotate) rope[r][i] = rotation(max(pos, 0), a.turns[i]);
     }
     __syncthreads();
-    if (a.rotate) {
-        for (int e = tid; e < kAppRows * (kD / 2); e += kAppThreads) {
-            const int r = e / (kD / 2), i = e % (kD / 2);
-            if (owner[r] < 0) continue;
-            double s, c;
-            sincos(pos_of[r] * a.inv_freq[i], &s, &c);
-            const float2 cc = split12(c), ss = split12(s);
-            rope[r][i] = make_float4(cc.x, cc.y, ss.x, ss.y);
-        }
-        __syncthreads();
-    }
-    const int heads = a.Hq + 2 * a.c.Hkv, words = heads * (kD / 8);
-    for (int r = 0; r < kAppRows; ++r) {
-        if (owner[r] < 0) continue;
-        const uint4* row = reinterpret_cast<const uint4*>(a.qkv + static_cast<size_t>(r0 + r) * a.qkv_stride);
-        for (int e = tid; e < words; e += kAppThreads) {
-            const int head = e / (kD / 8), w = e % (kD / 8);
-            const int kv = head - a.Hq;                  // >= 0: a key or value head
-            if (kv < 0 ? !a.q_out : dst[r] < 0) continue;
-            uint4 x = row[e];
+    for (int e = tid; e < words; e += kAppThreads) {
+        const int head = e / (kD / 8), w = e % (kD / 8);
+        const int kv = head - a.Hq;                      // >= 0: a key or value head
+        if (e != tid) load(e);
+#pragma unroll
+        for (int r = 0; r < kAppRows; ++r) {
+            if (owner[r] < 0 || (kv < 0 ? a.q_out == nullptr : dst[r] < 0)) continue;
             if (a.rotate && kv < a.c.Hkv) {
-                x.x = turn(x.x, rope[r][4 * w]);
-                x.y = turn(x.y, rope[r][4 * w + 1]);
-                x.z = turn(x.z, rope[r][4 * w + 2]);
-                x.w = turn(x.w, rope[r][4 * w + 3]);
+                x[r].x = turn(x[r].x, rope[r][4 * w]);
+                x[r].y = turn(x[r].y, rope[r][4 * w + 1]);
+                x[r].z = turn(x[r].z, rope[r][4 * w + 2]);
+                x[r].w = turn(x[r].w, rope[r][4 * w + 3]);
             }
             uint16_t* to;
             if (kv < 0)
@@ -146,7 +178,7 @@ __global__ void __launch_bounds__(kAppThreads) prompt_append_kernel(const __grid
             else
                 to = (kv < a.c.Hkv ? a.c.k : a.c.v) +
                      (dst[r] + static_cast<int64_t>(kv < a.c.Hkv ? kv : kv - a.c.Hkv) * a.c.page_size) * kD;
-            reinterpret_cast<uint4*>(to)[w] = x;
+            reinterpret_cast<uint4*>(to)[w] = x[r];
         }
     }
 }
@@ -162,12 +194,12 @@ __global__ void __launch_bounds__(kAppThreads) prompt_append_kernel(const __grid
 // unnormalised output in fp32) that a second kernel joins in their order.
 //
 // Warps: 0-3 and 4-7 the softmax of row tiles 0 and 1 (a thread a row), 8 the MMA
-// issuer, 9 and 10 the copies of queries and keys and of values, 11 what masks do
-// to values (below).  Scores S =
-// Q K^T of 128 x 128 go to tensor memory, one thread reads its row's 128, takes
-// the maximum and writes the weights as fp16 over the scores; O += P V reads
-// them there.  While one row tile's softmax runs, the tensor cores work for the
-// other.  An item of at most one row tile gives both softmax groups that tile,
+// issuer, 9 and 10 the copies of queries and keys and of values (with pages of 16
+// tokens 32 copies a key tile, ~100 cycles each in one warp), 11 what masks do to
+// values (below).  Scores S = Q K^T of 128 x 128 go to tensor memory, one thread
+// reads its row's 128, takes the maximum and writes the weights as fp16 over the
+// scores; O += P V reads them there.  While one row tile's softmax runs, the
+// tensor cores work for the other.  An item of at most one row tile gives both softmax groups that tile,
 // one the even and one the odd key tiles, and adds the two results at its end.
 //
 // The maximum that weights refer to follows the true one only when that is more
@@ -193,7 +225,9 @@ constexpr int kSlab = kTileBytes / 2;
 constexpr int kStages = 2;                         // of keys, and of values
 constexpr float kLift = 8.f, kLazy = 6.f;
 constexpr int kItem = 2;                           // an item's own cost, in key tiles
-constexpr int kMinShare = 4;                       // places of a block's share, at least: more than kItem
+constexpr int kUncut = 4;                          // key tiles that a context may have for its items to stay whole
+constexpr int kMinShare = 4;                       // places of a block's share, at least
+static_assert(kMinShare > kItem, "a share holds a tile");
 
 constexpr int kSlotRows = 256;
 constexpr size_t kSlotBytes = static_cast<size_t>(kSlotRows) * (kD + 2) * 4 + 256;   // O, m, l, flag
@@ -218,6 +252,7 @@ struct PromptArgs {
     float sl2;                       // |scale| * log2(e), not 0
     uint32_t neg;                    // kIdescNegA for a negative scale
     int box;                         // cache rows of one copy: a page's, or the part of it that divides a tile
+    int uncut;                       // shares of whole items
     int wide;                        // output rows are 32-byte aligned
     int stall;                       // test hook: no key or value is copied
     int32_t* desc;                   // [grid][kDescInts] items to join
@@ -313,6 +348,9 @@ struct Walk {
     int g, end, b, h, qt, is;      // is: where the present item begins
 };
 
+// The places that an item takes in the list.
+__device__ __forceinline__ int item_cost(const PromptArgs& a, const Seen& s) { return a.uncut ? 1 : kItem + s.tiles; }
+
 struct Piece {
     Seen seen;
     int t0, t1;                    // its tiles
@@ -332,7 +370,7 @@ __device__ __forceinline__ bool next_piece(const PromptArgs& a, const Seqs& s, i
     if (w.g >= w.end) return false;
     const int tok = kKeys / a.G, tt = 2 * tok;
     const Seen seen = item_seen(a, s, w.b, w.qt, tt);
-    const int t0 = max(0, w.g - w.is - kItem), t1 = min(seen.tiles, w.end - w.is - kItem);
+    const int t0 = a.uncut ? 0 : max(0, w.g - w.is - kItem), t1 = a.uncut ? seen.tiles : min(seen.tiles, w.end - w.is - kItem);
     if (t1 <= t0) {                      // the share ends before the item's first tile; p stays the last piece
         w.g = w.end;
         return false;
@@ -346,7 +384,7 @@ __device__ __forceinline__ bool next_piece(const PromptArgs& a, const Seqs& s, i
     p.ntok = min(tt, s.n[w.b] - w.qt * tt);
     p.dual = p.ntok <= tok;
     p.first = w.g == g_begin;
-    w.g = w.is + kItem + p.t1;
+    w.g = a.uncut ? w.is + 1 : w.is + kItem + p.t1;
     if (p.t1 == p.seen.tiles) {
         w.is = w.g;
         if (++w.qt * tt >= s.n[w.b]) {
@@ -388,6 +426,52 @@ struct Ring {
         }
     }
 };
+
+// The MMAs and the commit by the one thread for which `on` is set, without a branch:
+// the warp stays converged, so that operands stay in uniform registers.
+__device__ __forceinline__ void mma_ss_if(uint32_t on, uint32_t d, uint64_t ad, uint64_t bd, uint32_t idesc, uint32_t acc)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(ad), "l"(bd), "r"(idesc), "r"(acc), "r"(on)
+        : "memory");
+}
+
+__device__ __forceinline__ void mma_ts_if(uint32_t on, uint32_t d, uint32_t at, uint64_t bd, uint32_t idesc, uint32_t acc)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(at), "l"(bd), "r"(idesc), "r"(acc), "r"(on)
+        : "memory");
+}
+
+__device__ __forceinline__ void commit_if(uint32_t on, uint64_t* bar)
+{
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_addr(bar)),
+        "r"(on)
+        : "memory");
+}
+
+// A wait whose usual case, over or soon over, is one instruction and a branch not
+// taken.  ok: no wait has given up yet; after one has, none waits.
+__device__ __forceinline__ void wait(uint64_t* bar, uint32_t parity, bool& ok, uint32_t* err)
+{
+    if (__builtin_expect(!mbar_try_wait(bar, parity), 0)) {
+        if (ok) ok = mbar_wait(bar, parity, err);
+    }
+}
+
+// One arrival, by the lanes for which `on` is set, without a branch.
+__device__ __forceinline__ void arrive_if(uint32_t on, uint64_t* bar)
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(smem_addr(bar)),
+                 "r"(on)
+                 : "memory");
+}
 
 // Values read from tensor memory are used from here on, not before: the wait names
 // no registers, so the uses would not be ordered behind it.
@@ -521,6 +605,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc::prefetch_map(&maps.k);
         tc::prefetch_map(&maps.v);
     }
+    if (warp == kMmaWarp) tc::tmem_alloc(const_cast<uint32_t*>(reinterpret_cast<volatile uint32_t*>(misc + 6)), 512);
     grid_dependency_wait();              // every input may come from the previous kernel
     grid_dependents_launch();
 
@@ -537,7 +622,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         __syncwarp();
         int tiles = 0;
-        for (int qt = lane; qt * tt < n; qt += 32) tiles += item_seen(a, S, b, qt, tt).tiles + kItem;
+        for (int qt = lane; qt * tt < n; qt += 32) tiles += item_cost(a, item_seen(a, S, b, qt, tt));
         tiles = __reduce_add_sync(0xffffffffu, tiles);
         if (lane == 0) pre[b] = tiles;
     }
@@ -558,7 +643,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) pre[batch] = carry;
         __syncwarp();
         const int total = a.c.Hkv * carry, grid = static_cast<int>(gridDim.x);
-        const int R = max((total + grid - 1) / grid, kMinShare);
+        const int R = max((total + grid - 1) / grid, a.uncut ? 1 : kMinShare);
         const int g = min(static_cast<int64_t>(total), static_cast<int64_t>(blockIdx.x) * R);
         if (g < total) {
             int lo = 0, hi = batch - 1;
@@ -571,7 +656,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int h = (g - a.c.Hkv * pre[lo]) / of_head;
             int at = a.c.Hkv * pre[lo] + h * of_head, qt = 0;
             for (int q0 = 0;; q0 += 32) {       // ends: g lies within this head's tiles
-                const int v = (q0 + lane) * tt < sn[lo] ? item_seen(a, S, lo, q0 + lane, tt).tiles + kItem : 0;
+                const int v = (q0 + lane) * tt < sn[lo] ? item_cost(a, item_seen(a, S, lo, q0 + lane, tt)) : 0;
                 int incl = v;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
@@ -600,20 +685,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             misc[7] = R;
         }
     }
+    tc::fence_before_sync();
     __syncthreads();
+    tc::fence_after_sync();
     const int g_begin = misc[0];
     Walk walk = {g_begin, misc[1], misc[2], misc[3], misc[4], misc[5]};
     const int R = misc[7];
     int32_t* desc = a.desc + static_cast<size_t>(blockIdx.x) * kDescInts;
+    const uint32_t tbase = static_cast<uint32_t>(misc[6]);
     if (walk.g >= walk.end) {            // more blocks than shares
         if (threadIdx.x == 0) desc[0] = 0;
+        if (warp == kMmaWarp) tc::tmem_dealloc(tbase, 512);
         return;
     }
-    if (warp == kMmaWarp) tc::tmem_alloc(const_cast<uint32_t*>(reinterpret_cast<volatile uint32_t*>(misc + 6)), 512);
-    tc::fence_before_sync();
-    __syncthreads();
-    tc::fence_after_sync();
-    const uint32_t tbase = static_cast<uint32_t>(misc[6]);
     // tensor memory: scores (and weights over them) of row tile w at 128 w, output at 256 + 128 w
 
     // After a wait gave up (bounded, flagged) a role waits no more but goes on
@@ -622,236 +706,253 @@ __global__ void __launch_bounds__(kThreads, 1)
     Piece p;
     if (warp >= kMmaWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
-    if (warp == kKeyWarp || warp == kValueWarp) {
-        // ------------------------------------------------------------ copies
-        const bool keys = warp == kKeyWarp;
-        uint64_t* const full = keys ? kfull : vfull;
-        uint64_t* const empty = keys ? kempty : vempty;
-        uint8_t* const tiles = smem + kOffRing + (keys ? 0 : kStages * kTileBytes);
-        const CUtensorMap* const map = keys ? &maps.k : &maps.v;
-        Ring ring;
-        int issued = 0, nq[2] = {0, 0};
-        bool ok = true;
-        const int boxes = kKeys / a.box;
-        const uint32_t qbytes = static_cast<uint32_t>(a.G * tok) * 128u * 2u;
-        // A lane a box and half.  Boxes without a visible token, or on a page outside the
-        // pool, lie wholly outside the tensor: the copy reads zeros.  The next tile's
-        // page ids are under way while this one's copies are issued.
-        constexpr int kHidden = INT_MIN;
-        auto lookup = [&](const int32_t* table, int i) {
-            const int t = p.seen.token0(i) + (lane >> 1) * a.box;
-            const bool needed = lane < 2 * boxes && t <= p.seen.pl && (!a.window || t < a.sinks || t + a.box - 1 > p.seen.pf - a.window);
-            return needed ? __ldg(table + t / a.c.page_size) : kHidden;
-        };
-        auto tile = [&](int y) {
-            if (issued >= kStages && ok) ok = mbar_wait(&empty[ring.slot], ring.par ^ 1u, err);
-            if (!ok) return;
-            uint8_t* dst = tiles + ring.slot * kTileBytes;
-            if (lane == 0) mbar_arrive_expect_tx(&full[ring.slot], kTileBytes);
-            __syncwarp();
-            if (lane < 2 * boxes)
-                tc::tma_load_2d(dst + (lane & 1) * kSlab + (lane >> 1) * a.box * 128, map, 64 * (lane & 1), y, &full[ring.slot]);
-            ++issued;
-            ring.next();
-        };
-        while (ok && a.stall == 0) {
-            if (!next_piece(a, S, g_begin, walk, p)) break;
-            const int32_t* table = a.c.table + static_cast<size_t>(p.b) * a.c.stride;
-            int page = lookup(table, p.t0);
-            for (int i = p.t0; i < p.t1 && ok; ++i) {
-                const int next = i + 1 < p.t1 ? lookup(table, i + 1) : kHidden;
-                int y = -a.box;
-                if (page >= 0 && page < a.c.num_pages)
-                    y = (page * a.c.Hkv + p.h) * a.c.page_size + (p.seen.token0(i) + (lane >> 1) * a.box) % a.c.page_size;
-                else if (page != kHidden)
-                    atomicOr(err, kErrPageId);
-                page = next;
-                tile(y);
-                if (keys && i == p.t0)
-                    for (int w = 0; w < (p.dual ? 1 : 2) && ok; ++w) {
-                        if (nq[w] >= 1) ok = mbar_wait(&qempty[w], (nq[w] - 1) & 1, err);
-                        if (!ok) break;
-                        if (lane == 0) {
-                            mbar_arrive_expect_tx(&qfull[w], qbytes);
-                            for (int s = 0; s < 2; ++s)
-                                tc::tma_load_3d(smem + kOffQ + w * kTileBytes + s * kSlab, &maps.q, 64 * s, p.h * a.G, p.row0 + w * tok,
-                                                &qfull[w]);
+        if (warp == kKeyWarp || warp == kValueWarp) {
+            // ------------------------------------------------------------ copies
+            const bool keys = warp == kKeyWarp;
+            uint64_t* const full = keys ? kfull : vfull;
+            uint64_t* const empty = keys ? kempty : vempty;
+            uint8_t* const tiles = smem + kOffRing + (keys ? 0 : kStages * kTileBytes);
+            const CUtensorMap* const map = keys ? &maps.k : &maps.v;
+            Ring ring;
+            int issued = 0, nq[2] = {0, 0};
+            bool ok = true;
+            const int boxes = kKeys / a.box;
+            const uint32_t qbytes = static_cast<uint32_t>(a.G * tok) * 128u * 2u;
+            // A lane a box and half.  Boxes without a visible token, or on a page outside the
+            // pool, lie wholly outside the tensor: the copy reads zeros.  The next tile's
+            // page ids are under way while this one's copies are issued.
+            constexpr int kHidden = INT_MIN;
+            auto lookup = [&](const int32_t* table, int i) {
+                const int t = p.seen.token0(i) + (lane >> 1) * a.box;
+                const bool needed = lane < 2 * boxes && t <= p.seen.pl && (!a.window || t < a.sinks || t + a.box - 1 > p.seen.pf - a.window);
+                return needed ? __ldg(table + t / a.c.page_size) : kHidden;
+            };
+            auto tile = [&](int y) {
+                if (issued >= kStages && ok) ok = mbar_wait(&empty[ring.slot], ring.par ^ 1u, err);
+                if (!ok) return;
+                uint8_t* dst = tiles + ring.slot * kTileBytes;
+                if (lane == 0) mbar_arrive_expect_tx(&full[ring.slot], kTileBytes);
+                __syncwarp();
+                if (lane < 2 * boxes)
+                    tc::tma_load_2d(dst + (lane & 1) * kSlab + (lane >> 1) * a.box * 128, map, 64 * (lane & 1), y, &full[ring.slot]);
+                ++issued;
+                ring.next();
+            };
+            while (ok && a.stall == 0) {
+                if (!next_piece(a, S, g_begin, walk, p)) break;
+                const int32_t* table = a.c.table + static_cast<size_t>(p.b) * a.c.stride;
+                int page = lookup(table, p.t0);
+                for (int i = p.t0; i < p.t1 && ok; ++i) {
+                    const int next = i + 1 < p.t1 ? lookup(table, i + 1) : kHidden;
+                    int y = -a.box;
+                    if (page >= 0 && page < a.c.num_pages)
+                        y = (page * a.c.Hkv + p.h) * a.c.page_size + (p.seen.token0(i) + (lane >> 1) * a.box) % a.c.page_size;
+                    else if (page != kHidden)
+                        atomicOr(err, kErrPageId);
+                    page = next;
+                    tile(y);
+                    if (keys && i == p.t0)
+                        for (int w = 0; w < (p.dual ? 1 : 2) && ok; ++w) {
+                            if (nq[w] >= 1) ok = mbar_wait(&qempty[w], (nq[w] - 1) & 1, err);
+                            if (!ok) break;
+                            if (lane == 0) {
+                                mbar_arrive_expect_tx(&qfull[w], qbytes);
+                                for (int s = 0; s < 2; ++s)
+                                    tc::tma_load_3d(smem + kOffQ + w * kTileBytes + s * kSlab, &maps.q, 64 * s, p.h * a.G, p.row0 + w * tok,
+                                                    &qfull[w]);
+                            }
+                            ++nq[w];
                         }
-                        ++nq[w];
-                    }
+                }
             }
-        }
-        // every copy issued has landed before the block's memory goes away
-        for (int i = max(0, issued - kStages); i < issued; ++i) mbar_wait(&full[i % kStages], (i / kStages) & 1, err);
-        for (int w = 0; w < 2; ++w)
-            if (nq[w]) mbar_wait(&qfull[w], (nq[w] - 1) & 1, err);
-    } else if (warp == kMmaWarp) {
-        // -------------------------------------------------------- MMA issuer
-        // Units alternate between the groups; the scores of the unit after next are
-        // issued behind the weights x values of the present one, whose weights they
-        // overwrite (MMAs run in the order of issue).
-        // The loop's numbers come through a shuffle: warp-uniform for the compiler too,
-        // without which each MMA's operands pass through vector registers.
-        const uint32_t idesc_s = tc::idesc_f16_f32(128, kKeys) | a.neg;
-        const uint32_t idesc_o = tc::idesc_f16_f32(128, kD) | tc::kIdescTransB;
-        const uint32_t tb = __shfl_sync(0xffffffffu, tbase, 0);
-        const bool leader = tc::elect_one();
-        const uint64_t qdesc = tc::sw128_kmajor_desc(smem_addr(smem + kOffQ));
-        const uint64_t kdesc = tc::sw128_kmajor_desc(smem_addr(smem + kOffRing));
-        const uint64_t vdesc = tc::sw128_mnmajor_desc(smem_addr(smem + kOffRing + kStages * kTileBytes), kSlab);
-        Ring kr, vr;                     // the next key tile, the next value tile
-        uint32_t qpar[2] = {0, 0}, ppar[2] = {0, 0};
-        bool ok = true;
-        auto scores = [&](auto group, bool dual, bool first, bool last) {      // first, last: of this piece for its Q tile
-            constexpr int w = decltype(group)::value;
-            if (first && (w == 0 || !dual)) {
-                if (ok) ok = mbar_wait(&qfull[w], qpar[w], err);
-                qpar[w] ^= 1u;
-            }
-            if ((w == 0 || dual) && ok) ok = mbar_wait(&kfull[kr.slot], kr.par, err);
-            tc::fence_after_sync();
-            if (leader) {
+            // every copy issued has landed before the block's memory goes away
+            for (int i = max(0, issued - kStages); i < issued; ++i) mbar_wait(&full[i % kStages], (i / kStages) & 1, err);
+            for (int w = 0; w < 2; ++w)
+                if (nq[w]) mbar_wait(&qfull[w], (nq[w] - 1) & 1, err);
+        } else if (warp == kMmaWarp) {
+            // -------------------------------------------------------- MMA issuer
+            // The groups take turns at the key tiles; a group's next scores are issued
+            // behind its weights x values, whose weights they overwrite (MMAs run in
+            // the order of issue).  An MMA of 128 x 128 x 16 takes 64 cycles and the queue
+            // holds about two, so the loop must not lose time: its numbers come through a
+            // shuffle, warp-uniform for the compiler too, and MMAs are predicated rather
+            // than branched to, or their operands pass through vector registers (8192
+            // tokens of 32 heads 724 us with a branch and a search for each turn's kind).
+            const uint32_t idesc_s = tc::idesc_f16_f32(128, kKeys) | a.neg;
+            const uint32_t idesc_o = tc::idesc_f16_f32(128, kD) | tc::kIdescTransB;
+            const uint32_t tb = __shfl_sync(0xffffffffu, tbase, 0);
+            const uint32_t leader = tc::elect_one() ? 1u : 0u;
+            const uint64_t qdesc = tc::sw128_kmajor_desc(smem_addr(smem + kOffQ));
+            const uint64_t kdesc = tc::sw128_kmajor_desc(smem_addr(smem + kOffRing));
+            const uint64_t vdesc = tc::sw128_mnmajor_desc(smem_addr(smem + kOffRing + kStages * kTileBytes), kSlab);
+            Ring kr, vr;                     // the next key tile, the next value tile
+            uint32_t qpar[2] = {0, 0}, ppar[2] = {0, 0};
+            bool ok = true;
+            // first, last: of this piece for its Q tile
+            auto scores = [&](auto group, auto twin, bool first, bool last) {
+                constexpr int w = decltype(group)::value;
+                constexpr bool dual = decltype(twin)::value;
+                if (first && (w == 0 || !dual)) {
+                    wait(&qfull[w], qpar[w], ok, err);
+                    qpar[w] ^= 1u;
+                }
+                if (w == 0 || dual) wait(&kfull[kr.slot], kr.par, ok, err);
+                tc::fence_after_sync();
                 const uint64_t qd = qdesc + (w == 0 || dual ? 0u : kTileBytes >> 4);
                 const uint64_t kd = kdesc + kr.slot * (kTileBytes >> 4);
 #pragma unroll
                 for (int s = 0; s < 8; ++s) {
                     const uint64_t step = (s >> 2) * (kSlab >> 4) + (s & 3) * 2;
-                    tc::mma_f16_ss(tb + 128 * w, qd + step, kd + step, idesc_s, s > 0 ? 1u : 0u);
+                    mma_ss_if(leader, tb + 128 * w, qd + step, kd + step, idesc_s, s > 0 ? 1u : 0u);
                 }
-                tc::commit(&sfull[w]);
-                if (w == 1 || dual) tc::commit(&kempty[kr.slot]);
-                if (last) tc::commit(&qempty[dual ? 0 : w]);
-            }
-            if (w == 1 || dual) kr.next();
-        };
-        auto values = [&](auto group, bool dual, bool first, bool last) {
-            constexpr int w = decltype(group)::value;
-            if ((w == 0 || dual) && ok) ok = mbar_wait(&fixed[vr.slot], vr.par, err);
-            if (ok) ok = mbar_wait(&pfull[w], ppar[w], err);
-            ppar[w] ^= 1u;
-            tc::fence_after_sync();
-            if (leader) {
+                commit_if(leader, &sfull[w]);
+                if (w == 1 || dual) {
+                    commit_if(leader, &kempty[kr.slot]);
+                    kr.next();
+                }
+                if (last) commit_if(leader, &qempty[dual ? 0 : w]);
+            };
+            auto values = [&](auto group, auto twin, bool first, bool last) {
+                constexpr int w = decltype(group)::value;
+                constexpr bool dual = decltype(twin)::value;
+                if (w == 0 || dual) wait(&fixed[vr.slot], vr.par, ok, err);
+                wait(&pfull[w], ppar[w], ok, err);
+                ppar[w] ^= 1u;
+                tc::fence_after_sync();
                 const uint64_t vd = vdesc + vr.slot * (kTileBytes >> 4);
 #pragma unroll
                 for (int s = 0; s < 8; ++s)
-                    tc::mma_f16_ts(tb + 256 + 128 * w, tb + 128 * w + 8 * s, vd + s * (2048 >> 4), idesc_o, s > 0 || !first ? 1u : 0u);
-                if (last) tc::commit(&ofull[w]);
-                if (w == 1 || dual) tc::commit(&vempty[vr.slot]);
-            }
-            if (w == 1 || dual) vr.next();
-        };
-        using G0 = std::integral_constant<int, 0>;
-        using G1 = std::integral_constant<int, 1>;
-        struct Turns {
-            int nt, n0, n1;              // tiles of the piece, turns of the groups
-            bool dual;
-        };
-        auto fetch = [&](Turns& x) {
-            const int more = next_piece(a, S, g_begin, walk, p) ? 1 : 0;
-            if (!__shfl_sync(0xffffffffu, more, 0)) return false;
-            x.nt = __shfl_sync(0xffffffffu, p.t1 - p.t0, 0);
-            x.dual = __shfl_sync(0xffffffffu, p.dual ? 1 : 0, 0) != 0;
-            x.n0 = x.dual ? (x.nt + 1) / 2 : x.nt;
-            x.n1 = x.dual ? x.nt / 2 : x.nt;
-            return true;
-        };
-        auto first0 = [&](const Turns& x) { scores(G0{}, x.dual, true, x.nt == 1); };
-        auto first1 = [&](const Turns& x) {
-            if (x.n1 > 0) scores(G1{}, x.dual, true, x.dual ? x.nt == 2 : x.nt == 1);
-        };
-        // The next piece's first scores are issued behind a group's last values, where
-        // the groups end in their order; so its softmax finds them when its output is stored.
-        Turns x, next;
-        bool have = fetch(x);
-        if (have) {
-            first0(x);
-            first1(x);
-        }
-        while (have) {
-            const bool hn = fetch(next), even = x.n0 == x.n1;
-            for (int k = 0; k < x.n0; ++k) {
-                values(G0{}, x.dual, k == 0, k == x.n0 - 1);
-                if (k + 1 < x.n0) scores(G0{}, x.dual, false, x.dual ? 2 * k + 3 == x.nt : k + 2 == x.nt);
-                else if (hn && even) first0(next);
-                if (k < x.n1) {
-                    values(G1{}, x.dual, k == 0, k == x.n1 - 1);
-                    if (k + 1 < x.n1) scores(G1{}, x.dual, false, x.dual ? 2 * k + 4 == x.nt : k + 2 == x.nt);
-                    else if (hn && even) first1(next);
+                    mma_ts_if(leader, tb + 256 + 128 * w, tb + 128 * w + 8 * s, vd + s * (2048 >> 4), idesc_o, s > 0 || !first ? 1u : 0u);
+                if (last) commit_if(leader, &ofull[w]);
+                if (w == 1 || dual) {
+                    commit_if(leader, &vempty[vr.slot]);
+                    vr.next();
                 }
-            }
-            if (hn && !even) {
-                first0(next);
-                first1(next);
-            }
-            x = next;
-            have = hn;
-        }
-        if (leader) tc::commit(drain);   // all MMAs have completed before tensor memory is released
-        mbar_wait(drain, 0, err);
-    } else if (warp == kMaskWarp) {
-        // ---------------------------------------------------- masked values
-        Ring vr;
-        bool ok = true;
-        for (int piece = 0; next_piece(a, S, g_begin, walk, p); ++piece) {
-            for (int i = p.t0; i < p.t1; ++i) {
-                if (ok) ok = mbar_wait(&vfull[vr.slot], vr.par, err);
-                __syncwarp();
-                const int t0 = p.seen.token0(i), pf = p.seen.pf, pl = p.seen.pl;
-                if (!sees_all(t0, pf, pl, pl, a.window, a.sinks)) {
-                    uint8_t* base = smem + kOffRing + (kStages + vr.slot) * kTileBytes + ((lane >> 3) & 1) * kSlab + (lane & 7) * 16;
-                    __half2 big = __float2half2_rn(0.f);
-                    auto clip = [&](int tkn) { return min(max(tkn - t0, 0), kKeys); };
-                    // [from, to) of the tile's rows: 16 lanes a row
-                    auto zero = [&](int from, int to) {
-                        for (int r = clip(from) + (lane >> 4); r < clip(to); r += 2)
-                            *reinterpret_cast<uint4*>(base + r * 128) = make_uint4(0, 0, 0, 0);
-                    };
-                    auto look = [&](int from, int to) {        // the largest size, NaN above all
-                        const int f = clip(from), e = clip(to);
-                        for (int r = f + (lane >> 4); r - (lane >> 4) < e; r += 16) {
-                            uint4 x[8];
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const uint4*>(base + min(r + 2 * j, e - 1) * 128);
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                big = __hmax2_nan(big, __hmax2_nan(__habs2(as_half2(x[j].x)), __habs2(as_half2(x[j].y))));
-                                big = __hmax2_nan(big, __hmax2_nan(__habs2(as_half2(x[j].z)), __habs2(as_half2(x[j].w))));
-                            }
-                        }
-                    };
-                    // Seen by no row: behind pl, and between the sinks and pf - window (whole boxes
-                    // there were copied as zeros).  Seen by some: from pf on, and up to pl - window.
-                    zero(pl + 1, (pl / a.box + 1) * a.box);
-                    look(max(pf, -1) + 1, pl + 1);
-                    if (a.window) {
-                        const int gone = pf - a.window + 1;    // the first token that the window shows
-                        if (gone > a.sinks) {
-                            zero(a.sinks, min(gone, (a.sinks + a.box - 1) / a.box * a.box));
-                            zero(max(a.sinks, gone / a.box * a.box), gone);
-                        }
-                        look(max(a.sinks, gone), min(pl - a.window, pf) + 1);
+            };
+            using G0 = std::integral_constant<int, 0>;
+            using G1 = std::integral_constant<int, 1>;
+            using Two = std::false_type;     // a row tile each
+            using One = std::true_type;      // one row tile for both
+            struct Turns {
+                int nt;                      // tiles of the piece
+                bool dual;
+            };
+            auto fetch = [&](Turns& x) {
+                const int more = next_piece(a, S, g_begin, walk, p) ? 1 : 0;
+                if (!__shfl_sync(0xffffffffu, more, 0)) return false;
+                x.nt = __shfl_sync(0xffffffffu, p.t1 - p.t0, 0);
+                x.dual = __shfl_sync(0xffffffffu, p.dual ? 1 : 0, 0) != 0;
+                return true;
+            };
+            // The next piece's first scores are issued behind a group's last values, where the
+            // groups end in their order; so its softmax finds them when its output is stored.
+            Turns x, after;
+            bool have = fetch(x), begun = false;
+            auto first0 = [&](const Turns& y) {
+                if (y.dual) scores(G0{}, One{}, true, y.nt == 1);
+                else scores(G0{}, Two{}, true, y.nt == 1);
+            };
+            auto first1 = [&](const Turns& y) {
+                if (!y.dual) scores(G1{}, Two{}, true, y.nt == 1);
+                else if (y.nt > 1) scores(G1{}, One{}, true, y.nt == 2);
+            };
+            while (have) {
+                if (!begun) {
+                    first0(x);
+                    first1(x);
+                }
+                const bool more = fetch(after);
+                begun = false;
+                if (!x.dual) {
+                    for (int k = 0; k + 1 < x.nt; ++k) {
+                        values(G0{}, Two{}, k == 0, false);
+                        scores(G0{}, Two{}, false, k + 2 == x.nt);
+                        values(G1{}, Two{}, k == 0, false);
+                        scores(G1{}, Two{}, false, k + 2 == x.nt);
                     }
-                    if (__any_sync(0xffffffffu, not_finite(big)) && lane == 0) atomicOr(&again[(piece >> 5) & 31], 1u << (piece & 31));
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
+                    values(G0{}, Two{}, x.nt == 1, true);
+                    if (more) first0(after);
+                    values(G1{}, Two{}, x.nt == 1, true);
+                    if (more) first1(after);
+                    begun = more;
+                } else {
+                    for (int u = 0; u < x.nt; u += 2) {
+                        values(G0{}, One{}, u == 0, u + 2 >= x.nt);
+                        if (u + 2 < x.nt) scores(G0{}, One{}, false, u + 3 == x.nt);
+                        if (u + 1 == x.nt) break;
+                        values(G1{}, One{}, u == 0, u + 3 >= x.nt);
+                        if (u + 3 < x.nt) scores(G1{}, One{}, false, u + 4 == x.nt);
+                    }
                 }
-                if (lane == 0) mbar_arrive(&fixed[vr.slot]);
-                vr.next();
+                x = after;
+                have = more;
+            }
+            commit_if(leader, drain);   // all MMAs have completed before tensor memory is released
+            mbar_wait(drain, 0, err);
+        } else if (warp == kMaskWarp) {
+            // ---------------------------------------------------- masked values
+            Ring vr;
+            bool ok = true;
+            for (int piece = 0; next_piece(a, S, g_begin, walk, p); ++piece) {
+                for (int i = p.t0; i < p.t1; ++i) {
+                    if (ok) ok = mbar_wait(&vfull[vr.slot], vr.par, err);
+                    __syncwarp();
+                    const int t0 = p.seen.token0(i), pf = p.seen.pf, pl = p.seen.pl;
+                    if (!sees_all(t0, pf, pl, pl, a.window, a.sinks)) {
+                        uint8_t* base = smem + kOffRing + (kStages + vr.slot) * kTileBytes + ((lane >> 3) & 1) * kSlab + (lane & 7) * 16;
+                        __half2 big = __float2half2_rn(0.f);
+                        auto clip = [&](int tkn) { return min(max(tkn - t0, 0), kKeys); };
+                        // [from, to) of the tile's rows: 16 lanes a row
+                        auto zero = [&](int from, int to) {
+                            for (int r = clip(from) + (lane >> 4); r < clip(to); r += 2)
+                                *reinterpret_cast<uint4*>(base + r * 128) = make_uint4(0, 0, 0, 0);
+                        };
+                        auto look = [&](int from, int to) {        // the largest size, NaN above all
+                            const int f = clip(from), e = clip(to);
+                            for (int r = f + (lane >> 4); r - (lane >> 4) < e; r += 16) {
+                                uint4 x[8];
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const uint4*>(base + min(r + 2 * j, e - 1) * 128);
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) {
+                                    big = __hmax2_nan(big, __hmax2_nan(__habs2(as_half2(x[j].x)), __habs2(as_half2(x[j].y))));
+                                    big = __hmax2_nan(big, __hmax2_nan(__habs2(as_half2(x[j].z)), __habs2(as_half2(x[j].w))));
+                                }
+                            }
+                        };
+                        // Seen by no row: behind pl, and between the sinks and pf - window (whole boxes
+                        // there were copied as zeros).  Seen by some: from pf on, and up to pl - window.
+                        zero(pl + 1, (pl / a.box + 1) * a.box);
+                        look(max(pf, -1) + 1, pl + 1);
+                        if (a.window) {
+                            const int gone = pf - a.window + 1;    // the first token that the window shows
+                            if (gone > a.sinks) {
+                                zero(a.sinks, min(gone, (a.sinks + a.box - 1) / a.box * a.box));
+                                zero(max(a.sinks, gone / a.box * a.box), gone);
+                            }
+                            look(max(a.sinks, gone), min(pl - a.window, pf) + 1);
+                        }
+                        if (__any_sync(0xffffffffu, not_finite(big)) && lane == 0) atomicOr(&again[(piece >> 5) & 31], 1u << (piece & 31));
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                    }
+                    if (lane == 0) mbar_arrive(&fixed[vr.slot]);
+                    vr.next();
+                }
+            }
+            // the item that this share's end cuts, and does not begin in an earlier one: who joins it finds it here
+            if (lane == 0) {
+                const bool head = p.t0 == 0 && !p.whole();
+                desc[0] = head ? (walk.is + kItem + p.seen.tiles - 1) / R - static_cast<int>(blockIdx.x) + 1 : 0;
+                desc[1] = p.b;
+                desc[2] = p.h;
+                desc[3] = p.row0;
+                desc[4] = p.ntok;
+                desc[5] = p.seen.pf;
+                desc[6] = 2 * static_cast<int>(blockIdx.x) + (p.first ? 0 : 1);
+                for (int i = 0; i < 2; ++i) *slot_flag(a, 2 * blockIdx.x + i) = 0;
             }
         }
-        // the item that this share's end cuts, and does not begin in an earlier one: who joins it finds it here
-        if (lane == 0) {
-            const bool head = p.t0 == 0 && !p.whole();
-            desc[0] = head ? (walk.is + kItem + p.seen.tiles - 1) / R - static_cast<int>(blockIdx.x) + 1 : 0;
-            desc[1] = p.b;
-            desc[2] = p.h;
-            desc[3] = p.row0;
-            desc[4] = p.ntok;
-            desc[5] = p.seen.pf;
-            desc[6] = 2 * static_cast<int>(blockIdx.x) + (p.first ? 0 : 1);
-            for (int i = 0; i < 2; ++i) *slot_flag(a, 2 * blockIdx.x + i) = 0;
-        }
-    }
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsLaunch));
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
@@ -870,7 +971,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             float m = -INFINITY;
             uint64_t l2 = pair(0.f, 0.f);
             for (int k = 0; k < nk; ++k) {
-                if (ok) ok = mbar_wait(&sfull[w], spar, err);
+                wait(&sfull[w], spar, ok, err);
                 spar ^= 1u;
                 __syncwarp();
                 tc::fence_after_sync();
@@ -886,6 +987,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         const uint32_t see = first_bits(hi - 32 * c) & (~first_bits(lo - 32 * c) | first_bits(sk - 32 * c));
+                        if (__all_sync(0xffffffffu, see == 0xFFFFFFFFu)) continue;       // most: a tile has one edge or two
 #pragma unroll
                         for (int i = 0; i < 32; ++i) s[32 * c + i] = see & (1u << i) ? s[32 * c + i] : 0xFF800000u;   // -infinity
                     }
@@ -918,7 +1020,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc::st32(ts, pk);
                 tc::st32(ts + 32, pk + 32);
                 if (k > 0 && __any_sync(0xffffffffu, up)) {
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < 4; ++c) {
                         uint32_t o[32];
                         tc::ld32(to + 32 * c, o);
@@ -932,13 +1034,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc::st_wait();
                 tc::fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&pfull[w]);
+                arrive_if(lane == 0, &pfull[w]);
             }
             float l, lh;
             unpair(l2, l, lh);
             l += lh;
             if (nk > 0) {
-                if (ok) ok = mbar_wait(&ofull[w], opar, err);
+                wait(&ofull[w], opar, ok, err);
                 opar ^= 1u;
                 __syncwarp();
                 tc::fence_after_sync();
@@ -972,7 +1074,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 uint16_t* orow = a.out + static_cast<size_t>(p.row0 + base + (valid ? rtok : 0)) * a.out_stride +
                                  static_cast<size_t>(p.h * a.G + rhead) * kD;
                 const int prow = w * 128 + row;
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < 4; ++c) {
                     uint32_t o[32];
                     tc::ld32(to + 32 * c, o);
@@ -1046,13 +1148,17 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // Joins the parts of the items that shares cut, in their order: a block 32 rows
-// of one item, a lane a row, a warp 16 of the 128 dimensions.
+// of one item, a lane a row, a warp 4 kChunks dimensions (gridDim.z blocks for
+// all).  Many items are cut in two or three parts each (kChunks = 4: few blocks),
+// few items in many (kChunks = 1: the loads of eight parts at once; 19 parts of 64
+// rows join in JOIN1 us, with four chunks in JOIN4).
 constexpr int kMaxGrid = 256;
 
+template <int kChunks>
 __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs a)
 {
     __shared__ float sm[8][32], sl[8][32];
-    __shared__ __align__(16) uint16_t tile[32][kD + 8];
+    __shared__ __align__(8) uint16_t tile[32][32 * kChunks + 4];
     grid_dependency_wait();
     grid_dependents_launch();
     const int32_t* desc = a.desc + static_cast<size_t>(blockIdx.x) * kDescInts;
@@ -1085,7 +1191,7 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs a)
     sm[warp][lane] = M;
     sl[warp][lane] = L;
     if (__syncthreads_or(slow)) {
-        for (int i = 4 * warp; i < 4 * warp + 4; ++i) {
+        for (int i = 4 * warp; i < 4 * warp + 4 && blockIdx.z == 0; ++i) {
             const int r = r0 + i;
             int t;
             if (place(r, t)) attend_row(a, b, pf + t, row0 + t, h * a.G + (r & 127) % a.G);
@@ -1099,13 +1205,13 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs a)
     const float Ms = M == -INFINITY ? 0.f : M;
 #pragma unroll
     for (int w = 0; w < 8; ++w) L = fmaf(sl[w][lane], ex2(sm[w][lane] - Ms), L);
-    float4 acc[4] = {};
-#pragma unroll 4
+    float4 acc[kChunks] = {};
+#pragma unroll (8 / kChunks)
     for (int i = 0; i < parts; ++i) {
         const float f = valid ? ex2(__ldcg(stats(i) + r0 + lane) - Ms) : 0.f;
-        const float4* o = reinterpret_cast<const float4*>(part(i)) + (4 * warp) * kSlotRows + r0 + lane;
+        const float4* o = reinterpret_cast<const float4*>(part(i)) + kChunks * (8 * blockIdx.z + warp) * kSlotRows + r0 + lane;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < kChunks; ++c) {
             const float4 v = valid ? __ldcg(o + c * kSlotRows) : make_float4(0.f, 0.f, 0.f, 0.f);
             acc[c].x = fmaf(v.x, f, acc[c].x);
             acc[c].y = fmaf(v.y, f, acc[c].y);
@@ -1115,16 +1221,16 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs a)
     }
     const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-        *reinterpret_cast<uint2*>(&tile[lane][16 * warp + 4 * c]) =
+    for (int c = 0; c < kChunks; ++c)
+        *reinterpret_cast<uint2*>(&tile[lane][4 * (kChunks * warp + c)]) =
             make_uint2(half2_bits(acc[c].x * inv, acc[c].y * inv), half2_bits(acc[c].z * inv, acc[c].w * inv));
     __syncthreads();
-    for (int e = threadIdx.x; e < 32 * 16; e += 256) {
-        const int r = r0 + (e >> 4);
+    for (int e = threadIdx.x; e < 32 * 8 * kChunks; e += 256) {
+        const int i = e / (8 * kChunks), c = e % (8 * kChunks), r = r0 + i;
         int t;
         if (place(r, t))
-            reinterpret_cast<uint4*>(a.out + static_cast<size_t>(row0 + t) * a.out_stride + (h * a.G + (r & 127) % a.G) * kD)[e & 15] =
-                reinterpret_cast<const uint4*>(tile[e >> 4])[e & 15];
+            reinterpret_cast<uint2*>(a.out + static_cast<size_t>(row0 + t) * a.out_stride + (h * a.G + (r & 127) % a.G) * kD +
+                                     32 * kChunks * blockIdx.z)[c] = *reinterpret_cast<const uint2*>(&tile[i][4 * c]);
     }
 }
 
@@ -1230,7 +1336,13 @@ extern "C" int wq4_prompt_append(const wq4_kv_cache* cache, const uint16_t* qkv,
     a.rotate = rotate ? 1 : 0;
     a.err = status_word();
     if (!a.err) return WQ4_ERR_CUDA;
-    for (int i = 0; i < kD / 2; ++i) a.inv_freq[i] = rotate ? std::pow(rope_theta, -2.0 * i / kD) : 0.0;
+    for (int i = 0; i < kD / 2; ++i) {
+        // w / (2 pi) to more than a double's bits: the quotient and what it leaves
+        constexpr double k2Pi = 6.283185307179586476925, k2PiLow = 2.4492935982947064e-16;
+        const double w = rotate ? std::pow(rope_theta, -2.0 * i / kD) : 0.0, f = w / k2Pi;
+        const double rest = (std::fma(-f, k2Pi, w) - f * k2PiLow) / k2Pi;
+        a.turns[i] = static_cast<uint64_t>(std::ldexp(f, 64)) + static_cast<uint64_t>(static_cast<int64_t>(std::ldexp(rest, 64)));
+    }
     return launch(prompt_append_kernel, dim3((rows + kAppRows - 1) / kAppRows), kAppThreads, 0, stream, a);
 }
 
@@ -1269,12 +1381,15 @@ extern "C" int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q
     const int cap = cache->page_table_stride * cache->page_size;
     // the list of key tiles is indexed in int
     const int64_t items = static_cast<int64_t>(Hkv) * ((rows + 2 * tok - 1) / (2 * tok) + batch);
-    const int64_t most = items * (cap / kKeys + 1 + kItem);
-    if (most >= (int64_t(1) << 31)) return WQ4_ERR_UNSUPPORTED;
+    // Short contexts: an item of few tiles is not worth cutting, and without cuts there
+    // is nothing to join.
+    a.uncut = (cap + kKeys - 1) / kKeys <= kUncut ? 1 : 0;
+    const int64_t most = a.uncut ? items : items * (cap / kKeys + 1 + kItem);
+    if (most >= (int64_t(1) << 30)) return WQ4_ERR_UNSUPPORTED;
     int dev = 0;
     const DeviceInfo* di = current_device_info(&dev);
     if (!di || !prompt_ready(dev)) return WQ4_ERR_CUDA;
-    const int grid = static_cast<int>(std::min<int64_t>(prompt_grid(di), (most + kMinShare - 1) / kMinShare));
+    const int grid = static_cast<int>(std::min<int64_t>(prompt_grid(di), a.uncut ? most : (most + kMinShare - 1) / kMinShare));
     a.q = q;
     a.out = out;
     a.q_stride = q_stride;
@@ -1305,6 +1420,9 @@ extern "C" int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q
                               {64, static_cast<uint32_t>(G), static_cast<uint32_t>(tok)}, CU_TENSOR_MAP_SWIZZLE_128B))
         return WQ4_ERR_CUDA;
     const int r = launch(prompt_attn_kernel, dim3(grid), kThreads, prompt_smem_bytes(batch), stream, maps, a);
-    if (r != WQ4_OK || grid == 1) return r;      // one block cuts nothing
-    return launch(prompt_join_kernel, dim3(grid - 1, kSlotRows / 32), 256, 0, stream, a);
+    if (r != WQ4_OK || a.uncut || grid == 1) return r;      // one block cuts nothing
+    // fewer items than blocks (were every row owned): cut in many parts
+    return static_cast<int64_t>(Hkv) * ((rows + 2 * tok - 1) / (2 * tok)) < grid
+               ? launch(prompt_join_kernel<1>, dim3(grid - 1, kSlotRows / 32, 4), 256, 0, stream, a)
+               : launch(prompt_join_kernel<4>, dim3(grid - 1, kSlotRows / 32), 256, 0, stream, a);
 }

@@ -124,6 +124,85 @@ def test_longer(new, ctx, window, sinks):
     both(new, ctx, 8, 2, 32, window, sinks, seed=3)
 
 
+@pytest.mark.parametrize("P", [48, 80, 144, 384])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 20)])
+def test_pages_that_end_inside_a_tile(P, window, sinks):
+    both([90, 200], [170, 31], 8, 2, P, window, sinks, seed=14)
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(7, 1), (12, 2), (16, 2), (9, 3)])
+def test_groups(Hq, Hkv):
+    both([140, 37], [100, 0], Hq, Hkv, 32, 70, 9, seed=15)
+    both([140, 37], [100, 0], Hq, Hkv, 32, seed=15)
+
+
+@pytest.mark.parametrize("scale", [-0.07, 0.0, 1e-30, 0.5])
+def test_scales(scale):
+    """Of either sign and none: with 0 every row is the mean of the values it sees."""
+    q, k, v, table, given, starts, lens = make(16, [150, 3], [20, 300], 8, 2, 16)
+    call = Call(q, k, v, given, starts, lens, 8)
+    call(scale=scale)
+    check(call.result(), q, k, v, table, starts, lens, 8, scale=scale)
+
+
+def test_a_long_prompt_of_few_heads():
+    """More key tiles than blocks a head: every item cut, some into many parts."""
+    both([2500], [300], 2, 1, 64, seed=17)
+
+
+def test_beyond_32_bits():
+    """The sequence's pages lie behind 4 GiB of the pool, in bytes and in elements."""
+    Hq, Hkv, P, pages = 4, 2, 64, 140_000
+    k = torch.zeros((pages, Hkv, P, D), dtype=torch.int16, device="cuda")       # 4.6 GB each, 2.3e9 elements
+    v = torch.zeros_like(k)
+    q, ks, vs, table, _, starts, lens = make(18, [40], [60], Hq, Hkv, P, hide=False)
+    n = ks.shape[0]
+    k[pages - n:], v[pages - n:] = dev(ks), dev(vs)
+    small = Call(q, ks, vs, table, starts, lens, Hq)
+    small()
+    big = Call(q, ks, vs, table + (pages - n), starts, lens, Hq)
+    big.cache = wq4.kv_cache_desc(k, v, big.table, P)
+    big()
+    assert np.array_equal(small.result(), big.result())
+    ws = torch.zeros(wq4.wq4_paged_attention_workspace_bytes(1, Hq, Hkv, D), dtype=torch.uint8, device="cuda")
+    for c in (small, big):
+        wq4.wq4_window_attention(c.cache, c.q, Hq * D, c.lens, c.out, Hq * D, 1, Hq, SCALE, 50, 3, ws, ws.numel())
+    assert np.array_equal(small.result()[:1], big.result()[:1])
+    x = dev(synth.sum4_fp16(18, 5, 0, 40 * (Hq + 2 * Hkv) * D).reshape(40, -1))
+    for c in (small, big):
+        wq4.wq4_prompt_append(c.cache, x, (Hq + 2 * Hkv) * D, c.q, Hq * D, c.starts, c.lens, 1, 40, Hq, THETA)
+    torch.cuda.synchronize()
+    assert torch.equal(k[pages - n:], small.k) and torch.equal(v[pages - n:], small.v) and not k[:1000].any()
+    ints = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")   # noqa: E731
+    refs = torch.zeros(pages, dtype=torch.int32, device="cuda")
+    pool_ws = torch.empty(wq4.wq4_kv_pool_workspace_bytes(pages, 1), dtype=torch.uint8, device="cuda")
+    pool = wq4.kv_pool_desc([big.cache], big.table, big.lens, refs, pool_ws)
+    wq4.wq4_kv_copy_pages(pool, ints([pages - n]), ints([pages - n - 3]), 1)
+    torch.cuda.synchronize()
+    assert torch.equal(k[pages - n - 3], k[pages - n]) and torch.equal(v[pages - n - 3], v[pages - n])
+    assert wq4.wq4_device_status() == 0
+
+
+def test_without_its_copies_it_ends():
+    """Waits for copies that never come run out: the kernel ends, flags it, and the next call is clean."""
+    for new, ctx in (([300, 20], [500, 0]), ([10], [3000])):
+        q, k, v, table, given, starts, lens = make(19, new, ctx, 8, 2, 16)
+        call = Call(q, k, v, given, starts, lens, 8)
+        call()
+        want = call.result()
+        assert wq4.wq4_device_status() == 0
+        try:
+            wq4.wq4_test_copy_stall(4)
+            call()
+            torch.cuda.synchronize()
+        finally:
+            wq4.wq4_test_copy_stall()
+        assert wq4.wq4_device_status() & 1
+        call.out.fill_(-1)
+        call()
+        assert np.array_equal(call.result(), want) and wq4.wq4_device_status() == 0
+
+
 def test_many_sequences():
     rng = np.random.default_rng(0)
     new = rng.integers(0, 5, 1024)
@@ -202,7 +281,7 @@ def test_bad_pages_and_lengths_are_flagged():
     Call(q, k, v, bad, starts, lens, 8)()
     assert wq4.wq4_device_status() == 16
     Call(q, k, v, table, starts, lens + 50, 8)()
-    assert wq4.wq4_device_status() & 8
+    assert wq4.wq4_device_status() == 8
 
 
 @pytest.mark.parametrize("starts", [[0, 500, 40], [30, 10, 40], [-5, 20, 10 ** 9], [2 ** 31 - 1, 0, 0]])
