@@ -54,8 +54,9 @@ __device__ __forceinline__ int row_owner(const Rows& R, int r, int* pos)
 
 // ----------------------------------------------------------------- append --
 
-constexpr int kAppRows = 4;
-constexpr int kAppThreads = 256;
+constexpr int kAppRows = 2;
+constexpr int kAppHeads = 4;
+constexpr int kAppThreads = 64 * kAppRows;
 
 struct AppendArgs {
     Rows rows;
@@ -117,68 +118,60 @@ __device__ __forceinline__ uint32_t turn(uint32_t x, float4 t)
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// A block takes kAppRows rows: their owners and cache rows, the 64 rotations of
-// each (one a thread), and 16 bytes of every row a thread and step, all rows'
-// loads ahead of their stores.
+// A block takes kAppRows rows, 64 threads each: 16 bytes of a head by one thread,
+// every fourth head, kAppHeads heads' loads ahead of their stores.  A thread's four
+// rotations serve all its heads in registers (a table in shared memory, read again
+// for each head, cost 18 us of 52 over 8192 rows of 48 heads).  The first heads are
+// under way while the row's place and rotations are found.
 __global__ void __launch_bounds__(kAppThreads) prompt_append_kernel(const __grid_constant__ AppendArgs a)
 {
-    __shared__ float4 rope[kAppRows][kD / 2];
-    __shared__ int64_t dst[kAppRows];       // (page, row) as a row of head 0; -1: not written
-    __shared__ int owner[kAppRows];
-    static_assert(kAppRows * (kD / 2) == kAppThreads, "a rotation a thread");
     grid_dependency_wait();
     grid_dependents_launch();
-    const int r0 = blockIdx.x * kAppRows, tid = threadIdx.x;
-    const int words = (a.Hq + 2 * a.c.Hkv) * (kD / 8);
-    uint4 x[kAppRows];
-    // (a row that no sequence owns is in the buffer, if the batch has it)
-    auto load = [&](int e) {
+    const int row = blockIdx.x * kAppRows + (threadIdx.x >> 6), h0 = (threadIdx.x >> 4) & 3, w = threadIdx.x & 15;
+    if (row >= a.rows.rows) return;
+    const int heads = a.Hq + 2 * a.c.Hkv;
+    const uint4* in = reinterpret_cast<const uint4*>(a.qkv + static_cast<size_t>(row) * a.qkv_stride) + w;
+    uint4 x[kAppHeads];
+    auto load = [&](int h) {         // (a row that no sequence owns is in the buffer too)
 #pragma unroll
-        for (int r = 0; r < kAppRows; ++r)
-            if (e < words && r0 + r < a.rows.rows)
-                x[r] = __ldcs(reinterpret_cast<const uint4*>(a.qkv + static_cast<size_t>(r0 + r) * a.qkv_stride) + e);
+        for (int i = 0; i < kAppHeads; ++i)
+            if (h + 4 * i < heads) x[i] = __ldcs(in + (h + 4 * i) * (kD / 8));
     };
-    load(tid);                       // under way while the rows' places and rotations are found
-    {
-        const int r = tid / (kD / 2), i = tid % (kD / 2);
-        int pos = 0;
-        const int b = r0 + r < a.rows.rows ? row_owner(a.rows, r0 + r, &pos) : -1;
-        if (i == 0) {
-            int64_t d = -1;
-            if (b >= 0) {
-                const int page = pos >= 0 && pos < a.c.stride * a.c.page_size
-                                     ? __ldg(a.c.table + static_cast<size_t>(b) * a.c.stride + pos / a.c.page_size) : -1;
-                if (page >= 0 && page < a.c.num_pages)
-                    d = static_cast<int64_t>(page) * a.c.Hkv * a.c.page_size + pos % a.c.page_size;
-                else
-                    atomicOr(a.err, kErrAppend);
-            }
-            owner[r] = b;
-            dst[r] = d;
-        }
-        if (a.rotate) rope[r][i] = rotation(max(pos, 0), a.turns[i]);
-    }
-    __syncthreads();
-    for (int e = tid; e < words; e += kAppThreads) {
-        const int head = e / (kD / 8), w = e % (kD / 8);
-        const int kv = head - a.Hq;                      // >= 0: a key or value head
-        if (e != tid) load(e);
+    load(h0);
+    int pos;
+    const int b = row_owner(a.rows, row, &pos);
+    if (b < 0) return;
+    int64_t dst = -1;                // (page, row) as a row of head 0; -1: not written
+    const int page = pos >= 0 && pos < a.c.stride * a.c.page_size
+                         ? __ldg(a.c.table + static_cast<size_t>(b) * a.c.stride + pos / a.c.page_size) : -1;
+    if (page >= 0 && page < a.c.num_pages)
+        dst = static_cast<int64_t>(page) * a.c.Hkv * a.c.page_size + pos % a.c.page_size;
+    else if ((threadIdx.x & 63) == 0)
+        atomicOr(a.err, kErrAppend);
+    float4 rope[4];
+    if (a.rotate) {
 #pragma unroll
-        for (int r = 0; r < kAppRows; ++r) {
-            if (owner[r] < 0 || (kv < 0 ? a.q_out == nullptr : dst[r] < 0)) continue;
+        for (int i = 0; i < 4; ++i) rope[i] = rotation(max(pos, 0), a.turns[4 * w + i]);
+    }
+    for (int h = h0; h < heads; h += 4 * kAppHeads) {
+        if (h != h0) load(h);
+#pragma unroll
+        for (int i = 0; i < kAppHeads; ++i) {
+            const int head = h + 4 * i, kv = head - a.Hq;        // kv >= 0: a key or value head
+            if (head >= heads || (kv < 0 ? a.q_out == nullptr : dst < 0)) continue;
             if (a.rotate && kv < a.c.Hkv) {
-                x[r].x = turn(x[r].x, rope[r][4 * w]);
-                x[r].y = turn(x[r].y, rope[r][4 * w + 1]);
-                x[r].z = turn(x[r].z, rope[r][4 * w + 2]);
-                x[r].w = turn(x[r].w, rope[r][4 * w + 3]);
+                x[i].x = turn(x[i].x, rope[0]);
+                x[i].y = turn(x[i].y, rope[1]);
+                x[i].z = turn(x[i].z, rope[2]);
+                x[i].w = turn(x[i].w, rope[3]);
             }
             uint16_t* to;
             if (kv < 0)
-                to = a.q_out + static_cast<size_t>(r0 + r) * a.q_out_stride + head * kD;
+                to = a.q_out + static_cast<size_t>(row) * a.q_out_stride + head * kD;
             else
                 to = (kv < a.c.Hkv ? a.c.k : a.c.v) +
-                     (dst[r] + static_cast<int64_t>(kv < a.c.Hkv ? kv : kv - a.c.Hkv) * a.c.page_size) * kD;
-            reinterpret_cast<uint4*>(to)[w] = x[r];
+                     (dst + static_cast<int64_t>(kv < a.c.Hkv ? kv : kv - a.c.Hkv) * a.c.page_size) * kD;
+            reinterpret_cast<uint4*>(to)[w] = x[i];
         }
     }
 }
