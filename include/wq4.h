@@ -156,8 +156,7 @@ enum wq4_stall {
     WQ4_STALL_NONE = 0,
     WQ4_STALL_GEMM_X = 1,     /* wq4_gemm (17 tokens and more): the activations */
     WQ4_STALL_GEMM_W = 2,     /* ... : the weights and scales */
-    WQ4_STALL_ATTN = 3,       /* wq4_paged_attention, wq4_window_attention: the keys and values */
-    WQ4_STALL_PROMPT = 4      /* wq4_prompt_attention: queries, keys and values */
+    WQ4_STALL_ATTN = 3        /* the attention calls of wq4_attn.h: the keys and values (and a prompt's queries) */
 };
 int wq4_test_copy_stall(int stall);
 

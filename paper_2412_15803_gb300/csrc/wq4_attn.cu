@@ -741,10 +741,11 @@ extern "C" size_t wq4_paged_attention_workspace_bytes(int batch, int n_q_heads, 
 }
 
 namespace wq4 {
+namespace {
 
-int launch_paged_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_stride, const int32_t* seq_lens,
-                           uint16_t* out, int out_stride, int batch, int n_q_heads, float scale, void* workspace,
-                           size_t workspace_bytes, float* sq, int sq_ld, cudaStream_t stream, int window, int sinks)
+int launch_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_stride, const int32_t* seq_lens,
+                     uint16_t* out, int out_stride, int batch, int n_q_heads, float scale, void* workspace,
+                     size_t workspace_bytes, float* sq, int sq_ld, cudaStream_t stream, int window, int sinks)
 {
     if (!check_cache(cache) || !q || !seq_lens || !out || !workspace) return WQ4_ERR_INVALID;
     if (batch < 1 || batch > WQ4_ATTN_MAX_BATCH) return WQ4_ERR_INVALID;
@@ -827,6 +828,16 @@ int launch_paged_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_s
     return e == cudaSuccess ? WQ4_OK : WQ4_ERR_CUDA;
 }
 
+}  // namespace
+
+int launch_paged_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_stride, const int32_t* seq_lens,
+                           uint16_t* out, int out_stride, int batch, int n_q_heads, float scale, void* workspace,
+                           size_t workspace_bytes, float* sq, int sq_ld, cudaStream_t stream)
+{
+    return launch_attention(cache, q, q_stride, seq_lens, out, out_stride, batch, n_q_heads, scale, workspace,
+                            workspace_bytes, sq, sq_ld, stream, 0, 0);
+}
+
 }  // namespace wq4
 
 extern "C" int wq4_paged_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_stride,
@@ -842,8 +853,8 @@ extern "C" int wq4_window_attention(const wq4_kv_cache* cache, const uint16_t* q
                                     float scale, int window, int n_sinks, void* workspace, size_t workspace_bytes,
                                     void* stream)
 {
-    return launch_paged_attention(cache, q, q_stride, seq_lens, out, out_stride, batch, n_q_heads, scale, workspace,
-                                  workspace_bytes, nullptr, 0, static_cast<cudaStream_t>(stream), window, n_sinks);
+    return launch_attention(cache, q, q_stride, seq_lens, out, out_stride, batch, n_q_heads, scale, workspace,
+                            workspace_bytes, nullptr, 0, static_cast<cudaStream_t>(stream), window, n_sinks);
 }
 
 extern "C" int wq4_kv_append(const wq4_kv_cache* cache, const uint16_t* new_k, const uint16_t* new_v, int new_stride,

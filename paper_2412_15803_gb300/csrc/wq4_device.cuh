@@ -20,7 +20,6 @@ constexpr uint32_t kErrFlagTimeout = 2u;   // a wait on another CTA's data gave 
 constexpr uint32_t kErrSeqLen = 8u;        // attention: a length beyond the page table (clamped)
 constexpr uint32_t kErrPageId = 16u;       // attention: a page id outside the pool (zeros read)
 constexpr uint32_t kErrAppend = 32u;       // append: bad position or page id (row not written)
-constexpr uint32_t kErrPool = 128u;        // page pool: a call that could not be done in full
 constexpr uint32_t kErrScale = 64u;        // a scale beyond +-8188 met an fp16 dequantized-weight path
 
 // Largest fp16 scale magnitude whose dequantized weights (q - 7) s, |q - 7|

@@ -32,10 +32,10 @@ uint32_t* status_word();
 int test_copy_stall();
 
 // wq4_paged_attention that also leaves the sums of squares of every (row,
-// query head)'s outputs in sq [batch][sq_ld] (null: none); window 0: no window.
+// query head)'s outputs in sq [batch][sq_ld] (null: none).
 int launch_paged_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_stride, const int32_t* seq_lens,
                            uint16_t* out, int out_stride, int batch, int n_q_heads, float scale, void* workspace,
-                           size_t workspace_bytes, float* sq, int sq_ld, cudaStream_t stream, int window = 0, int sinks = 0);
+                           size_t workspace_bytes, float* sq, int sq_ld, cudaStream_t stream);
 
 // 2-D tiled tensor map (driver entry point, no libcuda link): dims
 // {inner, outer} elements, row pitch row_bytes, box {box_inner, box_outer}.

@@ -26,6 +26,7 @@
 namespace wq4 {
 namespace {
 
+constexpr uint32_t kErrPool = 128u;          // status word: a call that could not be done in full
 constexpr int kD = 128;
 constexpr int kPlan = 1024;                  // threads of a planning block
 constexpr int kPlanWarps = kPlan / 32;

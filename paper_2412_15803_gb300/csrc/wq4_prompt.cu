@@ -21,6 +21,51 @@
 namespace wq4 {
 namespace {
 
+// ------------------------------------------------------- tensor-core pieces --
+
+// 32 consecutive columns of the lane's own row.
+__device__ __forceinline__ void ld32(uint32_t taddr, uint32_t v[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        :
+        "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+        "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+        "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(taddr)
+        : "memory");
+}
+
+__device__ __forceinline__ void st32(uint32_t taddr, const uint32_t v[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+        "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]),
+        "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]),
+        "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+        : "memory");
+}
+
+// Bits of the instruction descriptor: A negated; B stored with N contiguous.
+constexpr uint32_t kIdescNegA = 1u << 13;
+constexpr uint32_t kIdescTransB = 1u << 16;
+
+// Shared-memory matrix descriptor of an operand stored with its M or N extent
+// contiguous, 128-byte swizzle (rows of 128 bytes = 64 fp16, one row a k): the
+// next 64 elements `lead` bytes on (leading byte offset / 16 at bits [16, 30)),
+// the next 8 k 1024 bytes on.  A K step of 16 advances the start by 2048 bytes.
+__device__ __forceinline__ uint64_t sw128_mnmajor_desc(uint32_t saddr, uint32_t lead)
+{
+    return static_cast<uint64_t>((saddr >> 4) & 0x3FFFu) | (static_cast<uint64_t>(lead >> 4) << 16) |
+           (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
 constexpr int kD = 128;
 constexpr int kMaxGroup = 8;
 
@@ -216,7 +261,7 @@ constexpr int kKeys = 128;                         // keys of a tile
 constexpr int kTileBytes = kKeys * kD * 2;         // Q, K and V tiles: two slabs of 64 dims, 128-byte swizzle
 constexpr int kSlab = kTileBytes / 2;
 constexpr int kStages = 2;                         // of keys, and of values
-constexpr float kLift = 8.f, kLazy = 6.f;
+constexpr float kLift = 4.f, kLazy = 11.f;
 constexpr int kItem = 2;                           // an item's own cost, in key tiles
 constexpr int kUncut = 4;                          // key tiles that a context may have for its items to stay whole
 constexpr int kMinShare = 4;                       // places of a block's share, at least
@@ -304,25 +349,31 @@ __device__ __noinline__ void attend_row(const PromptArgs& a, int b, int pos, int
     *reinterpret_cast<uint2*>(a.out + static_cast<size_t>(row) * a.out_stride + head * kD + 4 * lane) = w;
 }
 
-// What the rows at positions [pf, pl] of one item see, in tiles of 128 keys: tile
-// i of its list is tile i of the sequence, or i + gap from `front` on.
+// What the rows at positions [pf, pl] of one item see: a list of tokens in tiles
+// of 128.  Place x of the list is token x, from `front` on token x + gap: the
+// boxes (a.box tokens) between the sinks and the window are not in the list, so
+// that a few sinks share a tile with the window's first tokens.
 struct Seen {
     int pf, pl, tiles, front, gap;
-    __device__ __forceinline__ int token0(int i) const { return (i < front ? i : i + gap) * kKeys; }
+    __device__ __forceinline__ int token(int x) const { return x + (x >= front ? gap : 0); }
 };
 
-__device__ __forceinline__ Seen seen_by(int pf, int pl, int cap, int window, int sinks)
+__device__ __forceinline__ Seen seen_by(const PromptArgs& a, int pf, int pl)
 {
     Seen s;
     s.pf = pf;
-    s.pl = min(pl, cap - 1);
-    const int all = s.pl >= 0 ? s.pl / kKeys + 1 : 0;
+    s.pl = min(pl, a.c.stride * a.c.page_size - 1);
+    const int all = max(s.pl + 1, 0);
     s.front = s.gap = 0;
-    if (window) {
-        s.front = min((min(sinks, max(s.pl, -1) + 1) + kKeys - 1) / kKeys, all);
-        s.gap = max(0, min(max(0, pf - window + 1) / kKeys, all) - s.front);
+    if (a.window) {
+        const int front = (min(a.sinks, all) + a.box - 1) & -a.box, first = max(0, pf - a.window + 1) & -a.box;
+        if (first > front) {
+            s.front = front;
+            s.gap = first - front;
+        }
     }
-    s.tiles = max(1, all - s.gap);               // an item without keys still writes its zeros
+    // (positions beyond the table's end may leave the sinks alone); an item without keys still writes its zeros
+    s.tiles = max(1, (max(all - s.gap, min(s.front, all)) + kKeys - 1) / kKeys);
     return s;
 }
 
@@ -355,7 +406,7 @@ struct Piece {
 __device__ __forceinline__ Seen item_seen(const PromptArgs& a, const Seqs& s, int b, int qt, int tt)
 {
     const int pf = s.len[b] - s.n[b] + qt * tt;
-    return seen_by(pf, pf + min(tt, s.n[b] - qt * tt) - 1, a.c.stride * a.c.page_size, a.window, a.sinks);
+    return seen_by(a, pf, pf + min(tt, s.n[b] - qt * tt) - 1);
 }
 
 __device__ __forceinline__ bool next_piece(const PromptArgs& a, const Seqs& s, int g_begin, Walk& w, Piece& p)
@@ -402,10 +453,12 @@ __device__ __forceinline__ int turns(const Piece& p, int w)
 
 __device__ __forceinline__ int turn_tile(const Piece& p, int w, int k) { return p.t0 + (p.dual ? 2 * k + w : k); }
 
-// Whether the rows at [pf, pl] see every key of the tile at t0; end: the last token of the cache.
-__device__ __forceinline__ bool sees_all(int t0, int pf, int pl, int end, int window, int sinks)
+// Whether the rows at [pf, pl] see every key of tile i of the list; end: the last token of the cache.
+__device__ __forceinline__ bool sees_all(const PromptArgs& a, int i, int front, int gap, int pf, int pl, int end)
 {
-    return t0 + kKeys - 1 <= min(pf, end) && (!window || t0 > pl - window || t0 + kKeys <= sinks);
+    const int x = i * kKeys, t = x + (x >= front ? gap : 0);
+    return t + kKeys - 1 <= min(pf, end) && (!a.window || t > pl - a.window || t + kKeys <= a.sinks) &&
+           (x >= front || x + kKeys <= front);
 }
 
 struct Ring {
@@ -711,14 +764,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             bool ok = true;
             const int boxes = kKeys / a.box;
             const uint32_t qbytes = static_cast<uint32_t>(a.G * tok) * 128u * 2u;
-            // A lane a box and half.  Boxes without a visible token, or on a page outside the
+            // A lane a box and half.  Boxes behind the last token, or on a page outside the
             // pool, lie wholly outside the tensor: the copy reads zeros.  The next tile's
             // page ids are under way while this one's copies are issued.
             constexpr int kHidden = INT_MIN;
             auto lookup = [&](const int32_t* table, int i) {
-                const int t = p.seen.token0(i) + (lane >> 1) * a.box;
-                const bool needed = lane < 2 * boxes && t <= p.seen.pl && (!a.window || t < a.sinks || t + a.box - 1 > p.seen.pf - a.window);
-                return needed ? __ldg(table + t / a.c.page_size) : kHidden;
+                const int t = p.seen.token(i * kKeys + (lane >> 1) * a.box);
+                return lane < 2 * boxes && t <= p.seen.pl ? __ldg(table + t / a.c.page_size) : kHidden;
             };
             auto tile = [&](int y) {
                 if (issued >= kStages && ok) ok = mbar_wait(&empty[ring.slot], ring.par ^ 1u, err);
@@ -739,7 +791,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const int next = i + 1 < p.t1 ? lookup(table, i + 1) : kHidden;
                     int y = -a.box;
                     if (page >= 0 && page < a.c.num_pages)
-                        y = (page * a.c.Hkv + p.h) * a.c.page_size + (p.seen.token0(i) + (lane >> 1) * a.box) % a.c.page_size;
+                        y = (page * a.c.Hkv + p.h) * a.c.page_size + p.seen.token(i * kKeys + (lane >> 1) * a.box) % a.c.page_size;
                     else if (page != kHidden)
                         atomicOr(err, kErrPageId);
                     page = next;
@@ -772,12 +824,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             // than branched to, or their operands pass through vector registers (8192
             // tokens of 32 heads 724 us with a branch and a search for each turn's kind).
             const uint32_t idesc_s = tc::idesc_f16_f32(128, kKeys) | a.neg;
-            const uint32_t idesc_o = tc::idesc_f16_f32(128, kD) | tc::kIdescTransB;
+            const uint32_t idesc_o = tc::idesc_f16_f32(128, kD) | kIdescTransB;
             const uint32_t tb = __shfl_sync(0xffffffffu, tbase, 0);
             const uint32_t leader = tc::elect_one() ? 1u : 0u;
             const uint64_t qdesc = tc::sw128_kmajor_desc(smem_addr(smem + kOffQ));
             const uint64_t kdesc = tc::sw128_kmajor_desc(smem_addr(smem + kOffRing));
-            const uint64_t vdesc = tc::sw128_mnmajor_desc(smem_addr(smem + kOffRing + kStages * kTileBytes), kSlab);
+            const uint64_t vdesc = sw128_mnmajor_desc(smem_addr(smem + kOffRing + kStages * kTileBytes), kSlab);
             Ring kr, vr;                     // the next key tile, the next value tile
             uint32_t qpar[2] = {0, 0}, ppar[2] = {0, 0};
             bool ok = true;
@@ -890,12 +942,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int i = p.t0; i < p.t1; ++i) {
                     if (ok) ok = mbar_wait(&vfull[vr.slot], vr.par, err);
                     __syncwarp();
-                    const int t0 = p.seen.token0(i), pf = p.seen.pf, pl = p.seen.pl;
-                    if (!sees_all(t0, pf, pl, pl, a.window, a.sinks)) {
+                    const int pf = p.seen.pf, pl = p.seen.pl, gap = p.seen.gap;
+                    if (!sees_all(a, i, p.seen.front, gap, pf, pl, pl)) {
                         uint8_t* base = smem + kOffRing + (kStages + vr.slot) * kTileBytes + ((lane >> 3) & 1) * kSlab + (lane & 7) * 16;
                         __half2 big = __float2half2_rn(0.f);
-                        auto clip = [&](int tkn) { return min(max(tkn - t0, 0), kKeys); };
-                        // [from, to) of the tile's rows: 16 lanes a row
+                        auto clip = [&](int x) { return min(max(x - i * kKeys, 0), kKeys); };
+                        // places [from, to) of the list, as far as they lie in the tile: 16 lanes a row
                         auto zero = [&](int from, int to) {
                             for (int r = clip(from) + (lane >> 4); r < clip(to); r += 2)
                                 *reinterpret_cast<uint4*>(base + r * 128) = make_uint4(0, 0, 0, 0);
@@ -913,17 +965,19 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 }
                             }
                         };
-                        // Seen by no row: behind pl, and between the sinks and pf - window (whole boxes
-                        // there were copied as zeros).  Seen by some: from pf on, and up to pl - window.
-                        zero(pl + 1, (pl / a.box + 1) * a.box);
-                        look(max(pf, -1) + 1, pl + 1);
+                        // Seen by no row: behind pl in its box, and between the sinks and the window in
+                        // theirs.  Seen by some: behind pf, and up to pl - window.
+                        zero(pl + 1 - gap, (pl / a.box + 1) * a.box - gap);
+                        look(max(pf, -1) + 1 - gap, pl + 1 - gap);
                         if (a.window) {
                             const int gone = pf - a.window + 1;    // the first token that the window shows
-                            if (gone > a.sinks) {
-                                zero(a.sinks, min(gone, (a.sinks + a.box - 1) / a.box * a.box));
-                                zero(max(a.sinks, gone / a.box * a.box), gone);
+                            if (gap) {
+                                zero(a.sinks, p.seen.front);
+                                zero(p.seen.front, gone - gap);
+                            } else {
+                                zero(a.sinks, gone);
                             }
-                            look(max(a.sinks, gone), min(pl - a.window, pf) + 1);
+                            look(max(a.sinks, gone) - gap, min(pl - a.window, pf) + 1 - gap);
                         }
                         if (__any_sync(0xffffffffu, not_finite(big)) && lane == 0) atomicOr(&again[(piece >> 5) & 31], 1u << (piece & 31));
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -970,16 +1024,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc::fence_after_sync();
                 uint32_t s[128];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) tc::ld32(ts + 32 * c, s + 32 * c);
+                for (int c = 0; c < 4; ++c) ld32(ts + 32 * c, s + 32 * c);
                 tc::ld_wait();
                 pin<128>(s);
-                const int t0 = p.seen.token0(turn_tile(p, w, k));
-                if (!sees_all(t0, pf, pl, p.seen.pl, a.window, a.sinks)) {
-                    // a bit a key: those up to hi, less those from sk to lo
+                const int i = turn_tile(p, w, k);
+                if (!sees_all(a, i, p.seen.front, p.seen.gap, pf, pl, p.seen.pl)) {
+                    // a bit a key: those up to hi, less those from sk to lo; before fr the sinks that lie in front
+                    const int t0 = i * kKeys + p.seen.gap, fr = p.seen.front - i * kKeys, fs = min(min(a.sinks, pos + 1), p.seen.front) - i * kKeys;
                     const int hi = min(pos, p.seen.pl) - t0 + 1, lo = a.window ? pos - a.window - t0 + 1 : 0, sk = a.window ? a.sinks - t0 : 0;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const uint32_t see = first_bits(hi - 32 * c) & (~first_bits(lo - 32 * c) | first_bits(sk - 32 * c));
+                        const uint32_t see = first_bits(fs - 32 * c) | (first_bits(hi - 32 * c) & ~first_bits(fr - 32 * c) &
+                                                                        (~first_bits(lo - 32 * c) | first_bits(sk - 32 * c)));
                         if (__all_sync(0xffffffffu, see == 0xFFFFFFFFu)) continue;       // most: a tile has one edge or two
 #pragma unroll
                         for (int i = 0; i < 32; ++i) s[32 * c + i] = see & (1u << i) ? s[32 * c + i] : 0xFF800000u;   // -infinity
@@ -1010,18 +1066,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                     pk[c] = half2_bits(x0, x1);
                 }
                 l2 = fma2(l2, pair(alpha, alpha), add2(sum[0], sum[1]));
-                tc::st32(ts, pk);
-                tc::st32(ts + 32, pk + 32);
+                st32(ts, pk);
+                st32(ts + 32, pk + 32);
                 if (k > 0 && __any_sync(0xffffffffu, up)) {
 #pragma unroll 1
                     for (int c = 0; c < 4; ++c) {
                         uint32_t o[32];
-                        tc::ld32(to + 32 * c, o);
+                        ld32(to + 32 * c, o);
                         tc::ld_wait();
                         pin<32>(o);
 #pragma unroll
                         for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                        tc::st32(to + 32 * c, o);
+                        st32(to + 32 * c, o);
                     }
                 }
                 tc::st_wait();
@@ -1070,10 +1126,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
                 for (int c = 0; c < 4; ++c) {
                     uint32_t o[32];
-                    tc::ld32(to + 32 * c, o);
+                    ld32(to + 32 * c, o);
                     if (joined) {
                         uint32_t o1[32];
-                        tc::ld32(to + 128 + 32 * c, o1);
+                        ld32(to + 128 + 32 * c, o1);
                         tc::ld_wait();
                         pin<32>(o);
                         pin<32>(o1);
@@ -1392,11 +1448,11 @@ extern "C" int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q
     a.sinks = std::min(n_sinks, cap);
     a.sl2 = static_cast<float>(std::fabs(static_cast<double>(scale)) * 1.4426950408889634);
     if (a.sl2 < FLT_MIN) a.sl2 = FLT_MIN;        // every weight alike, and masked scores still -infinity
-    a.neg = scale < 0.f ? tc::kIdescNegA : 0u;
+    a.neg = scale < 0.f ? kIdescNegA : 0u;
     a.box = 16;
     while (a.box < kKeys && cache->page_size % (2 * a.box) == 0) a.box *= 2;
     a.wide = aligned(out, 32) && out_stride % 16 == 0 ? 1 : 0;
-    a.stall = test_copy_stall() == WQ4_STALL_PROMPT ? 1 : 0;
+    a.stall = test_copy_stall() == WQ4_STALL_ATTN ? 1 : 0;
     a.desc = static_cast<int32_t*>(workspace);
     a.slots = static_cast<uint8_t*>(workspace) + prompt_desc_bytes(prompt_grid(di));
     a.err = status_word();

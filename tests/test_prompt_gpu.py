@@ -192,7 +192,7 @@ def test_without_its_copies_it_ends():
         want = call.result()
         assert wq4.wq4_device_status() == 0
         try:
-            wq4.wq4_test_copy_stall(4)
+            wq4.wq4_test_copy_stall(3)
             call()
             torch.cuda.synchronize()
         finally:
