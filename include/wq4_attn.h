@@ -172,7 +172,7 @@ size_t wq4_prompt_attention_workspace_bytes(int batch, int rows, int n_q_heads, 
  * (appended before) included: the row at position i sees
  *   t <= i  with  window == 0  or  t > i - window  or  t < n_sinks
  * and o is as for wq4_paged_attention over those tokens; a row that sees none
- * (position below 0) gets zeros.  Grouping, scale and the accuracy contract are
+ * (position below 0), or only scores of -infinity, gets zeros.  Grouping, scale and the accuracy contract are
  * those of wq4_paged_attention.
  *   q, out : fp16 rows of q_stride, out_stride elements, [n_q_heads][head_dim]
  *            each; 16-byte aligned, strides % 8 == 0; out must not overlap the
