@@ -317,6 +317,41 @@ def test_same_bits_again_captured_and_on_other_streams():
     assert wq4.wq4_device_status() == 0
 
 
+def test_a_captured_call_follows_its_arrays():
+    """Lengths, row starts and the table are read on the device: a graph's replay takes their new contents."""
+    q, k, v, table, _, starts, lens = make(20, [60, 200], [900, 30], 8, 2, 16, hide=False)
+    call = Call(q, k, v, table, starts, lens, 8)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        call(100, 20, stream=s)
+    for new, T in (([60, 200], [960, 230]), ([1, 0], [17, 3]), ([130, 130], [130, 200]), ([0, 0], [5, 6]), ([0, 260], [1, 230])):
+        starts, lens = starts_of(new), np.asarray(T, np.int32)
+        flipped = table.copy()
+        flipped[:, :1] = table[::-1, :1]                          # another page in front
+        call.table.copy_(dev(flipped, np.int32))
+        call.starts.copy_(dev(np.asarray(starts, np.int32), np.int32))
+        call.lens.copy_(dev(lens, np.int32))
+        call.out.fill_(-1)
+        g.replay()
+        check(call.result(), q, k, v, flipped, starts, lens, 8, 100, 20)
+    assert wq4.wq4_device_status() == 0
+
+
+def test_a_row_of_nothing_but_minus_infinity_gets_zeros():
+    q, k, v, table, given, starts, lens = make(21, [20], [0], 2, 1, 16)
+    q[:] = 0x3C00                                                 # ones
+    k[table[0, 0], 0, :4, 0] = 0xFC00                             # the first four tokens score -infinity
+    call = Call(q, k, v, given, starts, lens, 2)
+    call()
+    got = call.result()
+    assert np.all(got[:4] == 0)
+    o, A, _ = oc.attention(q[4:], k, v, table, [0, 16], [20], SCALE, 2)
+    g = oracle.half_to_double(np.ascontiguousarray(got[4:])).reshape(o.shape)
+    assert np.all(np.abs(g - o) <= oc.attention_tolerance(o, A))
+
+
 # ------------------------------------------------------------------ append --
 
 def run_append(qkv, k, v, table, starts, lens, Hq, Hkv, theta, in_place=False, want_q=True):
