@@ -172,8 +172,11 @@ size_t wq4_prompt_attention_workspace_bytes(int batch, int rows, int n_q_heads, 
  * (appended before) included: the row at position i sees
  *   t <= i  with  window == 0  or  t > i - window  or  t < n_sinks
  * and o is as for wq4_paged_attention over those tokens; a row that sees none
- * (position below 0), or only scores of -infinity, gets zeros.  Grouping, scale and the accuracy contract are
- * those of wq4_paged_attention.
+ * (position below 0), or only scores of -infinity, gets zeros.  Grouping, scale
+ * and the accuracy contract are those of wq4_paged_attention.  A call whose key
+ * tiles, were every row at the page table's end, pass 2^30 (over a million rows
+ * of 8 key/value heads by 4 with room for a million tokens) returns
+ * WQ4_ERR_UNSUPPORTED: split it into chunks.
  *   q, out : fp16 rows of q_stride, out_stride elements, [n_q_heads][head_dim]
  *            each; 16-byte aligned, strides % 8 == 0; out must not overlap the
  *            inputs or the workspace.
@@ -183,7 +186,8 @@ size_t wq4_prompt_attention_workspace_bytes(int batch, int rows, int n_q_heads, 
  * be anything.  What a row does not see (NaN included) does not reach it.
  * Positions at or beyond the page table's end: the length is clamped there for
  * keys and values and bit 3 flagged; a page id outside the pool among the seen
- * ones reads as zeros and flags bit 4.  Deterministic on one device.
+ * ones reads as zeros and flags bit 4.  Row starts that decrease anywhere: no row
+ * is computed, bit 3 is flagged.  Deterministic on one device.
  */
 int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_stride, const int32_t* row_starts,
                          const int32_t* seq_lens, uint16_t* out, int out_stride, int batch, int rows, int n_q_heads,
@@ -207,7 +211,8 @@ int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_str
  * lowest-numbered free ones in order, so its result depends on the state alone.
  *   layers     : HOST array of num_layers caches, each with this page_table;
  *                at most WQ4_KV_MAX_LAYERS.
- *   page_table : device int32 [max_seqs][layers[0].page_table_stride].
+ *   page_table : device int32 [max_seqs][layers[0].page_table_stride], less than
+ *                2^31 entries (and a page less than 2^26 rows of all its heads).
  *   seq_lens   : device int32 [max_seqs];  max_seqs <= WQ4_KV_MAX_SEQS.
  *   page_refs  : device int32 [num_pages].
  *   workspace  : device memory of wq4_kv_pool_workspace_bytes(), 16-byte aligned,

@@ -67,6 +67,7 @@ __device__ __forceinline__ uint64_t sw128_mnmajor_desc(uint32_t saddr, uint32_t 
 
 constexpr int kD = 128;
 constexpr int kMaxGroup = 8;
+constexpr int kMaxHeads = 1 << 16;                 // widths of rows stay within an int
 
 // Rows of the batch: whose each is, and where it stands.
 struct Rows {
@@ -673,9 +674,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     grid_dependents_launch();
 
     // the sequences' rows, lengths and key tiles; their prefix
+    bool unordered = false;
     for (int b = warp; b < batch; b += kThreads / 32) {
-        const int s = min(max(a.rows.starts[b], 0), a.rows.rows);
-        const int n = min(max(a.rows.starts[b + 1], s), a.rows.rows) - s;
+        const int begin = a.rows.starts[b], end = a.rows.starts[b + 1];
+        const int s = min(max(begin, 0), a.rows.rows), n = min(max(end, s), a.rows.rows) - s;
+        unordered |= end < begin;
         const int L = max(a.rows.lens[b], 0);
         if (lane == 0) {
             sn[b] = n;
@@ -697,7 +700,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             smost[b] = most;
         }
     }
-    __syncthreads();
+    // Starts that go down may own rows twice, and more places than an int counts (the
+    // host has checked that others do not): no block has any then.
+    unordered = __syncthreads_or(unordered) != 0;
+    if (unordered && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(err, kErrSeqLen);
     if (warp == 0) {
         // An item a block, whole, where they fill a quarter of the blocks or more and the
         // longest is not much longer than a fair share and what a cut costs (parts written
@@ -734,7 +740,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (lane == 0) pre[batch] = carry;
         __syncwarp();
-        const int total = a.c.Hkv * carry, grid = static_cast<int>(gridDim.x);
+        const int total = unordered ? 0 : a.c.Hkv * carry, grid = static_cast<int>(gridDim.x);
         const int R = max((total + grid - 1) / grid, uncut ? 1 : kMinShare);
         const int g = min(static_cast<int64_t>(total), static_cast<int64_t>(blockIdx.x) * R);
         if (g < total) {
@@ -813,11 +819,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t qbytes = static_cast<uint32_t>(a.G * tok) * 128u * 2u;
             // A lane a box and half.  Boxes behind the last token, or on a page outside the
             // pool, lie wholly outside the tensor: the copy reads zeros.  The next tile's
-            // page ids are under way while this one's copies are issued.
-            constexpr int kHidden = INT_MIN;
+            // page ids are under way while this one's copies are issued (nothing is asked of them before).
+            auto token = [&](int i) { return p.seen.token(i * kKeys + (lane >> 1) * a.box); };
             auto lookup = [&](const int32_t* table, int i) {
-                const int t = p.seen.token(i * kKeys + (lane >> 1) * a.box);
-                return lane < 2 * boxes && t <= p.seen.pl ? table[t / a.c.page_size] : kHidden;
+                int page = 0;
+                if (lane < 2 * boxes && token(i) <= p.seen.pl) page = table[token(i) / a.c.page_size];
+                return page;
             };
             auto tile = [&](int y) {
                 if (issued >= kStages && ok) ok = mbar_wait(&empty[ring.slot], ring.par ^ 1u, err);
@@ -835,12 +842,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int32_t* table = a.c.table + static_cast<size_t>(p.b) * a.c.stride;
                 int page = lookup(table, p.t0);
                 for (int i = p.t0; i < p.t1 && ok; ++i) {
-                    const int next = i + 1 < p.t1 ? lookup(table, i + 1) : kHidden;
+                    const int next = i + 1 < p.t1 ? lookup(table, i + 1) : 0;
                     int y = -a.box;
-                    if (page >= 0 && page < a.c.num_pages)
-                        y = (page * a.c.Hkv + p.h) * a.c.page_size + p.seen.token(i * kKeys + (lane >> 1) * a.box) % a.c.page_size;
-                    else if (page != kHidden)
-                        atomicOr(err, kErrPageId);
+                    if (lane < 2 * boxes && token(i) <= p.seen.pl) {
+                        if (page >= 0 && page < a.c.num_pages)
+                            y = (page * a.c.Hkv + p.h) * a.c.page_size + token(i) % a.c.page_size;
+                        else
+                            atomicOr(err, kErrPageId);
+                    }
                     page = next;
                     tile(y);
                     if (keys && i == p.t0)
@@ -1342,7 +1351,7 @@ int check_rows(const wq4_kv_cache* c, const int32_t* row_starts, const int32_t* 
         batch > WQ4_ATTN_MAX_BATCH || rows < 1)
         return WQ4_ERR_INVALID;
     if (n_q_heads < c->n_kv_heads || n_q_heads % c->n_kv_heads) return WQ4_ERR_INVALID;
-    if (c->head_dim != kD || n_q_heads / c->n_kv_heads > kMaxGroup) return WQ4_ERR_UNSUPPORTED;
+    if (c->head_dim != kD || n_q_heads / c->n_kv_heads > kMaxGroup || n_q_heads > kMaxHeads) return WQ4_ERR_UNSUPPORTED;
     if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->page_table, 4) || !aligned(row_starts, 4) ||
         !aligned(seq_lens, 4))
         return WQ4_ERR_ALIGN;

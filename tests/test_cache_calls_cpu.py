@@ -106,6 +106,20 @@ def test_pool_calls_refuse_a_bad_pool(changes, want):
             L.wq4_kv_trim(r, A, 1, 5, 0, None), L.wq4_kv_compact(r, None), L.wq4_kv_copy_pages(r, A, A, 1, None)] == [want] * 6
 
 
+def test_sizes_that_an_int_does_not_count_are_refused():
+    L = wq4.load()
+    for caches, seqs in (([cache(num_pages=1, n_kv_heads=1 << 10, page_size=1 << 16)], 10), ([cache(page_table_stride=1 << 25)], 64)):
+        p = pool(layers=1, caches=caches, max_seqs=seqs)
+        r = ctypes.byref(p)
+        assert [L.wq4_kv_reserve(r, A, A, 1, None), L.wq4_kv_fork(r, A, A, 1, None), L.wq4_kv_free(r, A, 1, None),
+                L.wq4_kv_trim(r, A, 1, 5, 0, None), L.wq4_kv_compact(r, None), L.wq4_kv_copy_pages(r, A, A, 1, None)] == [UNSUPPORTED] * 6
+    many, wide = cache(num_pages=1, n_kv_heads=1 << 25), 1 << 30
+    for heads in (1 << 25, 1 << 27):
+        assert L.wq4_prompt_append(ctypes.byref(many), 4 * A, wide, 6 * A, wide, 8 * A, 5 * A, 1, 1, heads, 1e4, None) == UNSUPPORTED
+        assert L.wq4_prompt_attention(ctypes.byref(many), 4 * A, wide, 8 * A, 5 * A, 6 * A, wide, 1, 1, heads, 0.1, 0, 0, 7 * A,
+                                      1 << 40, None) == UNSUPPORTED
+
+
 def test_pool_calls_refuse_bad_lists():
     L, p = wq4.load(), pool()
     r = ctypes.byref(p)

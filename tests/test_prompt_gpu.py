@@ -280,6 +280,9 @@ def test_bad_pages_and_lengths_are_flagged():
     bad[0, 2] = k.shape[0]
     Call(q, k, v, bad, starts, lens, 8)()
     assert wq4.wq4_device_status() == 16
+    bad[0, 2] = -2 ** 31
+    Call(q, k, v, bad, starts, lens, 8)()
+    assert wq4.wq4_device_status() == 16
     Call(q, k, v, table, starts, lens + 50, 8)()
     assert wq4.wq4_device_status() == 8
 
@@ -292,6 +295,22 @@ def test_row_starts_of_any_contents_stay_within_the_buffers(starts):
     call()
     assert call.result().shape == guard.shape
     wq4.wq4_device_status()
+
+
+def test_row_starts_that_give_more_tiles_than_an_int_counts():
+    batch, rows, Hkv, cap = 1024, 65536, 8, 1 << 20
+    k = torch.zeros((1, Hkv, 16, D), dtype=torch.int16, device="cuda")
+    table = torch.zeros((batch, cap // 16), dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, rows] * (batch // 2) + [0], dtype=torch.int32, device="cuda")     # every other one owns all rows
+    lens = torch.full((batch,), cap, dtype=torch.int32, device="cuda")
+    q = torch.zeros((rows, Hkv * D), dtype=torch.int16, device="cuda")
+    out = torch.full_like(q, -1)
+    ws = torch.zeros(wq4.wq4_prompt_attention_workspace_bytes(batch, rows, Hkv, Hkv, D), dtype=torch.uint8, device="cuda")
+    wq4.wq4_prompt_attention(wq4.kv_cache_desc(k, k.clone(), table, 16), q, Hkv * D, starts, lens, out, Hkv * D, batch, rows, Hkv, SCALE,
+                             0, 0, ws, ws.numel())
+    torch.cuda.synchronize()
+    assert torch.all(out == -1)
+    assert wq4.wq4_device_status() == 8
 
 
 def test_same_bits_again_captured_and_on_other_streams():
