@@ -15,7 +15,6 @@
 #include <cfloat>
 #include <climits>
 #include <cmath>
-#include <type_traits>
 
 namespace wq4 {
 namespace {
@@ -301,6 +300,8 @@ struct PromptArgs {
     const uint16_t* q;
     uint16_t* out;
     int q_stride, out_stride, G;
+    int tok;                         // tokens of a row tile, kKeys / G
+    int cap;                         // tokens of a sequence that the page table has room for
     int window, sinks;               // window 0: none
     float sl2;                       // |scale| * log2(e), not 0
     uint32_t neg;                    // kIdescNegA for a negative scale
@@ -321,7 +322,7 @@ struct PromptMaps {
 __device__ __noinline__ void attend_row(const PromptArgs& a, int b, int pos, int row, int head)
 {
     const int lane = threadIdx.x & 31, h = head / a.G;
-    const int cap = a.c.stride * a.c.page_size;
+    const int cap = a.cap;
     const uint2 qb = *reinterpret_cast<const uint2*>(a.q + static_cast<size_t>(row) * a.q_stride + head * kD + 4 * lane);
     const float2 q0 = __half22float2(*reinterpret_cast<const __half2*>(&qb.x));
     const float2 q1 = __half22float2(*reinterpret_cast<const __half2*>(&qb.y));
@@ -377,7 +378,7 @@ __device__ __forceinline__ Seen seen_by(const PromptArgs& a, int pf, int pl)
 {
     Seen s;
     s.pf = pf;
-    s.pl = min(pl, a.c.stride * a.c.page_size - 1);
+    s.pl = min(pl, a.cap - 1);
     const int all = max(s.pl + 1, 0);
     s.front = s.gap = 0;
     if (a.window) {
@@ -428,7 +429,7 @@ __device__ __forceinline__ Seen item_seen(const PromptArgs& a, const Seqs& s, in
 __device__ __forceinline__ bool next_piece(const PromptArgs& a, const Seqs& s, int g_begin, Walk& w, Piece& p)
 {
     if (w.g >= w.end) return false;
-    const int tok = kKeys / a.G, tt = 2 * tok;
+    const int tok = a.tok, tt = 2 * tok;
     const Seen seen = item_seen(a, s, w.b, w.qt, tt);
     const int uncut = *s.uncut;
     const int t0 = uncut ? 0 : max(0, w.g - w.is - kItem), t1 = uncut ? seen.tiles : min(seen.tiles, w.end - w.is - kItem);
@@ -608,6 +609,28 @@ __device__ __forceinline__ void store32(void* p, const uint32_t v[8])
                  : "memory");
 }
 
+// Four blocks of N words by each of four lanes, transposed: lane j's k-th becomes
+// lane k's j-th.
+template <int N>
+__device__ __forceinline__ void turn_quads(uint32_t* v, int lane)
+{
+#pragma unroll
+    for (int s = 1; s < 4; s *= 2) {
+        const bool upper = lane & s;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            if (b & s) continue;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                uint32_t &lo = v[b * N + i], &hi = v[(b + s) * N + i];
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, upper ? lo : hi, s);
+                lo = upper ? got : lo;
+                hi = upper ? hi : got;
+            }
+        }
+    }
+}
+
 __device__ __forceinline__ int* slot_flag(const PromptArgs& a, int slot)
 {
     return reinterpret_cast<int*>(a.slots + static_cast<size_t>(slot) * kSlotBytes + static_cast<size_t>(kSlotRows) * (kD + 2) * 4);
@@ -641,8 +664,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     int* smost = srow + batch;
     const Seqs S = {pre, sn, slen, srow, const_cast<const int*>(misc) + 40};
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int cap = a.c.stride * a.c.page_size;
-    const int tok = kKeys / a.G, tt = 2 * tok;
+    const int cap = a.cap;
+    const int tok = a.tok, tt = 2 * tok;
     uint32_t* err = a.err;
 
     if (threadIdx.x == 0) {
@@ -879,6 +902,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             // shuffle, warp-uniform for the compiler too, and MMAs are predicated rather
             // than branched to, or their operands pass through vector registers (8192
             // tokens of 32 heads 724 us with a branch and a search for each turn's kind).
+            // One copy of the turn's code serves both groups, both kinds of items and their
+            // ends: with one for each (18) 8192 tokens took 1 % less, but short items, where
+            // the roles' code passes through the instruction cache all the time, more: 32
+            // prompts of 100 to 500 tokens 82.5 us against 77.3, 8 of 500 to 1500 96.3 and
+            // 94.5.
             const uint32_t idesc_s = tc::idesc_f16_f32(128, kKeys) | a.neg;
             const uint32_t idesc_o = tc::idesc_f16_f32(128, kD) | kIdescTransB;
             const uint32_t tb = __shfl_sync(0xffffffffu, tbase, 0);
@@ -887,56 +915,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint64_t kdesc = tc::sw128_kmajor_desc(smem_addr(smem + kOffRing));
             const uint64_t vdesc = sw128_mnmajor_desc(smem_addr(smem + kOffRing + kStages * kTileBytes), kSlab);
             Ring kr, vr;                     // the next key tile, the next value tile
-            uint32_t qpar[2] = {0, 0}, ppar[2] = {0, 0};
+            uint32_t qpar = 0, ppar = 0;     // parities, a bit a group
             bool ok = true;
-            // first, last: of this piece for its Q tile
-            auto scores = [&](auto group, auto twin, bool first, bool last) {
-                constexpr int w = decltype(group)::value;
-                constexpr bool dual = decltype(twin)::value;
-                if (first && (w == 0 || !dual)) {
-                    wait(&qfull[w], qpar[w], ok, err);
-                    qpar[w] ^= 1u;
-                }
-                if (w == 0 || dual) wait(&kfull[kr.slot], kr.par, ok, err);
-                tc::fence_after_sync();
-                const uint64_t qd = qdesc + (w == 0 || dual ? 0u : kTileBytes >> 4);
-                const uint64_t kd = kdesc + kr.slot * (kTileBytes >> 4);
-#pragma unroll
-                for (int s = 0; s < 8; ++s) {
-                    const uint64_t step = (s >> 2) * (kSlab >> 4) + (s & 3) * 2;
-                    mma_ss_if(leader, tb + 128 * w, qd + step, kd + step, idesc_s, s > 0 ? 1u : 0u);
-                }
-                commit_if(leader, &sfull[w]);
-                if (w == 1 || dual) {
-                    commit_if(leader, &kempty[kr.slot]);
-                    kr.next();
-                }
-                if (last) commit_if(leader, &qempty[dual ? 0 : w]);
-            };
-            auto values = [&](auto group, auto twin, bool first, bool last) {
-                constexpr int w = decltype(group)::value;
-                constexpr bool dual = decltype(twin)::value;
-                if (w == 0 || dual) wait(&fixed[vr.slot], vr.par, ok, err);
-                wait(&pfull[w], ppar[w], ok, err);
-                ppar[w] ^= 1u;
-                tc::fence_after_sync();
-                const uint64_t vd = vdesc + vr.slot * (kTileBytes >> 4);
-#pragma unroll
-                for (int s = 0; s < 8; ++s)
-                    mma_ts_if(leader, tb + 256 + 128 * w, tb + 128 * w + 8 * s, vd + s * (2048 >> 4), idesc_o, s > 0 || !first ? 1u : 0u);
-                if (last) commit_if(leader, &ofull[w]);
-                if (w == 1 || dual) {
-                    commit_if(leader, &vempty[vr.slot]);
-                    vr.next();
-                }
-            };
-            using G0 = std::integral_constant<int, 0>;
-            using G1 = std::integral_constant<int, 1>;
-            using Two = std::false_type;     // a row tile each
-            using One = std::true_type;      // one row tile for both
             struct Turns {
                 int nt;                      // tiles of the piece
                 bool dual;
+                __device__ __forceinline__ int count() const { return dual ? nt : 2 * nt; }
             };
             auto fetch = [&](Turns& x) {
                 const int more = next_piece(a, S, g_begin, walk, p) ? 1 : 0;
@@ -945,46 +929,62 @@ __global__ void __launch_bounds__(kThreads, 1)
                 x.dual = __shfl_sync(0xffffffffu, p.dual ? 1 : 0, 0) != 0;
                 return true;
             };
-            // The next piece's first scores are issued behind a group's last values, where the
-            // groups end in their order; so its softmax finds them when its output is stored.
+            // Turn u of a piece is group u & 1's.  Behind its values come the group's next
+            // scores, those of turn u + 2 or, where the groups end in their order, of the next
+            // piece's first turns; so its softmax finds them when its output is stored.
+            // Turns -2 and -1 are the first scores alone.
             Turns x, after;
-            bool have = fetch(x), begun = false;
-            auto first0 = [&](const Turns& y) {
-                if (y.dual) scores(G0{}, One{}, true, y.nt == 1);
-                else scores(G0{}, Two{}, true, y.nt == 1);
-            };
-            auto first1 = [&](const Turns& y) {
-                if (!y.dual) scores(G1{}, Two{}, true, y.nt == 1);
-                else if (y.nt > 1) scores(G1{}, One{}, true, y.nt == 2);
-            };
+            bool have = fetch(x), begun = false, more = false;
             while (have) {
-                if (!begun) {
-                    first0(x);
-                    first1(x);
-                }
-                const bool more = fetch(after);
-                begun = false;
-                if (!x.dual) {
-                    for (int k = 0; k + 1 < x.nt; ++k) {
-                        values(G0{}, Two{}, k == 0, false);
-                        scores(G0{}, Two{}, false, k + 2 == x.nt);
-                        values(G1{}, Two{}, k == 0, false);
-                        scores(G1{}, Two{}, false, k + 2 == x.nt);
+                const int turns = x.count();
+#pragma unroll 1
+                for (int u = begun ? 0 : -2; u < turns; ++u) {
+                    const int w = __shfl_sync(0xffffffffu, u & 1, 0);
+                    if (u == 0) more = fetch(after);
+                    // all that the scores need is known before the wait for the weights
+                    const bool here = u + 2 < turns;
+                    const int v = here ? u + 2 : w, nt = here ? x.nt : after.nt;
+                    const bool dual = here ? x.dual : after.dual;
+                    const bool next = (here || (more && !x.dual)) && !(dual && v >= nt);
+                    const bool new_q = v < 2 && (w == 0 || !dual), last_q = (dual ? v : v >> 1) + 1 == nt;
+                    const bool new_k = w == 0 || dual, last_k = w == 1 || dual;
+                    const uint64_t qd = qdesc + (new_k ? 0u : kTileBytes >> 4);
+                    const uint64_t kd = kdesc + kr.slot * (kTileBytes >> 4);
+                    if (u >= 0) {
+                        if (w == 0 || x.dual) wait(&fixed[vr.slot], vr.par, ok, err);
+                        wait(&pfull[w], (ppar >> w) & 1u, ok, err);
+                        ppar ^= 1u << w;
+                        tc::fence_after_sync();
+                        const uint64_t vd = vdesc + vr.slot * (kTileBytes >> 4);
+#pragma unroll
+                        for (int s = 0; s < 8; ++s)
+                            mma_ts_if(leader, tb + 256 + 128 * w, tb + 128 * w + 8 * s, vd + s * (2048 >> 4), idesc_o, s > 0 || u >= 2 ? 1u : 0u);
+                        if (u + 2 >= turns) commit_if(leader, &ofull[w]);
+                        if (w == 1 || x.dual) {
+                            commit_if(leader, &vempty[vr.slot]);
+                            vr.next();
+                        }
                     }
-                    values(G0{}, Two{}, x.nt == 1, true);
-                    if (more) first0(after);
-                    values(G1{}, Two{}, x.nt == 1, true);
-                    if (more) first1(after);
-                    begun = more;
-                } else {
-                    for (int u = 0; u < x.nt; u += 2) {
-                        values(G0{}, One{}, u == 0, u + 2 >= x.nt);
-                        if (u + 2 < x.nt) scores(G0{}, One{}, false, u + 3 == x.nt);
-                        if (u + 1 == x.nt) break;
-                        values(G1{}, One{}, u == 0, u + 3 >= x.nt);
-                        if (u + 3 < x.nt) scores(G1{}, One{}, false, u + 4 == x.nt);
+                    if (!next) continue;
+                    if (new_q) {
+                        wait(&qfull[w], (qpar >> w) & 1u, ok, err);
+                        qpar ^= 1u << w;
                     }
+                    if (new_k) wait(&kfull[kr.slot], kr.par, ok, err);
+                    tc::fence_after_sync();
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) {
+                        const uint64_t step = (s >> 2) * (kSlab >> 4) + (s & 3) * 2;
+                        mma_ss_if(leader, tb + 128 * w, qd + step, kd + step, idesc_s, s > 0 ? 1u : 0u);
+                    }
+                    commit_if(leader, &sfull[w]);
+                    if (last_k) {
+                        commit_if(leader, &kempty[kr.slot]);
+                        kr.next();
+                    }
+                    if (last_q) commit_if(leader, &qempty[dual ? 0 : w]);
                 }
+                begun = more && !x.dual;
                 x = after;
                 have = more;
             }
@@ -1066,7 +1066,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int rtok = row / a.G, rhead = row - rtok * a.G;
         uint32_t spar = 0, opar = 0;
         bool ok = true;
-        while (next_piece(a, S, g_begin, walk, p)) {
+        for (bool more = next_piece(a, S, g_begin, walk, p); more;) {
             const int base = p.dual ? 0 : w * tok;            // first token of the group's row tile
             const int pos = p.seen.pf + base + rtok;
             const int pf = p.seen.pf + base, pl = min(pf + tok, p.seen.pf + p.ntok) - 1;
@@ -1144,6 +1144,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             float l, lh;
             unpair(l2, l, lh);
             l += lh;
+            Piece after;                     // found while the last values are added (later: 8192 tokens 2 % more)
+            more = next_piece(a, S, g_begin, walk, after);
             if (nk > 0) {
                 wait(&ofull[w], opar, ok, err);
                 opar ^= 1u;
@@ -1224,6 +1226,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (joined) named_barrier_sync(1, 256);      // group 1's output and m, l are read
             tc::fence_before_sync();
+            p = after;
         }
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsLaunch));
     }
@@ -1273,7 +1276,7 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const PromptArgs a)
     const int b = __ldcg(desc + 1), h = __ldcg(desc + 2), row0 = __ldcg(desc + 3), ntok = __ldcg(desc + 4), pf = __ldcg(desc + 5);
     const int slot0 = __ldcg(desc + 6), slot1 = 2 * static_cast<int>(blockIdx.x) + 2;    // the following ones: 2 apart
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int tok = kKeys / a.G;
+    const int tok = a.tok;
     auto place = [&](int r, int& token) {          // row of the item -> its token; whether there is one
         const int rt = (r & 127) / a.G;
         token = (r >> 7) * tok + rt;
@@ -1516,6 +1519,8 @@ extern "C" int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q
     a.q_stride = q_stride;
     a.out_stride = out_stride;
     a.G = G;
+    a.tok = tok;
+    a.cap = cap;
     a.window = window < cap ? window : 0;        // a window that no sequence can outgrow hides nothing
     a.sinks = std::min(n_sinks, cap);
     a.sl2 = static_cast<float>(std::fabs(static_cast<double>(scale)) * 1.4426950408889634);
