@@ -16,9 +16,10 @@
 //
 // Measured: compacting 4096 pages of 16 layers (0.9 of 1.8 GB moved) 286 us, 6.3
 // TB/s of the 6.8 of a copy, of which the plan takes ~10; eight forks of a
-// sequence in 32 layers 15.7 us, trimming and growing 64 sequences 9.5 us, all
+// sequence in 32 layers 13.6 us, trimming and growing 64 sequences 8.3 us, all
 // three with the bookkeeping's copy before them: chains of dependent reads of a
-// few words, each ~0.7 us.
+// few words, each ~0.7 us.  So what does not depend on an earlier step is read ahead
+// of it, and short lists of pages stay in shared memory (16.1 and 9.7 us without).
 #include "wq4.h"
 #include "wq4_attn.h"
 #include "wq4_device.cuh"
@@ -38,6 +39,7 @@ constexpr int kPlan = 1024;                  // threads of a planning block
 constexpr int kPlanWarps = kPlan / 32;
 constexpr int kScan = 16;                    // pages a lane looks at in a pass
 constexpr int kScanPages = kPlan * kScan;
+constexpr int kNear = 2048;                  // free pages that reserve lists in shared memory; more go through the workspace
 constexpr int kCopyThreads = 256;
 constexpr int kHdr = 64;                     // workspace words before the lists
 
@@ -98,16 +100,23 @@ __device__ __forceinline__ int block_scan(int v, int* red, int* total)
     return __shfl_sync(0xffffffffu, wi - w, warp) + incl - v;
 }
 
-// The `want` lowest free pages into a.list; returns how many there are (at most want).
-__device__ int find_free(const PoolArgs& a, int want, int* red)
+// The references of a scan's pass from page `base` on: page base + 512 warp + 32 i + lane.
+__device__ __forceinline__ void load_refs(const PoolArgs& a, int base, int r[kScan])
+{
+    const int p0 = base + (threadIdx.x >> 5) * (32 * kScan) + (threadIdx.x & 31);
+#pragma unroll
+    for (int i = 0; i < kScan; ++i) r[i] = p0 + 32 * i < a.num_pages ? __ldcg(a.refs + p0 + 32 * i) : 1;
+}
+
+// The `want` lowest free pages into list; returns how many there are (at most want).
+// r: the first pass's references, which the caller loads as early as they hold.
+__device__ int find_free(const PoolArgs& a, int want, int* list, int* red, int r[kScan])
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int found = 0;
     for (int base = 0; base < a.num_pages && found < want; base += kScanPages) {
         const int p0 = base + warp * (32 * kScan) + lane;
-        int r[kScan];
-#pragma unroll
-        for (int i = 0; i < kScan; ++i) r[i] = p0 + 32 * i < a.num_pages ? __ldcg(a.refs + p0 + 32 * i) : 1;
+        if (base) load_refs(a, base, r);
         int mine = 0;
 #pragma unroll
         for (int i = 0; i < kScan; ++i) mine += __popc(__ballot_sync(0xffffffffu, r[i] == 0));
@@ -118,7 +127,7 @@ __device__ int find_free(const PoolArgs& a, int want, int* red)
         for (int i = 0; i < kScan; ++i) {
             const uint32_t m = __ballot_sync(0xffffffffu, r[i] == 0);
             const int k = at + __popc(m & ((1u << lane) - 1u));
-            if (r[i] == 0 && k < want) a.list[k] = p0 + 32 * i;
+            if (r[i] == 0 && k < want) list[k] = p0 + 32 * i;
             at += __popc(m);
         }
         found += total;
@@ -166,27 +175,34 @@ __global__ void __launch_bounds__(kPlan) pool_reserve_kernel(const PoolArgs a, c
 {
     __shared__ int red[32];
     __shared__ int first_at[WQ4_KV_MAX_SEQS];
+    __shared__ int near_list[kNear];
     __shared__ int off[WQ4_KV_MAX_SEQS], have[WQ4_KV_MAX_SEQS], seq_of[WQ4_KV_MAX_SEQS], need_of[WQ4_KV_MAX_SEQS];
     grid_dependency_wait();
     grid_dependents_launch();
     const int i = threadIdx.x, lane = i & 31, warp = i >> 5;
     first_at[i] = INT_MAX;
+    int refs[kScan];
+    load_refs(a, 0, refs);
     __syncthreads();
-    int s = -1, L = 0;
+    int s = -1, L = 0, T = 0;
     if (i < n) {
         s = seqs[i];
         L = new_lens[i];
-        if (s < 0 || s >= a.max_seqs) s = -1;
-        else atomicMin(&first_at[s], i);
+        if (s < 0 || s >= a.max_seqs) {
+            s = -1;
+        } else {
+            atomicMin(&first_at[s], i);
+            T = a.lens[s];
+        }
     }
     __syncthreads();
     int need = 0, old = 0;
     if (i < n) {
         if (s >= 0 && first_at[s] != i) s = -1;                            // listed before
-        if (s >= 0 && (L < 0 || L > static_cast<int64_t>(a.stride) * a.page_size || L < a.lens[s])) s = -1;
+        if (s >= 0 && (L < 0 || L > static_cast<int64_t>(a.stride) * a.page_size || L < T)) s = -1;
         if (s < 0) flag(a);
         else {
-            old = pages_of(a, a.lens[s]);
+            old = pages_of(a, T);
             need = pages_of(a, L) - old;
         }
     }
@@ -196,7 +212,8 @@ __global__ void __launch_bounds__(kPlan) pool_reserve_kernel(const PoolArgs a, c
     have[i] = old;
     need_of[i] = need;
     seq_of[i] = s;
-    const int avail = find_free(a, total, red);        // synchronises the block
+    int* list = total <= kNear ? near_list : a.list;
+    const int avail = find_free(a, total, list, red, refs);        // synchronises the block
     // a warp a sequence; from the first that does not fit, none gets any
     for (int k = warp; k < n; k += kPlanWarps) {
         if (seq_of[k] < 0 || need_of[k] == 0) continue;
@@ -206,7 +223,7 @@ __global__ void __launch_bounds__(kPlan) pool_reserve_kernel(const PoolArgs a, c
         }
         int32_t* row = a.table + static_cast<size_t>(seq_of[k]) * a.stride + have[k];
         for (int j = lane; j < need_of[k]; j += 32) {
-            const int p = a.list[off[k] + j];
+            const int p = list[off[k] + j];
             row[j] = p;
             a.refs[p] = 1;
         }
@@ -222,7 +239,8 @@ __global__ void __launch_bounds__(kPlan) pool_fork_kernel(const PoolArgs a, cons
     __shared__ int red[32];
     __shared__ int child_at[WQ4_KV_MAX_SEQS];
     __shared__ uint8_t is_parent[WQ4_KV_MAX_SEQS];
-    __shared__ int par[WQ4_KV_MAX_SEQS], chi[WQ4_KV_MAX_SEQS], page[WQ4_KV_MAX_SEQS];
+    __shared__ int par[WQ4_KV_MAX_SEQS], chi[WQ4_KV_MAX_SEQS], page[WQ4_KV_MAX_SEQS], list[WQ4_KV_MAX_SEQS];
+    __shared__ int held[WQ4_KV_MAX_SEQS], len[WQ4_KV_MAX_SEQS];
     grid_dependency_wait();
     grid_dependents_launch();
     const int i = threadIdx.x, lane = i & 31, warp = i >> 5;
@@ -244,14 +262,30 @@ __global__ void __launch_bounds__(kPlan) pool_fork_kernel(const PoolArgs a, cons
         if (c >= 0 && (child_at[c] != i || is_parent[c])) p = c = -1;
         if (c < 0) flag(a);
     }
+    // Lengths, and a page of its own where the parent's last one is not full.  (No parent
+    // is a child, so what a parent has does not change below.)
+    int need = 0, T = 0, last = -1;
+    if (c >= 0) {
+        held[i] = pages_of(a, a.lens[c]);
+        T = a.lens[p];
+        if (T < 0 || T > static_cast<int64_t>(a.stride) * a.page_size) {
+            flag(a);
+            T = 0;
+        }
+        if (T % a.page_size) {
+            last = a.table[static_cast<size_t>(p) * a.stride + T / a.page_size];
+            need = last >= 0 && last < a.num_pages ? 1 : 0;
+        }
+    }
     par[i] = p;
     chi[i] = c;
+    len[i] = T;
     __syncthreads();
     // what the children held goes back first; four entries a lane at a time
     for (int k = warp; k < n; k += kPlanWarps) {
         if (chi[k] < 0) continue;
         int32_t* row = a.table + static_cast<size_t>(chi[k]) * a.stride;
-        const int np = pages_of(a, a.lens[chi[k]]);
+        const int np = held[k];
 #pragma unroll 4
         for (int j = lane; j < np; j += 32) {
             const int e = row[j];
@@ -260,27 +294,16 @@ __global__ void __launch_bounds__(kPlan) pool_fork_kernel(const PoolArgs a, cons
         }
     }
     __syncthreads();
-    // a page of its own where the parent's last one is not full
-    int need = 0, T = 0;
-    if (c >= 0) {
-        T = a.lens[p];
-        if (T < 0 || T > static_cast<int64_t>(a.stride) * a.page_size) {
-            flag(a);
-            T = 0;
-        }
-        if (T % a.page_size) {
-            const int e = a.table[static_cast<size_t>(p) * a.stride + T / a.page_size];
-            need = e >= 0 && e < a.num_pages ? 1 : 0;
-        }
-    }
     int total;
     const int at = block_scan(need, red, &total);
-    const int avail = find_free(a, total, red);
+    int refs[kScan];
+    load_refs(a, 0, refs);
+    const int avail = find_free(a, total, list, red, refs);
     int mine = -1;                                     // the child's own last page
-    if (need && at < avail) mine = a.list[at];
+    if (need && at < avail) mine = list[at];
     page[i] = mine;
     if (i < n) {
-        a.src[i] = mine >= 0 ? a.table[static_cast<size_t>(p) * a.stride + T / a.page_size] : -1;
+        a.src[i] = mine >= 0 ? last : -1;
         a.dst[i] = mine;
         a.rows[i] = T % a.page_size;
         if (mine >= 0) a.refs[mine] = 1;
@@ -299,8 +322,7 @@ __global__ void __launch_bounds__(kPlan) pool_fork_kernel(const PoolArgs a, cons
         if (chi[k] < 0) continue;
         const int32_t* from = a.table + static_cast<size_t>(par[k]) * a.stride;
         int32_t* row = a.table + static_cast<size_t>(chi[k]) * a.stride;
-        const int len = a.lens[par[k]];
-        const int np = len < 0 || len > static_cast<int64_t>(a.stride) * a.page_size ? 0 : pages_of(a, len);
+        const int np = pages_of(a, len[k]);
         for (int j = lane; j < np; j += 32) {
             int e = from[j];
             if (e >= a.num_pages) {
