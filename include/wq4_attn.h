@@ -174,8 +174,8 @@ size_t wq4_prompt_attention_workspace_bytes(int batch, int rows, int n_q_heads, 
  * and o is as for wq4_paged_attention over those tokens; a row that sees none
  * (position below 0), or only scores of -infinity, gets zeros.  Grouping, scale
  * and the accuracy contract are those of wq4_paged_attention.  A call whose key
- * tiles, were every row at the page table's end, pass 2^30 (over a million rows
- * of 8 key/value heads by 4 with room for a million tokens) returns
+ * tiles, were every row at the page table's end, pass 2^30 (without a window a
+ * million rows of 8 key/value heads by 4 with room for a million tokens) returns
  * WQ4_ERR_UNSUPPORTED: split it into chunks.
  *   q, out : fp16 rows of q_stride, out_stride elements, [n_q_heads][head_dim]
  *            each; 16-byte aligned, strides % 8 == 0; out must not overlap the

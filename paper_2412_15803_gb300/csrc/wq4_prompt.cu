@@ -1493,13 +1493,6 @@ extern "C" int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q
     const int width = n_q_heads * kD;
     if (q_stride < width || out_stride < width || !std::isfinite(scale) || window < 0 || n_sinks < 0) return WQ4_ERR_INVALID;
     if (!aligned(q, 16) || q_stride % 8 || !aligned(out, 16) || out_stride % 8 || !aligned(workspace, 256)) return WQ4_ERR_ALIGN;
-    const size_t need = wq4_prompt_attention_workspace_bytes(batch, rows, n_q_heads, cache->n_kv_heads, kD);
-    if (need == 0) return WQ4_ERR_CUDA;
-    if (workspace_bytes < need) return WQ4_ERR_INVALID;
-    const size_t ob = rows_bytes(rows, out_stride, width), cb = cache_bytes(cache);
-    if (overlaps(out, ob, cache->k, cb) || overlaps(out, ob, cache->v, cb) || overlaps(out, ob, workspace, need) ||
-        overlaps(out, ob, q, rows_bytes(rows, q_stride, width)))
-        return WQ4_ERR_INVALID;
     const int Hkv = cache->n_kv_heads, G = n_q_heads / Hkv, tok = kKeys / G;
     const int cap = cache->page_table_stride * cache->page_size;
     // the list of key tiles is indexed in int
@@ -1508,8 +1501,16 @@ extern "C" int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q
     // nothing to join, which needs no launch then (512 tokens of 32 + 8 heads 14.4 us, cut
     // 21.0; eight sequences of 500 44.3 either way).
     a.uncut = (cap + kKeys - 1) / kKeys <= kUncut ? 1 : 0;
-    const int64_t most = a.uncut ? items : items * (cap / kKeys + 1 + kItem);
+    const int64_t span = window ? std::min<int64_t>(cap, int64_t(window) + n_sinks + 2 * tok + 2 * kKeys) : cap;   // an item sees at most
+    const int64_t most = a.uncut ? items : items * (span / kKeys + 1 + kItem);
     if (most >= (int64_t(1) << 30)) return WQ4_ERR_UNSUPPORTED;
+    const size_t need = wq4_prompt_attention_workspace_bytes(batch, rows, n_q_heads, cache->n_kv_heads, kD);
+    if (need == 0) return WQ4_ERR_CUDA;
+    if (workspace_bytes < need) return WQ4_ERR_INVALID;
+    const size_t ob = rows_bytes(rows, out_stride, width), cb = cache_bytes(cache);
+    if (overlaps(out, ob, cache->k, cb) || overlaps(out, ob, cache->v, cb) || overlaps(out, ob, workspace, need) ||
+        overlaps(out, ob, q, rows_bytes(rows, q_stride, width)))
+        return WQ4_ERR_INVALID;
     int dev = 0;
     const DeviceInfo* di = current_device_info(&dev);
     if (!di || !prompt_ready(dev)) return WQ4_ERR_CUDA;

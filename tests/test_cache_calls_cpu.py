@@ -113,6 +113,11 @@ def test_sizes_that_an_int_does_not_count_are_refused():
         r = ctypes.byref(p)
         assert [L.wq4_kv_reserve(r, A, A, 1, None), L.wq4_kv_fork(r, A, A, 1, None), L.wq4_kv_free(r, A, 1, None),
                 L.wq4_kv_trim(r, A, 1, 5, 0, None), L.wq4_kv_compact(r, None), L.wq4_kv_copy_pages(r, A, A, 1, None)] == [UNSUPPORTED] * 6
+    long = cache(num_pages=1 << 16, page_table_stride=1 << 16)              # room for 2^20 tokens
+    assert L.wq4_prompt_attention(ctypes.byref(long), 4 * A, 4096, 8 * A, 5 * A, 6 * A, 4096, 1, 1 << 20, 32, 0.1, 0, 0, 7 * A,
+                                  1 << 40, None) == UNSUPPORTED
+    assert L.wq4_prompt_attention(ctypes.byref(long), 4 * A, 4096, 8 * A, 5 * A, 6 * A, 4096, 1, 1 << 20, 32, 0.1, 4096, 16, 7 * A,
+                                  1 << 40, None) != UNSUPPORTED         # a window's tiles are few
     many, wide = cache(num_pages=1, n_kv_heads=1 << 25), 1 << 30
     for heads in (1 << 25, 1 << 27):
         assert L.wq4_prompt_append(ctypes.byref(many), 4 * A, wide, 6 * A, wide, 8 * A, 5 * A, 1, 1, heads, 1e4, None) == UNSUPPORTED
