@@ -100,9 +100,7 @@ __device__ __forceinline__ int row_owner(const Rows& R, int r, int* pos)
 
 // ----------------------------------------------------------------- append --
 
-constexpr int kAppRows = 2;
-constexpr int kAppHeads = 4;
-constexpr int kAppThreads = 64 * kAppRows;
+constexpr int kAppThreads = 128;
 
 struct AppendArgs {
     Rows rows;
@@ -164,24 +162,29 @@ __device__ __forceinline__ uint32_t turn(uint32_t x, float4 t)
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// A block takes kAppRows rows, 64 threads each: 16 bytes of a head by one thread,
-// every fourth head, kAppHeads heads' loads ahead of their stores.  A thread's four
+// A row is taken by 16 kGroups threads: 16 bytes of a head by one thread, every
+// kGroups-th head, kAhead heads' loads ahead of their stores.  A thread's four
 // rotations serve all its heads in registers (a table in shared memory, read again
 // for each head, cost 18 us of 52 over 8192 rows of 48 heads).  The first heads are
-// under way while the row's place and rotations are found.
+// under way while the row's place and rotations are found.  Few rows take four
+// groups, whose chains are shorter (512 rows 6.0 us, two groups 7.4), many take two,
+// which find half as many rotations (4096 rows 21.2 us, four groups 22.7; 8192 36.6
+// and 37.9); they part at ~10 rows an SM (1280 9.0 and 9.6, 1536 12.5 and 10.5).
+template <int kGroups, int kAhead>
 __global__ void __launch_bounds__(kAppThreads) prompt_append_kernel(const __grid_constant__ AppendArgs a)
 {
     grid_dependency_wait();
     grid_dependents_launch();
-    const int row = blockIdx.x * kAppRows + (threadIdx.x >> 6), h0 = (threadIdx.x >> 4) & 3, w = threadIdx.x & 15;
+    constexpr int kRow = 16 * kGroups;                 // threads of a row
+    const int row = blockIdx.x * (kAppThreads / kRow) + threadIdx.x / kRow, h0 = threadIdx.x / 16 % kGroups, w = threadIdx.x & 15;
     if (row >= a.rows.rows) return;
     const int heads = a.Hq + 2 * a.c.Hkv;
     const uint4* in = reinterpret_cast<const uint4*>(a.qkv + static_cast<size_t>(row) * a.qkv_stride) + w;
-    uint4 x[kAppHeads];
+    uint4 x[kAhead];
     auto load = [&](int h) {         // (a row that no sequence owns is in the buffer too)
 #pragma unroll
-        for (int i = 0; i < kAppHeads; ++i)
-            if (h + 4 * i < heads) x[i] = __ldcs(in + (h + 4 * i) * (kD / 8));
+        for (int i = 0; i < kAhead; ++i)
+            if (h + kGroups * i < heads) x[i] = __ldcs(in + (h + kGroups * i) * (kD / 8));
     };
     load(h0);
     int pos;
@@ -192,18 +195,18 @@ __global__ void __launch_bounds__(kAppThreads) prompt_append_kernel(const __grid
                          ? a.c.table[static_cast<size_t>(b) * a.c.stride + pos / a.c.page_size] : -1;
     if (page >= 0 && page < a.c.num_pages)
         dst = static_cast<int64_t>(page) * a.c.Hkv * a.c.page_size + pos % a.c.page_size;
-    else if ((threadIdx.x & 63) == 0)
+    else if (threadIdx.x % kRow == 0)
         atomicOr(a.err, kErrAppend);
     float4 rope[4];
     if (a.rotate) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) rope[i] = rotation(max(pos, 0), a.turns[4 * w + i]);
     }
-    for (int h = h0; h < heads; h += 4 * kAppHeads) {
+    for (int h = h0; h < heads; h += kGroups * kAhead) {
         if (h != h0) load(h);
 #pragma unroll
-        for (int i = 0; i < kAppHeads; ++i) {
-            const int head = h + 4 * i, kv = head - a.Hq;        // kv >= 0: a key or value head
+        for (int i = 0; i < kAhead; ++i) {
+            const int head = h + kGroups * i, kv = head - a.Hq;        // kv >= 0: a key or value head
             if (head >= heads || (kv < 0 ? a.q_out == nullptr : dst < 0)) continue;
             if (a.rotate && kv < a.c.Hkv) {
                 x[i].x = turn(x[i].x, rope[0]);
@@ -1466,7 +1469,11 @@ extern "C" int wq4_prompt_append(const wq4_kv_cache* cache, const uint16_t* qkv,
     a.err = status_word();
     if (!a.err) return WQ4_ERR_CUDA;
     if (rotate) turns_of(rope_theta, a.turns);
-    return launch(prompt_append_kernel, dim3((rows + kAppRows - 1) / kAppRows), kAppThreads, 0, stream, a);
+    int dev = 0;
+    const DeviceInfo* di = current_device_info(&dev);
+    if (!di) return WQ4_ERR_CUDA;
+    return rows < 10 * di->sm_count ? launch(prompt_append_kernel<4, 6>, dim3((rows + 1) / 2), kAppThreads, 0, stream, a)
+                                    : launch(prompt_append_kernel<2, 8>, dim3((rows + 3) / 4), kAppThreads, 0, stream, a);
 }
 
 extern "C" size_t wq4_prompt_attention_workspace_bytes(int batch, int rows, int n_q_heads, int n_kv_heads, int head_dim)

@@ -415,6 +415,28 @@ def test_append(Hq, Hkv, P, new, ctx, theta):
     assert wq4.wq4_device_status() == 0
 
 
+@pytest.mark.parametrize("Hq,Hkv,new", [(5, 1, [1501, 0, 602]), (16, 2, [2001]), (3, 3, [7] * 300)])
+def test_append_of_many_rows(Hq, Hkv, new):
+    P, lens = 16, np.asarray(new) + 5
+    pages = int(((lens + P - 1) // P).sum()) + 1
+    k, v = synth.kv_cache(4, pages, Hkv, P, D)
+    table = synth.page_table(4, lens, P, pages)
+    starts = starts_of(new)
+    qkv = synth.sum4_fp16(4, 78, 0, (starts[-1] + 3) * (Hq + 2 * Hkv) * D).reshape(starts[-1] + 3, -1)
+    for theta in (THETA, 0.0):
+        got = run_append(qkv, k, v, table, starts, lens, Hq, Hkv, theta)
+        check_append(got, qkv, k, v, table, starts, lens, Hq, Hkv, theta)
+        assert np.all(got[0][starts[-1]:] == 0xFFFF) and np.all(got[0][:, Hq * D:] == 0xFFFF)
+        place = run_append(qkv, k, v, table, starts, lens, Hq, Hkv, theta, in_place=True)
+        assert np.array_equal(place[0][:starts[-1], :Hq * D], got[0][:starts[-1], :Hq * D])
+        assert np.array_equal(place[0][:, Hq * D:], qkv[:, Hq * D:]) and np.array_equal(place[1], got[1]) and np.array_equal(place[2], got[2])
+    assert wq4.wq4_device_status() == 0
+    bad = table.copy()
+    bad[0, -1 if len(new) < 4 else 0] = pages                                # a page outside the pool
+    run_append(qkv, k, v, bad, starts, lens, Hq, Hkv, THETA)
+    assert wq4.wq4_device_status() == 32
+
+
 def test_append_without_a_place_is_flagged():
     k, v = synth.kv_cache(3, 3, 2, 16, D)
     table = np.array([[0, -1], [5, 1]], np.int32)
