@@ -183,7 +183,9 @@ size_t wq4_prompt_attention_workspace_bytes(int batch, int rows, int n_q_heads, 
  *   workspace : device memory of wq4_prompt_attention_workspace_bytes(), 256-byte
  *            aligned, of any contents, not shared by calls that may overlap.
  * Pages of which no row of the call sees a token are not read: their entries may
- * be anything.  What a row does not see (NaN included) does not reach it.
+ * be anything.  What a row does not see (NaN included) does not reach it.  (An
+ * infinite value that a row does see gives an infinity, or NaN where its weight
+ * rounds to 0.)
  * Positions at or beyond the page table's end: the length is clamped there for
  * keys and values and bit 3 flagged; a page id outside the pool among the seen
  * ones reads as zeros and flags bit 4.  Row starts that decrease anywhere: no row

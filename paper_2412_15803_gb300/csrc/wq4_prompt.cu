@@ -326,6 +326,7 @@ __device__ __noinline__ void attend_row(const PromptArgs& a, int b, int pos, int
 {
     const int lane = threadIdx.x & 31, h = head / a.G;
     const int cap = a.cap;
+    const float sl2 = a.neg ? -a.sl2 : a.sl2;        // the MMA's sign is in its descriptor
     const uint2 qb = *reinterpret_cast<const uint2*>(a.q + static_cast<size_t>(row) * a.q_stride + head * kD + 4 * lane);
     const float2 q0 = __half22float2(*reinterpret_cast<const __half2*>(&qb.x));
     const float2 q1 = __half22float2(*reinterpret_cast<const __half2*>(&qb.y));
@@ -348,7 +349,7 @@ __device__ __noinline__ void attend_row(const PromptArgs& a, int b, int pos, int
         }
         const float2 k0 = __half22float2(*reinterpret_cast<const __half2*>(&kb.x));
         const float2 k1 = __half22float2(*reinterpret_cast<const __half2*>(&kb.y));
-        const float x = warp_sum(fmaf(q0.x, k0.x, q0.y * k0.y) + fmaf(q1.x, k1.x, q1.y * k1.y)) * a.sl2;
+        const float x = warp_sum(fmaf(q0.x, k0.x, q0.y * k0.y) + fmaf(q1.x, k1.x, q1.y * k1.y)) * sl2;
         const float mn = fmaxf(m, x), ms = mn == -INFINITY ? 0.f : mn;
         const float f = exp2f(m - ms), p = exp2f(x - ms);
         m = mn;
