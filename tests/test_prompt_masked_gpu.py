@@ -49,3 +49,23 @@ def run(new, ctx, Hq, Hkv, P, where, window=0, sinks=0, scale=SCALE, seed=22):
 @pytest.mark.parametrize("window,sinks,tokens", [(0, 0, (150, 260)), (40, 2, (150,)), (64, 0, (30, 200))])
 def test_scales_of_either_sign(window, sinks, tokens, scale):
     run([300], [20], 8, 2, 16, [(0, t) for t in tokens], window, sinks, scale)
+
+
+@pytest.mark.parametrize("scale", [SCALE, -SCALE])
+@pytest.mark.parametrize("window,sinks,where", [(0, 0, (9005, 9011)), (5000, 40, (9003,)), (5000, 40, (4006,)), (6000, 0, (3010, 9014))])
+def test_a_few_rows_cut_into_many_parts(window, sinks, where, scale):
+    """16 tokens over 9000: 71 key tiles of each of two heads in shares of four, so every item is joined
+    from many parts.  The value is in the first, the last or both: of some rows' future or just behind
+    their window."""
+    run([16], [9000], 8, 2, 16, [(0, t) for t in where], window, sinks, scale)
+
+
+@pytest.mark.parametrize("scale", [SCALE, -SCALE])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (150, 20)])
+@pytest.mark.parametrize("new,ctx", [([200] * 26, [600] * 26), ([120] * 90 + [40], [20] * 90 + [900])])
+def test_several_items_a_block(new, ctx, window, sinks, scale):
+    """182 items of up to seven key tiles, and 362 of one or two (one of eight): more items than blocks,
+    a block's share holds parts of two or three and many are joined from two.  In every third sequence
+    a value in the middle of the new tokens, in every seventh one more at their end."""
+    where = [(b, ctx[b] + new[b] // 2) for b in range(0, len(new), 3)] + [(b, ctx[b] + new[b] - 2) for b in range(0, len(new), 7)]
+    run(new, ctx, 8, 1, 16, where, window, sinks, scale, seed=23)
