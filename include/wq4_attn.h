@@ -14,11 +14,15 @@
  * over the T = seq_lens[b] cached tokens t, token t being row t % page_size
  * of page page_table[b][t / page_size].
  *
- * Accuracy contract: |o - o_ref| <= 2e-3 * sum_t p_t |V_t| + ulp16(|o_ref|)
- * per element, o_ref and p the exact (fp64) result and weights.  The path
- * rounds each weight to fp16 for the value product and normalises by the sum
- * of the same rounded weights (<= 2 * 2^-11 relative per weight); scores and
- * all sums are fp32.  Valid while scale * sum_d |q_d K_t,d| <= 64.
+ * Accuracy contract: |o - o_ref| <= 2e-3 * sum_t p_t |V_t| + 2^-40 * sum_t |V_t| +
+ * ulp16(|o_ref|) per element, o_ref and p the exact (fp64) result and weights, the
+ * sums over the tokens seen.  The path rounds each weight to fp16 for the value
+ * product, in units in which the largest is 2^15: a weight of at least 2^-29 of
+ * the largest is within 2^-11 of itself, a smaller one within 2^-40 of the largest
+ * (the second term, felt only where nearly all the weight lies on tokens whose
+ * values are far smaller than the others').  It normalises by the sum of the same
+ * rounded weights; scores and all sums are fp32.  Valid while scale * sum_d |q_d
+ * K_t,d| <= 64 and values are finite.
  *
  * Conventions are those of wq4.h: device pointers owned by the caller,
  * asynchronous on `stream`, no allocation, argument errors returned before

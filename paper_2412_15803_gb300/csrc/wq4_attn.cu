@@ -57,6 +57,11 @@ constexpr int kMaxParts = 512;                  // parts of one segment the merg
 // shares only add parts to merge.
 constexpr int kShareMin = 8;
 constexpr int kShareWhole = 32;   // fair shares up to this many tiles are cut at the segments' ends
+// Weights go to fp16, and to the sums, times 2^15, with which the largest, 2^15, is
+// still finite: those of 2^-29 of the largest are then normal numbers (without it of
+// 2^-14, and the tail behind a sink that holds nearly all the weight was lost).  A
+// power of two: where no weight is subnormal either way the outputs are the same bits.
+constexpr float kLift = 32768.f;
 
 // Shared memory map (dynamic, base 1024-aligned).
 constexpr int kOffRing = 0;
@@ -490,8 +495,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) paged_attn_kernel(const 
             const float msafe = mnew == -INFINITY ? 0.f : mnew;
             const float alpha = exp2f(m - msafe);
             m = mnew;
-            const uint32_t p01 = pack_half2(exp2f(x0 - msafe), exp2f(x1 - msafe));
-            const uint32_t p23 = pack_half2(exp2f(x2 - msafe), exp2f(x3 - msafe));
+            const uint32_t p01 = pack_half2(kLift * exp2f(x0 - msafe), kLift * exp2f(x1 - msafe));
+            const uint32_t p23 = pack_half2(kLift * exp2f(x2 - msafe), kLift * exp2f(x3 - msafe));
             const float2 f01 = unpack_half2(p01), f23 = unpack_half2(p23);
             l = l * alpha + ((f01.x + f01.y) + (f23.x + f23.y));
 
