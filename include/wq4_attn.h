@@ -177,7 +177,10 @@ size_t wq4_prompt_attention_workspace_bytes(int batch, int rows, int n_q_heads, 
  *   t <= i  with  window == 0  or  t > i - window  or  t < n_sinks
  * and o is as for wq4_paged_attention over those tokens; a row that sees none
  * (position below 0), or only scores of -infinity, gets zeros.  Grouping, scale
- * and the accuracy contract are those of wq4_paged_attention.  A call whose key
+ * and the accuracy contract are those of wq4_paged_attention, but that the largest
+ * weight is at least 2^6 (weights of 2^-20 of it are within 2^-11 of themselves, and
+ * the contract's second term is 2^-31 * sum_t |V_t|) and that the sum that
+ * normalises is of the weights before their rounding.  A call whose key
  * tiles, were every row at the page table's end, pass 2^30 (without a window a
  * million rows of 8 key/value heads by 4 with room for a million tokens) returns
  * WQ4_ERR_UNSUPPORTED: split it into chunks.

@@ -256,10 +256,12 @@ __global__ void __launch_bounds__(kAppThreads) prompt_append_kernel(const __grid
 // (451 against 376); the warps' walks in shared memory (395 against 388).
 //
 // The maximum that weights refer to follows the true one only when that is more
-// than 2^kLazy above it, so that O in tensor memory is rarely rescaled (2^6: one
-// warp in ten every turn, and its group waits; 377 us, 2^11: 363); weights carry a
-// factor 2^kLift and so lie within [0, 2^(kLift + kLazy)] of fp16's range, those of
-// 2^-(24 + kLift) of the largest still above zero.
+// than 2^kLazy above it, so that O in tensor memory is rarely rescaled; weights carry a
+// factor 2^kLift and so lie within [0, 2^(kLift + kLazy)] of fp16's range, 2^15 of
+// which is still finite.  Those of 2^-(14 + kLift) of the largest are normal numbers,
+// those of 2^-(25 + kLift) vanish; the sums take them unrounded.  The two share 15
+// bits: 2^11 and 2^4 take 361 us, 2^9 and 2^6 363, 2^8 364, 2^7 369, 2^6 377 (the best
+// of 90 runs; at 2^6 one warp in ten rescales every turn, and its group waits).
 //
 // Values of masked tokens: a weight of 0 times a NaN or an infinity would reach
 // rows that do not see the token.  In a tile that is not seen whole by all of the
@@ -277,7 +279,7 @@ constexpr int kKeys = 128;                         // keys of a tile
 constexpr int kTileBytes = kKeys * kD * 2;         // Q, K and V tiles: two slabs of 64 dims, 128-byte swizzle
 constexpr int kSlab = kTileBytes / 2;
 constexpr int kStages = 2;                         // of keys, and of values
-constexpr float kLift = 4.f, kLazy = 11.f;
+constexpr float kLift = 6.f, kLazy = 9.f;
 constexpr int kItem = 2;                           // an item's own cost, in key tiles
 constexpr int kUncut = 4;                          // key tiles of contexts whose items stay whole, whatever their number
 constexpr int kMinShare = 4;                       // places of a block's share, at least

@@ -74,3 +74,25 @@ def test_one_token(nats, spread, T, heavy, window, sinks):
     deepest = (nats + 3 * spread) / np.log(2)
     check(out.cpu().numpy().view(np.uint16), q, k, v, table, T, 1, window, sinks,
           0.0 if deepest <= 14 + DECODE_LIFT else 2.0 ** -(25 + DECODE_LIFT))
+
+
+PROMPT_LIFT = 6
+
+
+@pytest.mark.parametrize("nats,spread", TAILS)
+@pytest.mark.parametrize("T,heavy,window,sinks", [(4000, 0, 0, 0), (4000, 0, 3000, 1), (4000, 2000, 0, 0), (500, 300, 400, 4),
+                                                  (9000, 2, 5000, 4)])
+def test_a_prompt(nats, spread, T, heavy, window, sinks):
+    rows = 20
+    q, k, v, table = make(T + window, T, nats, spread, heavy, rows)
+    kd, vd, td, qd, ld = dev(k), dev(v), dev(table, np.int32), dev(q), dev(np.array([T], np.int32), np.int32)
+    out = torch.full((rows, HQ * D), -1, dtype=torch.int16, device="cuda")
+    ws = torch.zeros(wq4.wq4_prompt_attention_workspace_bytes(1, rows, HQ, HKV, D), dtype=torch.uint8, device="cuda")
+    starts = dev(np.array([0, rows], np.int32), np.int32)
+    wq4.wq4_prompt_attention(wq4.kv_cache_desc(kd, vd, td, P), qd, HQ * D, starts, ld, out, HQ * D, 1, rows, HQ, 1.0, window, sinks,
+                             ws, ws.numel())
+    torch.cuda.synchronize()
+    assert wq4.wq4_device_status() == 0
+    deepest = (nats + 3 * spread) / np.log(2)
+    check(out.cpu().numpy().view(np.uint16), q, k, v, table, T, rows, window, sinks,
+          0.0 if deepest <= 14 + PROMPT_LIFT else 2.0 ** -(25 + PROMPT_LIFT))
