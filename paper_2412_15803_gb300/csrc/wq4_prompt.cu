@@ -5,6 +5,7 @@
 #include "wq4_attn.h"
 #include "wq4_device.cuh"
 #include "wq4_host.h"
+#include "wq4_seen.h"
 #include "wq4_tc.cuh"
 
 #include <cuda.h>
@@ -275,7 +276,6 @@ constexpr int kMmaWarp = 8, kKeyWarp = 9, kValueWarp = 10, kMaskWarp = 11;
 // of the launch's 384 x 168.
 constexpr int kRegsLaunch = 168, kRegsSoftmax = 208, kRegsOther = 80;
 static_assert(256 * kRegsSoftmax + 128 * kRegsOther <= kThreads * kRegsLaunch, "registers");
-constexpr int kKeys = 128;                         // keys of a tile
 constexpr int kTileBytes = kKeys * kD * 2;         // Q, K and V tiles: two slabs of 64 dims, 128-byte swizzle
 constexpr int kSlab = kTileBytes / 2;
 constexpr int kStages = 2;                         // of keys, and of values
@@ -299,18 +299,15 @@ constexpr int kOffSeq = kOffMisc + 176;            // int [5][batch] + 1: first 
 
 size_t prompt_smem_bytes(int batch) { return 1024 + kOffSeq + (5 * static_cast<size_t>(batch) + 1) * 4; }
 
-struct PromptArgs {
+struct PromptArgs : View {
     Rows rows;
     Paged c;
     const uint16_t* q;
     uint16_t* out;
     int q_stride, out_stride, G;
     int tok;                         // tokens of a row tile, kKeys / G
-    int cap;                         // tokens of a sequence that the page table has room for
-    int window, sinks;               // window 0: none
     float sl2;                       // |scale| * log2(e), not 0
     uint32_t neg;                    // kIdescNegA for a negative scale
-    int box;                         // cache rows of one copy: a page's, or the part of it that divides a tile
     int uncut;                       // shares of whole items
     int wide;                        // output rows are 32-byte aligned (32 prompts of 100 to 500 tokens 77 us; in 16-byte stores 84)
     int stall;                       // test hook: no key or value is copied
@@ -336,7 +333,7 @@ __device__ __noinline__ void attend_row(const PromptArgs& a, int b, int pos, int
     float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f, o2 = 0.f, o3 = 0.f;
     const int end = min(pos, cap - 1);
     if (pos >= cap && lane == 0) atomicOr(a.err, kErrSeqLen);
-    const int first = a.window ? max(0, pos - a.window + 1) : 0;
+    const int first = a.window ? window_first(a, pos) : 0;
     for (int t = a.window && a.sinks ? 0 : first; t <= end; ++t) {
         if (t < first && t >= a.sinks) t = first;
         if (t > end) break;
@@ -369,34 +366,6 @@ __device__ __noinline__ void attend_row(const PromptArgs& a, int b, int pos, int
     w.x = *reinterpret_cast<const uint32_t*>(&w0);
     w.y = *reinterpret_cast<const uint32_t*>(&w1);
     *reinterpret_cast<uint2*>(a.out + static_cast<size_t>(row) * a.out_stride + head * kD + 4 * lane) = w;
-}
-
-// What the rows at positions [pf, pl] of one item see: a list of tokens in tiles
-// of 128.  Place x of the list is token x, from `front` on token x + gap: the
-// boxes (a.box tokens) between the sinks and the window are not in the list, so
-// that a few sinks share a tile with the window's first tokens.
-struct Seen {
-    int pf, pl, tiles, front, gap;
-    __device__ __forceinline__ int token(int x) const { return x + (x >= front ? gap : 0); }
-};
-
-__device__ __forceinline__ Seen seen_by(const PromptArgs& a, int pf, int pl)
-{
-    Seen s;
-    s.pf = pf;
-    s.pl = min(pl, a.cap - 1);
-    const int all = max(s.pl + 1, 0);
-    s.front = s.gap = 0;
-    if (a.window) {
-        const int front = (min(a.sinks, all) + a.box - 1) & -a.box, first = max(0, pf - a.window + 1) & -a.box;
-        if (first > front) {
-            s.front = front;
-            s.gap = first - front;
-        }
-    }
-    // (positions beyond the table's end may leave the sinks alone); an item without keys still writes its zeros
-    s.tiles = max(1, (max(all - s.gap, min(s.front, all)) + kKeys - 1) / kKeys);
-    return s;
 }
 
 // The batch as every block sees it, in shared memory.
@@ -476,14 +445,6 @@ __device__ __forceinline__ int turns(const Piece& p, int w)
 }
 
 __device__ __forceinline__ int turn_tile(const Piece& p, int w, int k) { return p.t0 + (p.dual ? 2 * k + w : k); }
-
-// Whether the rows at [pf, pl] see every key of tile i of the list; end: the last token of the cache.
-__device__ __forceinline__ bool sees_all(const PromptArgs& a, int i, int front, int gap, int pf, int pl, int end)
-{
-    const int x = i * kKeys, t = x + (x >= front ? gap : 0);
-    return t + kKeys - 1 <= min(pf, end) && (!a.window || t > pl - a.window || t + kKeys <= a.sinks) &&
-           (x >= front || x + kKeys <= front);
-}
 
 struct Ring {
     int slot = 0;
@@ -594,9 +555,6 @@ __device__ __forceinline__ uint32_t half2_bits(float lo, float hi)
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-
-// The lowest n bits (none for n <= 0, all for n >= 32).
-__device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? 0xFFFFFFFFu : (1u << max(n, 0)) - 1u; }
 
 __device__ __forceinline__ __half2 as_half2(uint32_t v) { return *reinterpret_cast<const __half2*>(&v); }
 
@@ -1004,8 +962,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int i = p.t0; i < p.t1; ++i) {
                     if (ok) ok = mbar_wait(&vfull[vr.slot], vr.par, err);
                     __syncwarp();
-                    const int pf = p.seen.pf, pl = p.seen.pl, gap = p.seen.gap;
-                    if (!sees_all(a, i, p.seen.front, gap, pf, pl, pl)) {
+                    if (!sees_all(a, i, p.seen.front, p.seen.gap, p.seen.pf, p.seen.pl, p.seen.pl)) {
                         uint8_t* base = smem + kOffRing + (kStages + vr.slot) * kTileBytes + ((lane >> 3) & 1) * kSlab + (lane & 7) * 16;
                         __half2 big = __float2half2_rn(0.f);
                         auto clip = [&](int x) { return min(max(x - i * kKeys, 0), kKeys); };
@@ -1027,20 +984,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 }
                             }
                         };
-                        // Seen by no row: behind pl in its box, and between the sinks and the window in
-                        // theirs.  Seen by some: behind pf, and up to pl - window.
-                        zero(pl + 1 - gap, (pl / a.box + 1) * a.box - gap);
-                        look(max(pf, -1) + 1 - gap, pl + 1 - gap);
-                        if (a.window) {
-                            const int gone = pf - a.window + 1;    // the first token that the window shows
-                            if (gap) {
-                                zero(a.sinks, p.seen.front);
-                                zero(p.seen.front, gone - gap);
-                            } else {
-                                zero(a.sinks, gone);
-                            }
-                            look(max(a.sinks, gone) - gap, min(pl - a.window, pf) + 1 - gap);
-                        }
+                        hidden_places(a, p.seen, zero, look);
                         if (__any_sync(0xffffffffu, not_finite(big)) && lane == 0) atomicOr(&again[(piece >> 5) & 31], 1u << (piece & 31));
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
@@ -1074,8 +1018,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         bool ok = true;
         for (bool more = next_piece(a, S, g_begin, walk, p); more;) {
             const int base = p.dual ? 0 : w * tok;            // first token of the group's row tile
-            const int pos = p.seen.pf + base + rtok;
-            const int pf = p.seen.pf + base, pl = min(pf + tok, p.seen.pf + p.ntok) - 1;
+            const int pos = p.seen.pf + base + min(rtok, p.ntok - base - 1);      // (rows behind the last token: its)
+            const int pf = p.seen.pf + base, pl = pf + min(tok, p.ntok - base) - 1;
             const int nk = turns(p, w);
             float m = -INFINITY;
             uint64_t l2 = pair(0.f, 0.f);
@@ -1091,13 +1035,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 pin<128>(s);
                 const int i = turn_tile(p, w, k);
                 if (!sees_all(a, i, p.seen.front, p.seen.gap, pf, pl, p.seen.pl)) {
-                    // a bit a key: those up to hi, less those from sk to lo; before fr the sinks that lie in front
-                    const int t0 = i * kKeys + p.seen.gap, fr = p.seen.front - i * kKeys, fs = min(min(a.sinks, pos + 1), p.seen.front) - i * kKeys;
-                    const int hi = min(pos, p.seen.pl) - t0 + 1, lo = a.window ? pos - a.window - t0 + 1 : 0, sk = a.window ? a.sinks - t0 : 0;
+                    const RowMask mask = row_mask(a, p.seen, i, pos);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const uint32_t see = first_bits(fs - 32 * c) | (first_bits(hi - 32 * c) & ~first_bits(fr - 32 * c) &
-                                                                        (~first_bits(lo - 32 * c) | first_bits(sk - 32 * c)));
+                        const uint32_t see = mask.word(c);
                         if (__all_sync(0xffffffffu, see == 0xFFFFFFFFu)) continue;       // most: a tile has one edge or two
 #pragma unroll
                         for (int i = 0; i < 32; ++i) s[32 * c + i] = see & (1u << i) ? s[32 * c + i] : 0xFF800000u;   // -infinity
