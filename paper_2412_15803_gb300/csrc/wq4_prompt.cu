@@ -962,7 +962,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int i = p.t0; i < p.t1; ++i) {
                     if (ok) ok = mbar_wait(&vfull[vr.slot], vr.par, err);
                     __syncwarp();
-                    if (!sees_all(a, i, p.seen.front, p.seen.gap, p.seen.pf, p.seen.pl, p.seen.pl)) {
+                    const int last = p.seen.pf + p.ntok - 1;
+                    if (!sees_all(a, i, p.seen.front, p.seen.gap, p.seen.pf, last, p.seen.pl)) {
                         uint8_t* base = smem + kOffRing + (kStages + vr.slot) * kTileBytes + ((lane >> 3) & 1) * kSlab + (lane & 7) * 16;
                         __half2 big = __float2half2_rn(0.f);
                         auto clip = [&](int x) { return min(max(x - i * kKeys, 0), kKeys); };
@@ -984,7 +985,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 }
                             }
                         };
-                        hidden_places(a, p.seen, zero, look);
+                        hidden_places(a, p.seen, last, zero, look);
                         if (__any_sync(0xffffffffu, not_finite(big)) && lane == 0) atomicOr(&again[(piece >> 5) & 31], 1u << (piece & 31));
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();

@@ -96,12 +96,13 @@ WQ4_SEEN RowMask row_mask(const View& a, const Seen& s, int i, int pos)
 
 // The places [from, to) of the list whose values a mask hides: zero(from, to) of those
 // that no row of the item sees but a copy brings, look(from, to) of those that some see.
+// last: the position of the item's last row (s.pl, but where that lies behind the table's end).
 template <typename Zero, typename Look>
-WQ4_SEEN void hidden_places(const View& a, const Seen& s, Zero zero, Look look)
+WQ4_SEEN void hidden_places(const View& a, const Seen& s, int last, Zero zero, Look look)
 {
     const int pf = s.pf, pl = s.pl, gap = s.gap;
     // Seen by no row: behind pl in its box, and between the sinks and the window in
-    // theirs.  Seen by some: behind pf, and up to the window's beginning at pl.
+    // theirs.  Seen by some: behind pf, and up to the window's beginning at the last row.
     zero(pl + 1 - gap, (pl / a.box + 1) * a.box - gap);
     look(max(pf, -1) + 1 - gap, pl + 1 - gap);
     if (a.window) {
@@ -112,7 +113,7 @@ WQ4_SEEN void hidden_places(const View& a, const Seen& s, Zero zero, Look look)
         } else {
             zero(a.sinks, gone);
         }
-        look(max(a.sinks, gone) - gap, min(window_first(a, pl), pf + 1) - gap);
+        look(max(a.sinks, gone) - gap, min(window_first(a, last), pf + 1) - gap);
     }
 }
 

@@ -70,6 +70,37 @@ static void walk(const View& a, const Seen& s, int pf, int ntok, int tok)
         }
 }
 
+// Which places of a tile the masked-value warp zeroes or looks at; false: it passes the tile by.
+static bool places(const View& a, const Seen& s, int i, int last, std::vector<int>& zeroed, std::vector<int>& looked)
+{
+    if (sees_all(a, i, s.front, s.gap, s.pf, last, s.pl)) return false;
+    auto mark = [i](std::vector<int>& v) {
+        return [i, &v](int from, int to) {
+            for (int r = std::min(std::max(from - i * kKeys, 0), kKeys); r < std::min(std::max(to - i * kKeys, 0), kKeys); ++r) v[r] = 1;
+        };
+    };
+    hidden_places(a, s, last, mark(zeroed), mark(looked));
+    return true;
+}
+
+static void hidden(const View& a, const Seen& s, int pf, int ntok)
+{
+    for (int i = 0; i < s.tiles; ++i) {
+        std::vector<int> zeroed(kKeys, 0), looked(kKeys, 0);
+        places(a, s, i, pf + ntok - 1, zeroed, looked);
+        for (int x = 0; x < kKeys; ++x) {
+            const int t = s.token(i * kKeys + x), seen_rows = [&] {
+                int n = 0;
+                for (int r = 0; r < ntok; ++r) n += sees(a, static_cast<long long>(pf) + r, t);
+                return n;
+            }();
+            if (seen_rows && zeroed[x]) bad("zeroed, but seen: token", t);
+            const bool copied = s.token(i * kKeys + x / a.box * a.box) <= s.pl;      // else the copy brings zeros
+            if (copied && seen_rows < ntok && !zeroed[x] && !looked[x]) bad("not seen by every row, and passed by: token", t);
+        }
+    }
+}
+
 int main(int argc, char** argv)
 {
     if (argc != 4) return 4;
@@ -92,6 +123,7 @@ int main(int argc, char** argv)
         snprintf(g_case, sizeof g_case, "rows at [%d, %d], cap %d, box %d, window %d, sinks %d", pf, pl, a.cap, a.box, a.window, a.sinks);
         const Seen s = seen_by(a, pf, pl);
         if (!strcmp(argv[1], "walk")) walk(a, s, pf, ntok, tok);
+        else hidden(a, s, pf, ntok);
     }
     return g_bad != 0;
 }

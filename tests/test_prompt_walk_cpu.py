@@ -25,3 +25,9 @@ def run(exe, what, seed):
 @pytest.mark.parametrize("seed", range(4))
 def test_lookups_list_and_masks(prompt_walk, seed):
     run(prompt_walk, "walk", seed)
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_values_that_a_mask_hides(prompt_walk, seed):
+    """Of what a copy brings into a tile, all that some row does not see is zeroed or looked at."""
+    run(prompt_walk, "hidden", seed)
