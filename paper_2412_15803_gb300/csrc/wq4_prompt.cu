@@ -1491,7 +1491,7 @@ extern "C" int wq4_prompt_attention(const wq4_kv_cache* cache, const uint16_t* q
     a.G = G;
     a.tok = tok;
     a.cap = cap;
-    a.window = window < cap ? window : 0;        // a window that no sequence can outgrow hides nothing
+    a.window = window;           // (of the table's capacity too: rows behind its end outgrow it)
     a.sinks = std::min(n_sinks, cap);
     a.sl2 = static_cast<float>(std::fabs(static_cast<double>(scale)) * 1.4426950408889634);
     if (a.sl2 < FLT_MIN) a.sl2 = FLT_MIN;        // every weight alike, and masked scores still -infinity

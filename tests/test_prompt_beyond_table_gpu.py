@@ -50,3 +50,11 @@ def test_beyond_the_end(cap, Hq, Hkv, beyond, window, sinks):
 def test_what_only_rows_beyond_the_end_do_not_see(cap, Hq, Hkv, sinks):
     """A NaN that the rows on the table's tokens see and those behind the end, past their window, do not."""
     run(cap, Hq, Hkv, cap + 30, 100, sinks, nan=(cap - 90, cap - 75))
+
+
+@pytest.mark.parametrize("cap,Hq,Hkv", [(320, 8, 2), (1600, 6, 2)])
+@pytest.mark.parametrize("beyond", [1, 30, 1000, None])
+@pytest.mark.parametrize("more,sinks", [(0, 0), (0, 5), (1, 0), (25, 7), (None, 3)])
+def test_windows_of_the_capacity_and_more(cap, Hq, Hkv, beyond, more, sinks):
+    """Rows behind the end outgrow them too."""
+    run(cap, Hq, Hkv, cap + beyond if beyond else MOST, MOST if more is None else cap + more, sinks)
