@@ -35,6 +35,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <cstring>
 #include <mutex>
@@ -45,6 +46,7 @@ namespace {
 constexpr int kD = 128;            // head_dim
 constexpr int kTile = 16;          // tokens per tile
 constexpr int kMaxGroup = 8;       // query heads per kv head
+constexpr int kMaxHeads = INT_MAX / kD;          // a row's elements are counted in int
 constexpr int kConsumers = 4;      // consumer warps
 constexpr int kThreads = (kConsumers + 1) * 32;
 constexpr int kSlots = 8;
@@ -763,15 +765,15 @@ int launch_attention(const wq4_kv_cache* cache, const uint16_t* q, int q_stride,
     if (batch < 1 || batch > WQ4_ATTN_MAX_BATCH) return WQ4_ERR_INVALID;
     const int Hkv = cache->n_kv_heads;
     if (n_q_heads < Hkv || n_q_heads % Hkv) return WQ4_ERR_INVALID;
-    if (cache->head_dim != kD || n_q_heads / Hkv > kMaxGroup) return WQ4_ERR_UNSUPPORTED;
+    if (cache->head_dim != kD || n_q_heads / Hkv > kMaxGroup || n_q_heads > kMaxHeads) return WQ4_ERR_UNSUPPORTED;
     if (q_stride < n_q_heads * kD || out_stride < n_q_heads * kD) return WQ4_ERR_INVALID;
     if (!(scale == scale) || std::isinf(scale) || window < 0 || sinks < 0) return WQ4_ERR_INVALID;
     if (!aligned(q, 16) || q_stride % 8 || !aligned(cache->k, 16) || !aligned(cache->v, 16) ||
         !aligned(out, 4) || out_stride % 2 || !aligned(workspace, 16) || !aligned(seq_lens, 4) ||
         !aligned(cache->page_table, 4))
         return WQ4_ERR_ALIGN;
-    const int64_t rows = static_cast<int64_t>(cache->num_pages) * Hkv * cache->page_size;
-    if (rows >= (int64_t(1) << 31)) return WQ4_ERR_UNSUPPORTED;
+    const int64_t rows = cache_rows(*cache);
+    if (rows < 0) return WQ4_ERR_UNSUPPORTED;
     if (static_cast<int64_t>(cache->page_table_stride) * cache->page_size >= (int64_t(1) << 30))
         return WQ4_ERR_UNSUPPORTED;
     // the tile list (every sequence at its page table's capacity) is indexed in int
@@ -873,7 +875,7 @@ extern "C" int wq4_kv_append(const wq4_kv_cache* cache, const uint16_t* new_k, c
                              const int32_t* positions, int batch, void* stream)
 {
     if (!check_cache(cache) || !new_k || !new_v || !positions || batch < 1) return WQ4_ERR_INVALID;
-    if (cache->head_dim != kD) return WQ4_ERR_UNSUPPORTED;
+    if (cache->head_dim != kD || cache->n_kv_heads > kMaxHeads) return WQ4_ERR_UNSUPPORTED;
     if (new_stride < cache->n_kv_heads * kD) return WQ4_ERR_INVALID;
     if (!aligned(new_k, 16) || !aligned(new_v, 16) || new_stride % 8 || !aligned(cache->k, 16) ||
         !aligned(cache->v, 16) || !aligned(positions, 4) || !aligned(cache->page_table, 4))

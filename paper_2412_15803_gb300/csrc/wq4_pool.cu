@@ -501,8 +501,7 @@ int check_pool(const wq4_kv_pool* pool, PoolArgs* a)
         if (!aligned(c.k, 16) || !aligned(c.v, 16)) return WQ4_ERR_ALIGN;
     }
     // what is counted in int: a sequence's tokens, a layer's rows, a page's 16-byte words, the pages of all sequences
-    if (static_cast<int64_t>(c0.page_table_stride) * c0.page_size >= (int64_t(1) << 30) ||
-        static_cast<int64_t>(c0.num_pages) * c0.n_kv_heads * c0.page_size >= (int64_t(1) << 31) ||
+    if (static_cast<int64_t>(c0.page_table_stride) * c0.page_size >= (int64_t(1) << 30) || cache_rows(c0) < 0 ||
         static_cast<int64_t>(c0.n_kv_heads) * c0.page_size >= (int64_t(1) << 26) ||
         static_cast<int64_t>(pool->max_seqs) * c0.page_table_stride >= (int64_t(1) << 31))
         return WQ4_ERR_UNSUPPORTED;

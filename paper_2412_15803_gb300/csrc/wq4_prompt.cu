@@ -1306,8 +1306,7 @@ int check_rows(const wq4_kv_cache* c, const int32_t* row_starts, const int32_t* 
     if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->page_table, 4) || !aligned(row_starts, 4) ||
         !aligned(seq_lens, 4))
         return WQ4_ERR_ALIGN;
-    if (static_cast<int64_t>(c->num_pages) * c->n_kv_heads * c->page_size >= (int64_t(1) << 31) ||
-        static_cast<int64_t>(c->page_table_stride) * c->page_size >= (int64_t(1) << 30) || rows >= (1 << 30))
+    if (cache_rows(*c) < 0 || static_cast<int64_t>(c->page_table_stride) * c->page_size >= (int64_t(1) << 30) || rows >= (1 << 30))
         return WQ4_ERR_UNSUPPORTED;
     *R = {row_starts, seq_lens, batch, rows};
     *P = {c->k, c->v, c->page_table, c->page_table_stride, c->page_size, c->num_pages, c->n_kv_heads};
