@@ -277,8 +277,8 @@ int wq4_kv_trim(const wq4_kv_pool* pool, const int32_t* seqs, int n, int window,
 int wq4_kv_compact(const wq4_kv_pool* pool, void* stream);
 
 /* Copies page src[i] to page dst[i] in every layer (n up to num_pages; table and
- * references stay as they are).  Refused: an id outside the pool, a page that is
- * the destination of two pairs or both a source and a destination. */
+ * references stay as they are).  Refused: a pair with an id outside the pool, with
+ * a destination that is another's too, or with a source that is any pair's destination. */
 int wq4_kv_copy_pages(const wq4_kv_pool* pool, const int32_t* src, const int32_t* dst, int n, void* stream);
 
 /* ------------------------------------------------------------------------ */
