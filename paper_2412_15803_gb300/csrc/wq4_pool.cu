@@ -65,7 +65,8 @@ __device__ __forceinline__ void flag(const PoolArgs& a) { atomicOr(a.err, kErrPo
 
 __device__ __forceinline__ int pages_of(const PoolArgs& a, int T)
 {
-    return min(a.stride, (max(T, 0) + a.page_size - 1) / a.page_size);
+    const unsigned P = a.page_size;             // (the largest length and a page pass an int)
+    return min(a.stride, static_cast<int>((static_cast<unsigned>(max(T, 0)) + P - 1u) / P));
 }
 
 // One reference of page e less.  A page that had none is flagged and stays at 0.

@@ -82,3 +82,14 @@ def test_copies_of_many_pages(pool):
     for i, c in enumerate(pool.caches):
         assert torch.equal(pool.numbers(c, torch.arange(PAGES, device="cuda")), want)
         assert torch.all(c[:, 0, 0, 2] == i)
+
+
+@pytest.mark.parametrize("length", [STRIDE * P + 1, 2 ** 31 - 17, 2 ** 31 - 1])
+def test_a_length_beyond_the_table_still_frees_its_pages(pool, length):
+    wq4.wq4_kv_reserve(pool.pool, ints([4, 9]), ints([STRIDE * P, 100]), 2)
+    pool.lens[4] = length
+    wq4.wq4_kv_free(pool.pool, ints([4]), 1)
+    torch.cuda.synchronize()
+    assert wq4.wq4_device_status() == 0
+    assert pool.lens[[4, 9]].tolist() == [0, 100] and torch.all(pool.table[4] == -1)
+    assert int(pool.refs.sum()) == 7 and pool.refs[pool.table[9, :7].long()].tolist() == [1] * 7
