@@ -28,6 +28,7 @@
 // cost of a call that is split and merged.
 #include "wq4.h"
 #include "wq4_attn.h"
+#include "wq4_cache.h"
 #include "wq4_device.cuh"
 #include "wq4_host.h"
 

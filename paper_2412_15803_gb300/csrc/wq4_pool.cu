@@ -22,6 +22,7 @@
 // of it, and short lists of pages stay in shared memory (16.1 and 9.7 us without).
 #include "wq4.h"
 #include "wq4_attn.h"
+#include "wq4_cache.h"
 #include "wq4_device.cuh"
 #include "wq4_host.h"
 

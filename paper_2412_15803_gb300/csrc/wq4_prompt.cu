@@ -3,6 +3,7 @@
 // sliding window and first tokens that stay visible.
 #include "wq4.h"
 #include "wq4_attn.h"
+#include "wq4_cache.h"
 #include "wq4_device.cuh"
 #include "wq4_host.h"
 #include "wq4_seen.h"
