@@ -83,7 +83,8 @@ size_t wq4_paged_attention_workspace_bytes(int batch, int n_q_heads, int n_kv_he
  *   n_q_heads  : a multiple of n_kv_heads with n_q_heads / n_kv_heads <= 8.
  *   scale      : the score scale (1/sqrt(head_dim) for standard attention).
  *   workspace  : device memory of wq4_paged_attention_workspace_bytes(),
- *                16-byte aligned, not shared by concurrent calls.
+ *                16-byte aligned, its counters zero (see there), not shared by
+ *                concurrent calls.
  * Sequences are split across the GPU's thread blocks by tokens in equal
  * shares and the shares are merged in a fixed order: the same inputs on the
  * same device give the same bits.  Launched with programmatic dependent
@@ -188,11 +189,16 @@ size_t wq4_prompt_attention_workspace_bytes(int batch, int rows, int n_q_heads, 
  *            each; 16-byte aligned, strides % 8 == 0; out must not overlap the
  *            inputs or the workspace.
  *   workspace : device memory of wq4_prompt_attention_workspace_bytes(), 256-byte
- *            aligned, of any contents, not shared by calls that may overlap.
+ *            aligned, of any contents, not shared by calls that may overlap.  It is
+ *            left with any contents too: wq4_paged_attention and wq4_window_attention,
+ *            whose counters must be zero, may be given it only after it was set to 0
+ *            (else their merges are wrong, and nothing is flagged).
  * Pages of which no row of the call sees a token are not read: their entries may
  * be anything.  What a row does not see (NaN included) does not reach it.  (An
  * infinite value that a row does see gives an infinity, or NaN where its weight
- * rounds to 0.)
+ * rounds to 0.)  Rows beside a value that is not finite and that some row of their
+ * few dozen does not see are right, but computed one by one: milliseconds in place of
+ * microseconds (16 rows of 32 heads over 4096 tokens 9 ms).
  * Positions at or beyond the page table's end: the length is clamped there for
  * keys and values and bit 3 flagged; a page id outside the pool among the seen
  * ones reads as zeros and flags bit 4.  Row starts that decrease anywhere: no row
@@ -267,7 +273,9 @@ int wq4_kv_free(const wq4_kv_pool* pool, const int32_t* seqs, int n, void* strea
 /* Frees the pages of the listed sequences that their coming tokens do not see
  * under a window (>= 1) with n_sinks (>= 0) first tokens: those without a token t
  * < n_sinks or t > seq_lens - window.  Their entries become -1; lengths stay.
- * Refusals as for wq4_kv_free. */
+ * Refusals as for wq4_kv_free.  From then on the sequence is for wq4_window_attention
+ * and wq4_prompt_attention under that window: wq4_paged_attention and wq4_decode_step
+ * see the whole context and take its freed pages for ids outside the pool (bit 4). */
 int wq4_kv_trim(const wq4_kv_pool* pool, const int32_t* seqs, int n, int window, int n_sinks, void* stream);
 
 /* Moves the pages in use to the front of the pool: with m in use, the k-th one at

@@ -246,9 +246,10 @@ __global__ void __launch_bounds__(kAppThreads) prompt_append_kernel(const __grid
 // tensor cores work for the other.  An item of at most one row tile gives both softmax groups that tile,
 // one the even and one the odd key tiles, and adds the two results at its end.
 //
-// What bounds it: 8192 tokens of 32 + 8 heads take 363 us, 1.51 PFLOP/s, 0.80 of
-// the measured cuBLAS burst rate; the tensor pipe is 69 % active at 1.75 GHz (the
-// power limit).  A group's turn is a chain, softmax ~1500 cycles, values 512, next
+// What bounds it: 8192 tokens of 32 + 8 heads take 363 us at best (six calls in a
+// graph), 1.51 PFLOP/s, 0.80 of the measured cuBLAS burst rate, and 393 back to back,
+// 1.40 PFLOP/s, 0.83 of cuBLAS's sustained rate (the power limit); the tensor pipe is
+// 69 % active.  A group's turn is a chain, softmax ~1500 cycles, values 512, next
 // scores 512, and the other group's fills the gaps but for the handovers; leaving
 // out the maximum, half of the exponentials or the stores gains 3 to 4 % each.
 // Measured slower: one score buffer for both groups and weights apart, the scores
@@ -274,7 +275,9 @@ __global__ void __launch_bounds__(kAppThreads) prompt_append_kernel(const __grid
 constexpr int kThreads = 384;
 constexpr int kMmaWarp = 8, kKeyWarp = 9, kValueWarp = 10, kMaskWarp = 11;
 // Registers a thread: the softmax groups take over what the other four warps leave
-// of the launch's 384 x 168.
+// of the launch's 384 x 168.  (ptxas spills 348 bytes.  The counters of 8192 and of 2048
+// tokens put them at the items' ends: a group's turn holds no local store and four
+// local loads, all warps together, among 2660 instructions.)
 constexpr int kRegsLaunch = 168, kRegsSoftmax = 208, kRegsOther = 80;
 static_assert(256 * kRegsSoftmax + 128 * kRegsOther <= kThreads * kRegsLaunch, "registers");
 constexpr int kTileBytes = kKeys * kD * 2;         // Q, K and V tiles: two slabs of 64 dims, 128-byte swizzle
@@ -321,7 +324,11 @@ struct PromptMaps {
     CUtensorMap q, k, v;
 };
 
-// One row and query head by one warp, a token at a time, four dimensions a lane.
+// One row and query head by one warp, a token at a time, four dimensions a lane: a
+// chain of a page id, a row and a reduction, ~0.6 us a token.  A block's 12 warps take
+// ~22 rows each of a whole item of 256, a joining block's 8 warps 4 each: 16 tokens
+// over 4096 9 ms in place of 28 us, a prompt of 4096 tokens with one infinity 63 ms in
+// place of 123 us.
 __device__ __noinline__ void attend_row(const PromptArgs& a, int b, int pos, int row, int head)
 {
     const int lane = threadIdx.x & 31, h = head / a.G;
