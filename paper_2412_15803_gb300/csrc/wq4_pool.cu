@@ -14,9 +14,9 @@
 // kernel over the whole GPU moves the bytes.  free and trim touch each table
 // entry by itself and need one kernel over all of them.
 //
-// Measured: compacting 4096 pages of 16 layers (0.9 of 1.8 GB moved) 286 us, 6.3
+// Measured: compacting 4096 pages of 16 layers (0.9 GB moved) 290 us, 6.2
 // TB/s of the 6.8 of a copy, of which the plan takes ~10; eight forks of a
-// sequence in 32 layers 13.6 us, trimming and growing 64 sequences 8.3 us, all
+// sequence in 32 layers 13.8 us, trimming and growing 64 sequences 8.3 us, all
 // three with the bookkeeping's copy before them: chains of dependent reads of a
 // few words, each ~0.7 us.  So what does not depend on an earlier step is read ahead
 // of it, and short lists of pages stay in shared memory (16.1 and 9.7 us without).
