@@ -156,7 +156,8 @@ enum wq4_stall {
     WQ4_STALL_NONE = 0,
     WQ4_STALL_GEMM_X = 1,     /* wq4_gemm (17 tokens and more): the activations */
     WQ4_STALL_GEMM_W = 2,     /* ... : the weights and scales */
-    WQ4_STALL_ATTN = 3        /* the attention calls of wq4_attn.h: the keys and values (and a prompt's queries) */
+    WQ4_STALL_ATTN = 3,       /* the attention calls of wq4_attn.h: the keys and values (and a prompt's queries) */
+    WQ4_STALL_MX = 4          /* wq4_mx_gemm: weights, activations and their scales */
 };
 int wq4_test_copy_stall(int stall);
 
@@ -176,6 +177,87 @@ const char* wq4_status_string(int status);
  * any bit was set, WQ4_OK otherwise, WQ4_ERR_CUDA on a CUDA failure.
  */
 int wq4_device_status(void* stream, int* flags_out);
+
+/* ------------------------------------------------------------------------ */
+/* Microscaled weights and activations                                        */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * A microscaled (MX) matrix holds rows of K values, K % 128 == 0, as codes of
+ * 8 or 4 bits with one power of two for each 32 consecutive codes of a row:
+ * value(r, k) = code(r, k) * 2^(scale(r, k/32) - 127).  This is the format
+ * that the tensor cores of sm_103a multiply as it is, without an unpacking
+ * step; the paper says only "4-bit quantized" (Section 3).
+ *   codes  bits 8: e4m3 bytes [rows][K] (448 the largest value, no infinity);
+ *          bits 4: e2m1 nibbles [rows][K/2 bytes], the lower nibble first
+ *          (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign).
+ *   scales e8m0 bytes (255: NaN) in blocks of 128 rows by four groups, of 512
+ *          bytes: row r, group g at byte ((r / 128) * (K / 128) + g / 4) * 512
+ *          + (r % 32) * 16 + (r % 128) / 32 * 4 + g % 4.  A buffer holds whole
+ *          blocks (wq4_mx_scale_bytes); bytes of rows behind the last are
+ *          neither written by the calls below nor of any effect.
+ * Codes are made so: a group's scale is the least power of two (2^-127 at
+ * least) with which no value of the group is over the type's largest, each
+ * code its value over the scale, rounded once to nearest even.  A group of
+ * zeros has the scale 1; one with a value that is not finite the scale NaN and
+ * the codes 0, so that what is multiplied with it is NaN.
+ * Conventions for the calls: codes 32-byte aligned, scales 16-byte aligned,
+ * fp16 rows 16-byte aligned with strides (in elements) that are multiples of
+ * 8, y of wq4_mx_gemm 2-byte aligned; outputs overlap neither inputs nor each
+ * other (buffers are compared from their first byte to their last).  bits is 4
+ * or 8, M and N at least 1, N * K at most 2^41.  Launched with programmatic
+ * dependent launch; everything is read after the previous kernel in `stream`
+ * has completed.  Deterministic.  WQ4_ERR_INVALID for sizes, null pointers and
+ * overlaps, WQ4_ERR_ALIGN, WQ4_ERR_CUDA.
+ */
+
+/* Bytes of the scales of `rows` rows of K values; 0 for bad sizes. */
+size_t wq4_mx_scale_bytes(int rows, int K);
+
+/*
+ * y[m][n] = fp16( sum_k x(m,k) * w(n,k) ), m < M, n < N, with microscaled
+ * weights of 4 bits (W, W_scales: N rows) and activations of `bits` bits (x,
+ * x_scales: M rows), on the tensor cores: products are exact, sums in fp32.
+ * Accuracy: |y - y_ref| <= 2^-12 * sum_k |w*x| + ulp16(|y_ref|); a sum beyond
+ * fp16's range comes back as an infinity.  y is fp16 [M][N].
+ */
+int wq4_mx_gemm(const uint8_t* W, const uint8_t* W_scales, const uint8_t* x, const uint8_t* x_scales, uint16_t* y,
+                int N, int K, int M, int bits, void* stream);
+
+/*
+ * The residual's addition, the root-mean-square norm and the projection's
+ * input in one pass over M rows of K:
+ *   h = fp16(x + residual);  codes, scales = microscaled(gain * h / sqrt(mean(h^2) + eps))
+ *   x, residual : fp16 rows, strides x_stride, residual_stride (>= K);
+ *                 residual NULL: h = x (its stride is not looked at).
+ *   gain        : fp16 [K], 16-byte aligned; NULL: 1.
+ *   sum         : receives h, stride sum_stride; NULL: not written.  It may be
+ *                 x or residual itself (same address and stride).
+ *   eps         : finite and > 0.  Norms are held in fp32.
+ */
+int wq4_mx_norm(const uint16_t* x, int x_stride, const uint16_t* residual, int residual_stride, const uint16_t* gain,
+                float eps, uint16_t* sum, int sum_stride, uint8_t* codes, uint8_t* scales, int M, int K, int bits,
+                void* stream);
+
+/*
+ * codes, scales = microscaled(silu(gate) * up) of M fused rows fp16 [gate of K,
+ * up of K], stride >= 2 K; silu(t) = t / (1 + e^-t) in fp32, nothing rounded
+ * before the codes.
+ */
+int wq4_mx_silu(const uint16_t* gate_up, int stride, uint8_t* codes, uint8_t* scales, int M, int K, int bits,
+                void* stream);
+
+/* codes, scales = microscaled(x) of M fp16 rows of K, stride x_stride >= K. */
+int wq4_mx_quantize(const uint16_t* x, int x_stride, uint8_t* codes, uint8_t* scales, int M, int K, int bits,
+                    void* stream);
+
+/*
+ * The way back: y = fp16(value(r, k)), M rows of K, stride y_stride >= K,
+ * rounded to nearest even (beyond fp16's range: an infinity; scale or code
+ * NaN: NaN).
+ */
+int wq4_mx_dequantize(const uint8_t* codes, const uint8_t* scales, uint16_t* y, int y_stride, int M, int K, int bits,
+                      void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Per-token decode chain                                                     */

@@ -143,6 +143,66 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* map)
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
 
+// ------------------------------------------------- block-scaled products --
+
+// Instruction descriptors of the block-scaled kinds with e8m0 scales (scale
+// type at bit 23) and an fp32 accumulator: A's and B's types at bits [7, 10)
+// and [10, 13), N / 8 at [17, 23), M / 16 at [24, 29).  A group's scale is a
+// byte of a 32-bit word of tensor memory: which one (for kind::mxf4, of two
+// scales a step, which the first) is said for B at bits [4, 6) and for A at
+// [29, 31).
+// mxf8f6f4, K = 32: A e2m1 (5), spread in shared memory to 16 bytes for 16 codes; B e4m3 (0).
+__host__ __device__ constexpr uint32_t idesc_mx_e2m1_e4m3(int M, int N)
+{
+    return (5u << 7) | (0u << 10) | (static_cast<uint32_t>(N >> 3) << 17) | (1u << 23) | (static_cast<uint32_t>(M >> 4) << 24);
+}
+// mxf4, K = 64: A and B e2m1 (1), packed.
+__host__ __device__ constexpr uint32_t idesc_mx_e2m1_e2m1(int M, int N)
+{
+    return (1u << 7) | (1u << 10) | (static_cast<uint32_t>(N >> 3) << 17) | (1u << 23) | (static_cast<uint32_t>(M >> 4) << 24);
+}
+__host__ __device__ constexpr uint32_t idesc_mx_scale_byte(int byte)
+{
+    return (static_cast<uint32_t>(byte) << 4) | (static_cast<uint32_t>(byte) << 29);
+}
+
+// D (+)= (A scaled by sfa) * (B scaled by sfb), A and B in shared memory (K-major,
+// 128-byte swizzle), the scales in tensor memory; issued by one thread.
+__device__ __forceinline__ void mma_mxf8f6f4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                             uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+        : "memory");
+}
+
+__device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                         uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+        : "memory");
+}
+
+// Shared-memory descriptor of 32 rows of 16 bytes, one after another (8-row
+// groups 128 bytes apart, no swizzle): a block of scales.
+__device__ __forceinline__ uint64_t scales_desc(uint32_t saddr)
+{
+    return static_cast<uint64_t>((saddr >> 4) & 0x3FFFu) | (static_cast<uint64_t>(128 >> 4) << 32) | (1ull << 46);
+}
+
+// A block of scales, shared memory -> four columns of tensor memory (32 lanes,
+// repeated in each of the four quarters): column c, lane l is word c of row l.
+// Executed in order with the MMAs that this thread issues after it.
+__device__ __forceinline__ void cp_scales(uint32_t taddr, uint64_t desc)
+{
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
 __device__ __forceinline__ uint32_t hmul2_u32(uint32_t a, uint32_t b)
 {
     uint32_t d;

@@ -90,6 +90,13 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     L = ctypes.CDLL(_build.LIB)
     L.wq4_gemv.argtypes = [_P, _P, _P, _P, _I, _I, _I, _P]
     L.wq4_gemm.argtypes = [_P, _P, _P, _P, _I, _I, _I, _P]
+    L.wq4_mx_scale_bytes.argtypes = [_I, _I]
+    L.wq4_mx_scale_bytes.restype = _SZ
+    L.wq4_mx_gemm.argtypes = [_P, _P, _P, _P, _P, _I, _I, _I, _I, _P]
+    L.wq4_mx_norm.argtypes = [_P, _I, _P, _I, _P, ctypes.c_float, _P, _I, _P, _P, _I, _I, _I, _P]
+    L.wq4_mx_silu.argtypes = [_P, _I, _P, _P, _I, _I, _I, _P]
+    L.wq4_mx_quantize.argtypes = [_P, _I, _P, _P, _I, _I, _I, _P]
+    L.wq4_mx_dequantize.argtypes = [_P, _P, _P, _I, _I, _I, _I, _P]
     L.wq4_unpack_debug.argtypes = [_P, _P, _P, _P, _I, _I, _P]
     L.wq4_pack_host.argtypes = [_P, _P, _I, _I]
     L.wq4_status_string.argtypes = [_I]
@@ -146,6 +153,7 @@ EXPORTED = ["wq4_gemv", "wq4_gemm", "wq4_unpack_debug", "wq4_pack_host", "wq4_st
             "wq4_chain_trace_offsets",
             "wq4_test_chain_waits", "wq4_test_gemv_path", "wq4_test_copy_stall",
             "wq4_decode_step_workspace_bytes", "wq4_decode_step", "wq4_decode_step_host",
+            "wq4_mx_scale_bytes", "wq4_mx_gemm", "wq4_mx_norm", "wq4_mx_silu", "wq4_mx_quantize", "wq4_mx_dequantize",
             "wq4_synth_codes", "wq4_synth_scales", "wq4_synth_sum4",
             "wq4_paged_attention_workspace_bytes", "wq4_paged_attention", "wq4_window_attention", "wq4_kv_append",
             "wq4_prompt_append", "wq4_prompt_attention_workspace_bytes", "wq4_prompt_attention",
@@ -194,6 +202,37 @@ def wq4_gemv(W, scales, x, y, N: int, K: int, batch: int, stream=None, check: bo
 def wq4_gemm(W, scales, x, y, N: int, K: int, M: int, stream=None, check: bool = True) -> int:
     rc = load().wq4_gemm(_ptr(W), _ptr(scales), _ptr(x), _ptr(y), N, K, M, _stream(stream))
     return _check("wq4_gemm", rc) if check else rc
+
+
+def wq4_mx_scale_bytes(rows: int, K: int) -> int:
+    return load().wq4_mx_scale_bytes(rows, K)
+
+
+def wq4_mx_gemm(W, W_scales, x, x_scales, y, N: int, K: int, M: int, bits: int, stream=None, check: bool = True) -> int:
+    rc = load().wq4_mx_gemm(_ptr(W), _ptr(W_scales), _ptr(x), _ptr(x_scales), _ptr(y), N, K, M, bits, _stream(stream))
+    return _check("wq4_mx_gemm", rc) if check else rc
+
+
+def wq4_mx_norm(x, x_stride: int, residual, residual_stride: int, gain, eps: float, sum, sum_stride: int, codes, scales,
+                M: int, K: int, bits: int, stream=None, check: bool = True) -> int:
+    rc = load().wq4_mx_norm(_ptr(x), x_stride, _ptr(residual), residual_stride, _ptr(gain), eps, _ptr(sum), sum_stride,
+                            _ptr(codes), _ptr(scales), M, K, bits, _stream(stream))
+    return _check("wq4_mx_norm", rc) if check else rc
+
+
+def wq4_mx_silu(gate_up, stride: int, codes, scales, M: int, K: int, bits: int, stream=None, check: bool = True) -> int:
+    rc = load().wq4_mx_silu(_ptr(gate_up), stride, _ptr(codes), _ptr(scales), M, K, bits, _stream(stream))
+    return _check("wq4_mx_silu", rc) if check else rc
+
+
+def wq4_mx_quantize(x, x_stride: int, codes, scales, M: int, K: int, bits: int, stream=None, check: bool = True) -> int:
+    rc = load().wq4_mx_quantize(_ptr(x), x_stride, _ptr(codes), _ptr(scales), M, K, bits, _stream(stream))
+    return _check("wq4_mx_quantize", rc) if check else rc
+
+
+def wq4_mx_dequantize(codes, scales, y, y_stride: int, M: int, K: int, bits: int, stream=None, check: bool = True) -> int:
+    rc = load().wq4_mx_dequantize(_ptr(codes), _ptr(scales), _ptr(y), y_stride, M, K, bits, _stream(stream))
+    return _check("wq4_mx_dequantize", rc) if check else rc
 
 
 def wq4_unpack_debug(W, scales, w_out, q_out, N: int, K: int, stream=None, check: bool = True) -> int:
