@@ -149,6 +149,14 @@ def operand(rng, rows, K, bits, scale):
     return mx.quantize(v, bits)
 
 
+def any_operand(rng, rows, K, bits):
+    """Codes of every finite value and scales of a few binades."""
+    c = rng.integers(0, 256, (rows, K * bits // 8), dtype=np.uint8)
+    if bits == 8:
+        c[(c & 127) == 127] = 0x3A
+    return c, rng.integers(124, 130, (rows, K // 32), dtype=np.uint8)
+
+
 def gemm(W, ws, x, xs, M, N, K, bits, fill=0xFF):
     y = torch.full((M + 1, N), -1, dtype=torch.int16, device="cuda")
     wq4.wq4_mx_gemm(dev(W), dev(mx.tiled(ws, K, fill)), dev(x), dev(mx.tiled(xs, K, fill)), y, N, K, M, bits)
@@ -178,3 +186,20 @@ def test_gemm(M, N, K, bits):
     W, ws = operand(rng, N, K, 4, 1.0)
     x, xs = operand(rng, M, K, bits, K ** -0.5)
     check_product(gemm(W, ws, x, xs, M, N, K, bits), W, ws, x, xs, bits)
+
+
+# pairs of blocks: tiles of 256 rows by 256 tokens, one and several a pair, ragged in each direction, rows that a
+# tensor copy can write and rows that it cannot
+PAIRS = [(129, 19464, 128), (200, 20003, 384), (513, 6600, 1280), (256, 40000, 256), (1000, 9728, 640), (700, 25001, 128), (2000, 5128, 2176)]
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("M,N,K", PAIRS)
+def test_gemm_pairs(M, N, K, bits):
+    rng = np.random.default_rng(M * N + K)
+    W, ws = any_operand(rng, N, K, 4)
+    x, xs = any_operand(rng, M, K, bits)
+    xs -= 6 if bits == 8 else 0
+    y = gemm(W, ws, x, xs, M, N, K, bits)
+    check_product(y, W, ws, x, xs, bits)
+    assert np.array_equal(gemm(W, ws, x, xs, M, N, K, bits, 0x00), y)
