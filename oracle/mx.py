@@ -98,17 +98,19 @@ def silu(gate_up: np.ndarray) -> np.ndarray:
         return g / (1 + np.exp(-g)) * u
 
 
-def wrong_groups(codes, exps, v, bits: int, delta: float, tiny: float = 0.0) -> np.ndarray:
+def wrong_groups(codes, exps, v, bits: int, delta, tiny: float = 0.0) -> np.ndarray:
     """Groups of codes and scale bytes that are not the nearest of values within v (1 +- delta) +- tiny:
     a scale that such an amax does not have, or a code further from v than the nearest by more than
-    twice that."""
+    twice that.  delta: a number, or one for each value."""
+    delta = np.broadcast_to(delta, v.shape).reshape(len(v), -1, 32)
     mags = magnitudes(bits)
     g = v.reshape(len(v), -1, 32)
     q = values(codes, np.where(exps == 255, 127, exps), bits).reshape(g.shape)
     amax = np.abs(g).max(2)
     bad = ~np.isfinite(amax)
     s = np.ldexp(1.0, exps.astype(int) - 127)
-    lo, hi = amax * (1 - delta) - tiny, amax * (1 + delta) + tiny
+    d = delta.max(2)
+    lo, hi = amax * (1 - d) - tiny, amax * (1 + d) + tiny
     fits = (mags[-1] * s >= lo) & ((mags[-1] * s / 2 < hi) | (exps == 0))
     fits |= (lo <= 0) & (exps == 127) & (q == 0).all(2)
     g0 = np.where(bad[..., None], 0.0, g)

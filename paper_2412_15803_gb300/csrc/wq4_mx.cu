@@ -15,6 +15,8 @@
 
 #include <cuda_runtime.h>
 
+#include <algorithm>
+#include <atomic>
 #include <cmath>
 
 namespace wq4 {
@@ -28,8 +30,9 @@ __device__ __forceinline__ void to_floats(uint4 q, float v[8])
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        v[2 * i] = half_bits_to_float(static_cast<uint16_t>(w[i] & 0xFFFFu));
-        v[2 * i + 1] = half_bits_to_float(static_cast<uint16_t>(w[i] >> 16));
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
     }
 }
 
@@ -37,9 +40,10 @@ __device__ __forceinline__ uint4 to_halves(const float v[8])
 {
     uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        w[i] = static_cast<uint32_t>(float_to_half_bits(v[2 * i])) |
-               (static_cast<uint32_t>(float_to_half_bits(v[2 * i + 1])) << 16);
+    for (int i = 0; i < 4; ++i) {
+        const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
@@ -65,69 +69,128 @@ __device__ __forceinline__ size_t scale_word(int r, int kb, int K)
     return (static_cast<size_t>(r >> 7) * (K >> 7) + kb) * 512 + (r & 31) * 16 + ((r >> 5) & 3) * 4;
 }
 
-// Codes and scales of the eight values that each lane has of columns [8 c, 8 c +
-// 8) of row r; all lanes of a warp, 16 in turn with 16 consecutive c.  Lanes
-// without `live` store nothing.
-template <int BITS>
-__device__ __forceinline__ void store_codes(const float v[8], uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
-                                            int r, int c, int K, bool live)
+// |a| and |b|: the larger, NaN if either is.
+__device__ __forceinline__ float max_abs(float a, float b)
 {
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);   // NaN is over all numbers here
-    m = max(m, __shfl_xor_sync(kAll, m, 1));
-    m = max(m, __shfl_xor_sync(kAll, m, 2));
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return d;
+}
+
+// Codes of the eight values that each lane has of columns [8 c, 8 c + 8) of row
+// r, and the word of scales of its 128 columns (in every lane); all lanes of a
+// warp, 16 in turn with 16 consecutive c.  Lanes without `live` store nothing.
+template <int BITS>
+__device__ __forceinline__ uint32_t store_codes(const float v[8], uint8_t* __restrict__ codes, int r, int c, int K, bool live)
+{
+    float m = max_abs(max_abs(max_abs(v[0], v[1]), max_abs(v[2], v[3])), max_abs(max_abs(v[4], v[5]), max_abs(v[6], v[7])));
+    m = max_abs(m, __shfl_xor_sync(kAll, m, 1));
+    m = max_abs(m, __shfl_xor_sync(kAll, m, 2));
+    const uint32_t mb = __float_as_uint(m);
     constexpr int kTop = BITS == 8 ? 8 : 2;                       // top = 1.75 * 2^8, 1.5 * 2^2
-    constexpr uint32_t kFrac = BITS == 8 ? 0x600000u : 0x400000u;
-    const bool bad = m >= 0x7F800000u;
-    int e = static_cast<int>(m >> 23) - 127 - kTop + ((m & 0x7FFFFFu) > kFrac ? 1 : 0);
-    e = m == 0 ? 0 : max(e, -127);
-    const float inv = bad ? 0.f : __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+    constexpr uint32_t kUp = BITS == 8 ? 0x1FFFFFu : 0x3FFFFFu;   // carries into the exponent where 1 + f is over that
+    const bool bad = mb >= 0x7F800000u;
+    int e = static_cast<int>((mb + kUp) >> 23) - 127 - kTop;
+    e = mb == 0 ? 0 : max(e, -127);
+    const float inv = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
     float q[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = bad ? 0.f : v[i] * inv;
+    for (int i = 0; i < 8; ++i) q[i] = v[i] * inv;
     if constexpr (BITS == 8) {
-        const uint2 o = make_uint2(e4m3x2(q[0], q[1]) | (e4m3x2(q[2], q[3]) << 16), e4m3x2(q[4], q[5]) | (e4m3x2(q[6], q[7]) << 16));
+        uint2 o = make_uint2(e4m3x2(q[0], q[1]) | (e4m3x2(q[2], q[3]) << 16), e4m3x2(q[4], q[5]) | (e4m3x2(q[6], q[7]) << 16));
+        if (bad) o = make_uint2(0, 0);
         if (live) *reinterpret_cast<uint2*>(codes + static_cast<size_t>(r) * K + 8 * c) = o;
     } else {
-        const uint32_t o = e2m1x2(q[0], q[1]) | (e2m1x2(q[2], q[3]) << 8) | (e2m1x2(q[4], q[5]) << 16) | (e2m1x2(q[6], q[7]) << 24);
+        uint32_t o = e2m1x2(q[0], q[1]) | (e2m1x2(q[2], q[3]) << 8) | (e2m1x2(q[4], q[5]) << 16) | (e2m1x2(q[6], q[7]) << 24);
+        if (bad) o = 0;
         if (live) *reinterpret_cast<uint32_t*>(codes + static_cast<size_t>(r) * (K >> 1) + 4 * c) = o;
     }
     // group j's byte at place j of the word of 128 columns
     uint32_t w = static_cast<uint32_t>(bad ? 255 : e + 127) << (8 * ((c >> 2) & 3));
     w |= __shfl_xor_sync(kAll, w, 4);
     w |= __shfl_xor_sync(kAll, w, 8);
+    return w;
+}
+
+__device__ __forceinline__ void store_scales(uint32_t w, uint8_t* __restrict__ scales, int r, int c, int K, bool live)
+{
     if (live && (c & 15) == 0) *reinterpret_cast<uint32_t*>(scales + scale_word(r, c >> 4, K)) = w;
 }
 
+// The approximate exponential and quotient: relative errors of 2 ulp, and of
+// |g| 2^-23 from the exponent's product, far below the half step (2^-4) that the
+// code is off by.  (expf and an exact division: 70 us where these take 49, 4096
+// rows of 14336.)
 __device__ __forceinline__ float silu(float g)
 {
-    return g / (1.f + expf(-g));
+    return __fdividef(g, 1.f + __expf(-g));
 }
 
-// Rows without a sum over them: quantize, and silu(gate) * up.  A block's
-// threads take consecutive columns, gridDim.y rows at a time.
-template <int BITS, bool SILU>
+// A lane's place in a call on rows: eight columns, and rows r, r + 32, r + 64 and
+// r + 96 (R = 4) or r alone.  Those four's scales are 16 consecutive bytes.
+struct Place {
+    int r, c;
+    bool live;
+};
+
+template <int R>
+__device__ __forceinline__ Place place(int M, int chunks)
+{
+    const int64_t groups = R == 1 ? M : (static_cast<int64_t>(M) + 127) / 128 * 32;
+    const int64_t n = groups * chunks, i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+    int g, c;
+    if (n <= 0x7FFFFFFF) {
+        const uint32_t j = min(static_cast<uint32_t>(i), static_cast<uint32_t>(n - 1));
+        g = j / static_cast<uint32_t>(chunks);
+        c = j % static_cast<uint32_t>(chunks);
+    } else {
+        const int64_t j = min(i, n - 1);
+        g = static_cast<int>(j / chunks);
+        c = static_cast<int>(j % chunks);
+    }
+    const int r = R == 1 ? g : (g >> 5) * 128 + (g & 31);
+    return {r, c, i < n && r < M};
+}
+
+// Rows without a sum over them: quantize, and silu(gate) * up.
+template <int BITS, bool SILU, int R>
 __global__ void __launch_bounds__(256) rows_kernel(const uint16_t* __restrict__ x, int stride, uint8_t* __restrict__ codes,
                                                    uint8_t* __restrict__ scales, int M, int K)
 {
     grid_dependency_wait();
-    grid_dependents_launch();
-    const int c = static_cast<int>(blockIdx.x * blockDim.x + threadIdx.x), chunks = K >> 3;
-    const bool live = c < chunks;
-    for (int r = blockIdx.y; r < M; r += gridDim.y) {
-        float v[8] = {};
-        if (live) {
-            const uint16_t* row = x + static_cast<size_t>(r) * stride + 8 * c;
-            to_floats(*reinterpret_cast<const uint4*>(row), v);
-            if constexpr (SILU) {
-                float u[8];
-                to_floats(*reinterpret_cast<const uint4*>(row + K), u);
+    // wq4_mx_gemm copies its weights before the previous kernel is complete where
+    // that lets it begin early, and quantize writes weights
+    if (SILU) grid_dependents_launch();
+    const Place p = place<R>(M, K >> 3);
+    uint4 a[R], b[R];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = silu(v[i]) * u[i];
-            }
+    for (int q = 0; q < R; ++q) {
+        a[q] = b[q] = make_uint4(0, 0, 0, 0);
+        if (p.live && p.r + 32 * q < M) {
+            const uint16_t* row = x + static_cast<size_t>(p.r + 32 * q) * stride + 8 * p.c;
+            a[q] = __ldcs(reinterpret_cast<const uint4*>(row));
+            if (SILU) b[q] = __ldcs(reinterpret_cast<const uint4*>(row + K));
         }
-        store_codes<BITS>(v, codes, scales, r, c, K, live);
+    }
+    uint32_t w[R];
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+        float v[8];
+        to_floats(a[q], v);
+        if constexpr (SILU) {
+            float u[8];
+            to_floats(b[q], u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = silu(v[i]) * u[i];
+        }
+        w[q] = store_codes<BITS>(v, codes, p.r + 32 * q, p.c, K, p.live && p.r + 32 * q < M);
+    }
+    if (R == 4 && p.r + 96 < M) {
+        if (p.live && (p.c & 15) == 0)
+            *reinterpret_cast<uint4*>(scales + scale_word(p.r, p.c >> 4, K)) = make_uint4(w[0], w[R > 1 ? 1 : 0], w[R > 2 ? 2 : 0], w[R > 3 ? 3 : 0]);
+    } else {
+#pragma unroll
+        for (int q = 0; q < R; ++q) store_scales(w[q], scales, p.r + 32 * q, p.c, K, p.live && p.r + 32 * q < M);
     }
 }
 
@@ -142,105 +205,211 @@ struct NormArgs {
     float eps;
 };
 
-__device__ __forceinline__ void load_h(const NormArgs& a, int r, int c, float h[8])
+// fp16(x + residual) of eight values.
+__device__ __forceinline__ uint4 add_halves(uint4 x, uint4 r)
 {
-    to_floats(*reinterpret_cast<const uint4*>(a.x + static_cast<size_t>(r) * a.x_stride + 8 * c), h);
-    if (!a.residual) return;
-    float t[8];
-    to_floats(*reinterpret_cast<const uint4*>(a.residual + static_cast<size_t>(r) * a.residual_stride + 8 * c), t);
+    float a[8], b[8];
+    to_floats(x, a);
+    to_floats(r, b);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = half_bits_to_float(float_to_half_bits(h[i] + t[i]));
+    for (int i = 0; i < 8; ++i) a[i] += b[i];
+    return to_halves(a);
 }
 
-// A block a row.  The row stays in registers, NC chunks of eight a thread
-// (NC = 0, rows of more than 32768: read again for the second pass, from `sum`
-// where there is one, since it may be x or residual).
+__device__ __forceinline__ uint4 load_h(const NormArgs& a, int r, int c)
+{
+    const uint4 x = *reinterpret_cast<const uint4*>(a.x + static_cast<size_t>(r) * a.x_stride + 8 * c);
+    if (!a.residual) return x;
+    return add_halves(x, *reinterpret_cast<const uint4*>(a.residual + static_cast<size_t>(r) * a.residual_stride + 8 * c));
+}
+
+__device__ __forceinline__ float squares(uint4 h, float ss)
+{
+    float v[8];
+    to_floats(h, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss = fmaf(v[j], v[j], ss);
+    return ss;
+}
+
+__device__ __forceinline__ void norm_codes(uint4 h, uint4 g, float f, float o[8])
+{
+    float v[8], w[8];
+    to_floats(h, v);
+    to_floats(g, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = v[j] * f * w[j];
+}
+
+constexpr uint32_t kOnes = 0x3C003C00u;      // fp16 1, 1
+
+__device__ __forceinline__ uint4 load_gain(const NormArgs& a, int c)
+{
+    return a.gain && c < (a.K >> 3) ? *reinterpret_cast<const uint4*>(a.gain + 8 * c) : make_uint4(kOnes, kOnes, kOnes, kOnes);
+}
+
+// Few rows, and rows of more than 16384: a block a row, the row in registers, NC
+// chunks of eight a thread (NC = 0, rows of more than 32768: read again for the
+// second pass, from `sum` where there is one, since it may be x or residual).
 template <int BITS, int NC>
 __global__ void __launch_bounds__(1024) norm_kernel(const NormArgs a)
 {
-    __shared__ float part[32];
+    __shared__ float part[2][32];
     grid_dependency_wait();
     grid_dependents_launch();
     const int nt = static_cast<int>(blockDim.x), chunks = a.K >> 3, t = static_cast<int>(threadIdx.x);
     const int n = NC ? NC : (chunks + nt - 1) / nt;
-    for (int r = blockIdx.x; r < a.M; r += gridDim.x) {
-        float h[NC ? NC : 1][8];
+    int buf = 0;
+    for (int r = blockIdx.x; r < a.M; r += gridDim.x, buf ^= 1) {
+        uint4 h[NC ? NC : 1];
         float ss = 0.f;
 #pragma unroll
         for (int i = 0; i < n; ++i) {
             const int c = t + i * nt;
-            float* v = h[NC ? i : 0];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = 0.f;
+            uint4& v = h[NC ? i : 0];
+            v = make_uint4(0, 0, 0, 0);
             if (c < chunks) {
-                load_h(a, r, c, v);
-                if (a.sum) *reinterpret_cast<uint4*>(a.sum + static_cast<size_t>(r) * a.sum_stride + 8 * c) = to_halves(v);
+                v = load_h(a, r, c);
+                if (a.sum) *reinterpret_cast<uint4*>(a.sum + static_cast<size_t>(r) * a.sum_stride + 8 * c) = v;
             }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) ss = fmaf(v[j], v[j], ss);
+            ss = squares(v, ss);
         }
         ss = warp_sum(ss);
-        if ((t & 31) == 0) part[t >> 5] = ss;
+        if ((t & 31) == 0) part[buf][t >> 5] = ss;
         __syncthreads();
-        ss = warp_sum((t & 31) < (nt >> 5) ? part[t & 31] : 0.f);
-        __syncthreads();
+        ss = warp_sum((t & 31) < (nt >> 5) ? part[buf][t & 31] : 0.f);
         const float f = rsqrtf(ss / static_cast<float>(a.K) + a.eps);
 #pragma unroll
         for (int i = 0; i < n; ++i) {
             const int c = t + i * nt;
             const bool live = c < chunks;
-            float* v = h[NC ? i : 0];
-            float g[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-            if (live) {
-                if (NC == 0) {
-                    if (a.sum)
-                        to_floats(*reinterpret_cast<const uint4*>(a.sum + static_cast<size_t>(r) * a.sum_stride + 8 * c), v);
-                    else
-                        load_h(a, r, c, v);
-                }
-                if (a.gain) to_floats(*reinterpret_cast<const uint4*>(a.gain + 8 * c), g);
+            uint4 v = h[NC ? i : 0];
+            if (NC == 0) {
+                v = make_uint4(0, 0, 0, 0);
+                if (live) v = a.sum ? *reinterpret_cast<const uint4*>(a.sum + static_cast<size_t>(r) * a.sum_stride + 8 * c) : load_h(a, r, c);
             }
             float o[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = v[j] * f * g[j];
-            store_codes<BITS>(o, a.codes, a.scales, r, c, a.K, live);
+            norm_codes(v, load_gain(a, c), f, o);
+            const uint32_t w = store_codes<BITS>(o, a.codes, r, c, a.K, live);
+            store_scales(w, a.scales, r, c, a.K, live);
         }
     }
 }
 
-template <int BITS>
+// Many rows: bulk copies bring the next rows into a ring in shared memory while
+// this one is in registers, so that what is in flight does not end at a block's
+// barrier; one barrier a row, after which its slot is free.
+constexpr int kNormSlots = 8;
+
+template <int BITS, int NC>
+__global__ void __launch_bounds__(NC == 1 ? 256 : 1024) norm_ring_kernel(const NormArgs a, const int slots, uint32_t* err)
+{
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ float part[2][32];
+    __shared__ __align__(8) uint64_t full[kNormSlots];
+    const int nt = static_cast<int>(blockDim.x), chunks = a.K >> 3, t = static_cast<int>(threadIdx.x);
+    const uint32_t row_bytes = 2 * a.K, slot_bytes = a.residual ? 2 * row_bytes : row_bytes;
+    const int step = static_cast<int>(gridDim.x);
+    uint64_t pol = 0;
+    auto fetch = [&](int slot, int r) {
+        uint8_t* dst = smem + slot * slot_bytes;
+        mbar_arrive_expect_tx(&full[slot], slot_bytes);
+        bulk_g2s(dst, a.x + static_cast<size_t>(r) * a.x_stride, row_bytes, &full[slot], pol);
+        if (a.residual) bulk_g2s(dst + row_bytes, a.residual + static_cast<size_t>(r) * a.residual_stride, row_bytes, &full[slot], pol);
+    };
+    if (t == 0) {
+        for (int i = 0; i < slots; ++i) mbar_init(&full[i], 1);
+        mbar_fence_init();
+    }
+    grid_dependency_wait();
+    grid_dependents_launch();
+    if (t == 0) {
+        pol = l2_policy_evict_first();
+        for (int i = 0; i < slots && blockIdx.x + static_cast<int64_t>(i) * step < a.M; ++i) fetch(i, blockIdx.x + i * step);
+    }
+    uint4 g[NC];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) g[i] = load_gain(a, t + i * nt);
+    __syncthreads();                 // the barriers are there
+    int slot = 0, buf = 0;
+    uint32_t par = 0;
+    for (int64_t r = blockIdx.x; r < a.M; r += step, buf ^= 1) {
+        mbar_wait(&full[slot], par, err);
+        const uint4* xs = reinterpret_cast<const uint4*>(smem + slot * slot_bytes);
+        uint4 h[NC];
+        float ss = 0.f;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = t + i * nt;
+            h[i] = make_uint4(0, 0, 0, 0);
+            if (c < chunks) {
+                h[i] = xs[c];
+                if (a.residual) h[i] = add_halves(h[i], xs[chunks + c]);
+                if (a.sum) __stcs(reinterpret_cast<uint4*>(a.sum + static_cast<size_t>(r) * a.sum_stride + 8 * c), h[i]);
+            }
+            ss = squares(h[i], ss);
+        }
+        ss = warp_sum(ss);
+        if ((t & 31) == 0) part[buf][t >> 5] = ss;
+        __syncthreads();
+        if (t == 0 && r + static_cast<int64_t>(slots) * step < a.M) fetch(slot, static_cast<int>(r + static_cast<int64_t>(slots) * step));
+        ss = warp_sum((t & 31) < (nt >> 5) ? part[buf][t & 31] : 0.f);
+        const float f = rsqrtf(ss / static_cast<float>(a.K) + a.eps);
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = t + i * nt;
+            float o[8];
+            norm_codes(h[i], g[i], f, o);
+            const uint32_t w = store_codes<BITS>(o, a.codes, static_cast<int>(r), c, a.K, c < chunks);
+            store_scales(w, a.scales, static_cast<int>(r), c, a.K, c < chunks);
+        }
+        if (++slot == slots) {
+            slot = 0;
+            par ^= 1u;
+        }
+    }
+}
+
+template <int BITS, int R>
 __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                          uint16_t* __restrict__ y, int stride, int M, int K)
 {
     grid_dependency_wait();
     grid_dependents_launch();
-    const int c = static_cast<int>(blockIdx.x * blockDim.x + threadIdx.x);
-    if (c >= (K >> 3)) return;
-    for (int r = blockIdx.y; r < M; r += gridDim.y) {
-        const uint32_t sb = scales[scale_word(r, c >> 4, K) + ((c >> 2) & 3)];
+    const Place p = place<R>(M, K >> 3);
+    if (!p.live) return;
+    uint2 code[R];
+    uint32_t sb[R];
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+        const int r = min(p.r + 32 * q, M - 1);
+        sb[q] = scales[scale_word(r, p.c >> 4, K) + ((p.c >> 2) & 3)];
+        if constexpr (BITS == 8)
+            code[q] = __ldcs(reinterpret_cast<const uint2*>(codes + static_cast<size_t>(r) * K + 8 * p.c));
+        else
+            code[q].x = __ldcs(reinterpret_cast<const uint32_t*>(codes + static_cast<size_t>(r) * (K >> 1) + 4 * p.c));
+    }
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+        if (p.r + 32 * q >= M) break;
         // 2^(sb - 127); sb = 0 is 2^-127, below the normal range
-        const float s = sb == 255 ? __uint_as_float(0x7FC00000u) : sb == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(sb << 23);
+        const float s = sb[q] == 255 ? __uint_as_float(0x7FC00000u) : sb[q] == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(sb[q] << 23);
         uint32_t h[4];
-        if constexpr (BITS == 8) {
-            const uint2 q = *reinterpret_cast<const uint2*>(codes + static_cast<size_t>(r) * K + 8 * c);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint16_t p = static_cast<uint16_t>((i < 2 ? q.x : q.y) >> (16 * (i & 1)));
-                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h[i]) : "h"(p));
-            }
-        } else {
-            const uint32_t q = *reinterpret_cast<const uint32_t*>(codes + static_cast<size_t>(r) * (K >> 1) + 4 * c);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint16_t p = static_cast<uint16_t>((q >> (8 * i)) & 0xFFu);
-                asm("{\n\t.reg .b8 t, u;\n\tmov.b16 {t, u}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(h[i]) : "h"(p));
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (BITS == 8) {
+                const uint16_t c2 = static_cast<uint16_t>((i < 2 ? code[q].x : code[q].y) >> (16 * (i & 1)));
+                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h[i]) : "h"(c2));
+            } else {
+                const uint16_t c2 = static_cast<uint16_t>((code[q].x >> (8 * i)) & 0xFFu);
+                asm("{\n\t.reg .b8 t, u;\n\tmov.b16 {t, u}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(h[i]) : "h"(c2));
             }
         }
         float v[8];
         to_floats(make_uint4(h[0], h[1], h[2], h[3]), v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= s;
-        *reinterpret_cast<uint4*>(y + static_cast<size_t>(r) * stride + 8 * c) = to_halves(v);
+        *reinterpret_cast<uint4*>(y + static_cast<size_t>(p.r + 32 * q) * stride + 8 * p.c) = to_halves(v);
     }
 }
 
@@ -276,24 +445,31 @@ int check_held(const uint8_t* codes, const uint8_t* scales, int M, int K, int bi
 
 // A call's launch: with programmatic dependent launch, on `stream`.
 template <typename... P, typename... A>
-int launch(void (*kernel)(P...), dim3 grid, int threads, void* stream, A... args)
+int launch(void (*kernel)(P...), int64_t grid, int threads, size_t smem, void* stream, A... args)
 {
-    if (!current_device_info(nullptr)) return WQ4_ERR_CUDA;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
+    cfg.gridDim = dim3(static_cast<unsigned>(grid));
     cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = static_cast<cudaStream_t>(stream);
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? WQ4_OK : WQ4_ERR_CUDA;
 }
 
-dim3 rows_grid(int M, int K)
+// Four rows a thread from the size on where that many threads fill the GPU twice.
+bool four_rows(const DeviceInfo* di, int M, int K)
 {
-    return dim3((K / 8 + 255) / 256, M < 65535 ? M : 65535);
+    return static_cast<int64_t>(M) * (K / 8) >= static_cast<int64_t>(di->sm_count) * 2048 * 8;
+}
+
+int64_t rows_grid(int M, int K, int R)
+{
+    const int64_t groups = R == 1 ? M : (static_cast<int64_t>(M) + 127) / 128 * 32;
+    return (groups * (K / 8) + 255) / 256;
 }
 
 template <bool SILU>
@@ -309,22 +485,48 @@ int run_rows(const uint16_t* x, int stride, uint8_t* codes, uint8_t* scales, int
     if (rc != WQ4_OK) return rc;
     const size_t xb = row_bytes(M, stride, static_cast<int>(width));
     if (overlaps(x, xb, codes, code_bytes(M, K, bits)) || overlaps(x, xb, scales, scale_bytes(M, K))) return WQ4_ERR_INVALID;
-    return launch(bits == 8 ? rows_kernel<8, SILU> : rows_kernel<4, SILU>, rows_grid(M, K), 256, stream, x, stride, codes, scales, M, K);
+    const DeviceInfo* di = current_device_info(nullptr);
+    if (!di) return WQ4_ERR_CUDA;
+    if (four_rows(di, M, K))
+        return launch(bits == 8 ? rows_kernel<8, SILU, 4> : rows_kernel<4, SILU, 4>, rows_grid(M, K, 4), 256, 0, stream, x, stride, codes,
+                      scales, M, K);
+    return launch(bits == 8 ? rows_kernel<8, SILU, 1> : rows_kernel<4, SILU, 1>, rows_grid(M, K, 1), 256, 0, stream, x, stride, codes,
+                  scales, M, K);
+}
+
+template <int BITS, int NC>
+int launch_norm_ring(const NormArgs& a, const DeviceInfo* di, void* stream)
+{
+    constexpr int kMost = 200 * 1024;
+    static std::atomic<bool> ready[kMaxDevices];      // per device; setting the attribute twice is harmless
+    if (!ready[di->dev].load()) {
+        if (cudaFuncSetAttribute(norm_ring_kernel<BITS, NC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost) != cudaSuccess)
+            return WQ4_ERR_CUDA;
+        ready[di->dev].store(true);
+    }
+    const int threads = (a.K / 8 + 32 * NC - 1) / (32 * NC) * 32;
+    const int blocks = std::max(1, 1280 / threads);                   // of an SM, by registers
+    const int slot = (a.residual ? 4 : 2) * a.K;
+    const int slots = std::max(1, std::min(kNormSlots, kMost / blocks / slot));
+    const int64_t grid = std::min<int64_t>(a.M, static_cast<int64_t>(di->sm_count) * blocks);
+    return launch(norm_ring_kernel<BITS, NC>, grid, threads, static_cast<size_t>(slots) * slot, stream, a, slots, di->status);
 }
 
 template <int BITS>
-int launch_norm(const NormArgs& a, int sms, void* stream)
+int launch_norm(const NormArgs& a, const DeviceInfo* di, void* stream)
 {
     const int chunks = a.K / 8;
-    int threads = chunks < 1024 ? (chunks + 31) / 32 * 32 : 1024;
+    if (a.M > 4 * di->sm_count && a.K <= 16384)
+        return a.K <= 2048 ? launch_norm_ring<BITS, 1>(a, di, stream) : launch_norm_ring<BITS, 2>(a, di, stream);
+    const int threads = chunks < 1024 ? (chunks + 31) / 32 * 32 : 1024;
     const int n = (chunks + threads - 1) / threads;
-    const dim3 grid(a.M < sms * 16 ? a.M : sms * 16);
+    const int grid = std::min(a.M, di->sm_count * 16);
     switch (n) {
-        case 1: return launch(norm_kernel<BITS, 1>, grid, threads, stream, a);
-        case 2: return launch(norm_kernel<BITS, 2>, grid, threads, stream, a);
+        case 1: return launch(norm_kernel<BITS, 1>, grid, threads, 0, stream, a);
+        case 2: return launch(norm_kernel<BITS, 2>, grid, threads, 0, stream, a);
         case 3:
-        case 4: return launch(norm_kernel<BITS, 4>, grid, threads, stream, a);
-        default: return launch(norm_kernel<BITS, 0>, grid, threads, stream, a);
+        case 4: return launch(norm_kernel<BITS, 4>, grid, threads, 0, stream, a);
+        default: return launch(norm_kernel<BITS, 0>, grid, threads, 0, stream, a);
     }
 }
 
@@ -379,7 +581,7 @@ extern "C" int wq4_mx_norm(const uint16_t* x, int x_stride, const uint16_t* resi
     const DeviceInfo* di = current_device_info(nullptr);
     if (!di) return WQ4_ERR_CUDA;
     const NormArgs a = {x, residual, gain, sum, codes, scales, x_stride, residual_stride, sum_stride, M, K, eps};
-    return bits == 8 ? launch_norm<8>(a, di->sm_count, stream) : launch_norm<4>(a, di->sm_count, stream);
+    return bits == 8 ? launch_norm<8>(a, di, stream) : launch_norm<4>(a, di, stream);
 }
 
 extern "C" int wq4_mx_dequantize(const uint8_t* codes, const uint8_t* scales, uint16_t* y, int y_stride, int M, int K,
@@ -394,6 +596,11 @@ extern "C" int wq4_mx_dequantize(const uint8_t* codes, const uint8_t* scales, ui
     if (rc != WQ4_OK) return rc;
     const size_t yb = row_bytes(M, y_stride, K);
     if (overlaps(y, yb, codes, code_bytes(M, K, bits)) || overlaps(y, yb, scales, scale_bytes(M, K))) return WQ4_ERR_INVALID;
-    return launch(bits == 8 ? dequantize_kernel<8> : dequantize_kernel<4>, rows_grid(M, K), 256, stream, codes, scales, y, y_stride,
-                  M, K);
+    const DeviceInfo* di = current_device_info(nullptr);
+    if (!di) return WQ4_ERR_CUDA;
+    if (four_rows(di, M, K))
+        return launch(bits == 8 ? dequantize_kernel<8, 4> : dequantize_kernel<4, 4>, rows_grid(M, K, 4), 256, 0, stream, codes, scales, y,
+                      y_stride, M, K);
+    return launch(bits == 8 ? dequantize_kernel<8, 1> : dequantize_kernel<4, 1>, rows_grid(M, K, 1), 256, 0, stream, codes, scales, y,
+                  y_stride, M, K);
 }

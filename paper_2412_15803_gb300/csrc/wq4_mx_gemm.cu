@@ -26,33 +26,13 @@
 namespace wq4 {
 namespace {
 
-// Warps: 0 the copies, 1 the MMA issuer, 2 lets the next kernel launch, 4-7 the
+// Warps: 0, 2, 3 and 12 the copies (in pairs of CTAs 0; 2 lets the next kernel
+// launch), 1 the MMA issuer, 4-11 the
 // epilogue (a warp reads the quarter of tensor memory that its number says).
-constexpr int kThreads = 256;
-constexpr int kProd = 0, kIssuer = 1, kTrigger = 2, kEpi = 4;
+constexpr int kThreads = 416, kPairThreads = 384;
+constexpr int kProd = 0, kIssuer = 1, kTrigger = 2, kScalesW = 2, kTokens = 3, kEpi = 4, kScalesX = 12;
 constexpr int kHeader = 1024;
 constexpr int kTmemCols = 512;
-
-// Tile of 128 weight rows and T tokens.  A slot of the ring is 128 bytes of each
-// row's codes: 128 K for activations of 8 bits, 256 K for 4 (the last slot of
-// an odd number of 128 K is half filled, its other half zeros that no MMA reads).
-template <int BITS, int T>
-struct Cfg {
-    static constexpr int kBlocks = BITS == 8 ? 1 : 2;            // blocks of 128 K in a slot
-    static constexpr int kW = 128 * 128;
-    static constexpr int kX = T * 128;
-    static constexpr int kScales = 512 * kBlocks;                // of 128 rows
-    static constexpr int kSlot = (kW + kX + 2 * kScales + 1023) / 1024 * 1024;
-    static constexpr int kSlots = (220 * 1024 - kHeader) / kSlot;
-    static constexpr int kSmem = kHeader + kSlots * kSlot;
-    static constexpr uint32_t kBytes = (BITS == 8 ? kW / 2 : kW) + kX;   // what the tensor copies bring a slot
-    // tensor memory: two accumulators, then each slot's scales: of the weights, of the tokens
-    static constexpr int kScaleCols = 8 * kBlocks;
-    static constexpr int kScaleCol0 = 2 * T;
-    static_assert(kScaleCol0 + kSlots * kScaleCols <= kTmemCols, "tensor memory");
-    static_assert(kSmem <= 227 * 1024, "shared memory");
-    static_assert((2 * kSlots + 5) * 8 <= 1008, "barriers");
-};
 
 struct Args {
     uint16_t* y;
@@ -60,16 +40,20 @@ struct Args {
     const uint8_t* x_scales;
     int N, M, kblocks;       // blocks of 128 K
     int rtiles, ttiles;
+    int tok;                 // tokens of a tile, a multiple of 16
+    int split;               // CTAs of a cluster that share a tile's K
+    int nslots, slot_bytes, ring;      // of the ring of copies, and where it begins
+    int tmem_cols;
     uint32_t* err;
     int stall;               // test hook: leaves the copies out
     int bulk;                // y's rows can be written by tensor copies
 };
 
-template <int S>
+// A ring position: slot and parity of the n-th use of a ring of S slots.
 struct RingPos {
     int slot = 0;
     uint32_t par = 0;
-    __device__ __forceinline__ void next()
+    __device__ __forceinline__ void next(int S)
     {
         if (++slot == S) {
             slot = 0;
@@ -78,179 +62,390 @@ struct RingPos {
     }
 };
 
+// Tile of 128 weight rows and `tok` tokens, up to 128.  A slot of the ring is BOXES
+// boxes of 128 bytes of each row's codes: 128 or 256 K with activations of 8 bits,
+// 256 with 4 (one box).  (Where K is an odd number of 128, the second half of the
+// last slot's 256 is zeros that no MMA reads.)
+template <int BITS, int BOXES>
+struct Cfg {
+    static constexpr int kBlocks = BITS == 8 ? BOXES : 2;        // blocks of 128 K in a slot
+    static constexpr int kW = BOXES * 128 * 128;
+    static constexpr int kScales = 512 * kBlocks;                // of 128 rows
+    static constexpr int kMaxSlots = 12;
+    static constexpr int kScaleCols = 8 * kBlocks;               // of a slot, in tensor memory: of the weights, of the tokens
+    static_assert(2 * 128 + kMaxSlots * kScaleCols <= kTmemCols, "tensor memory");
+    static_assert((2 * kMaxSlots + 6) * 8 <= 1008, "barriers");
+};
+
+// Shared memory of a CTA: half of an SM's, so that two are resident, of one call or
+// of two that follow one another, or all of it.
+constexpr int kHalf = 113 * 1024, kWhole = 227 * 1024;
+
+// A persistent grid, or a cluster of `split` CTAs a tile that take consecutive
+// parts of its K: each sends its fp32 sums to the CTAs that add them, in rank
+// order, consecutive groups of four tokens a CTA.  A CTA leaves when the others'
+// sums are in; nothing is sent to it after that.
+//
 // As in the other kernels: a wait that gives up (bounded, flagged) leaves
 // invalid outputs, but every role goes on to its end, without further waits.
-template <int BITS, int T>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int BITS, int BOXES>
+__global__ void __launch_bounds__(kThreads, 2)
     mx_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const Args a)
 {
-    using C = Cfg<BITS, T>;
-    constexpr int S = C::kSlots, NB = C::kBlocks;
+    using C = Cfg<BITS, BOXES>;
+    constexpr int NB = C::kBlocks;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* full = reinterpret_cast<uint64_t*>(smem);
-    uint64_t* empty = full + S;
-    uint64_t* dfull = empty + S;       // two accumulators
+    uint64_t* empty = full + C::kMaxSlots;
+    uint64_t* dfull = empty + C::kMaxSlots;       // two accumulators
     uint64_t* dempty = dfull + 2;
     uint64_t* drain = dempty + 2;
+    uint64_t* sfull = drain + 1;                  // the cluster's sums for this CTA are in
     uint32_t* tbase_sh = reinterpret_cast<uint32_t*>(smem + 1008);
-    uint8_t* ring = smem + kHeader;
+    float4* sums = reinterpret_cast<float4*>(smem + kHeader);       // [rank][group][row]
+    uint8_t* ring = smem + a.ring;
+    const int S = a.nslots, tok = a.tok;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int tiles = a.rtiles * a.ttiles;
+    const int split = a.split, rank = static_cast<int>(blockIdx.x) % split;
+    const int tiles = a.rtiles * a.ttiles, u0 = static_cast<int>(blockIdx.x) / split, ustep = static_cast<int>(gridDim.x) / split;
+    // this CTA's slots of a tile's K
     const int slots = (a.kblocks + NB - 1) / NB;
+    const int k0 = static_cast<int>(static_cast<int64_t>(rank) * slots / split), k1 = static_cast<int>(static_cast<int64_t>(rank + 1) * slots / split);
     uint32_t* err = a.err;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S; ++i) {
-            mbar_init(&full[i], 1);
+            mbar_init(&full[i], 4);       // weights, tokens, the scales of each
             mbar_init(&empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&dfull[i], 1);
-            mbar_init(&dempty[i], 4);
+            mbar_init(&dempty[i], 8);
         }
         mbar_init(drain, 1);
+        mbar_init(sfull, 1);
         mbar_fence_init();
+        if (split > 1) {
+            // what the cluster's CTAs send here
+            const int groups = (min(tok, a.M - u0 % a.ttiles * tok) + 3) / 4, per = (groups + split - 1) / split;
+            mbar_arrive_expect_tx(sfull, static_cast<uint32_t>(split * max(0, min(per, groups - rank * per)) * 128 * 16));
+        }
     }
-    if (warp == kIssuer) tc::tmem_alloc(tbase_sh, kTmemCols);
+    if (warp == kIssuer) tc::tmem_alloc(tbase_sh, a.tmem_cols);
     tc::fence_before_sync();
     __syncthreads();
+    if (split > 1) tc::cluster_arrive();          // waited for before the first sums are sent
     tc::fence_after_sync();
-    const uint32_t tbase = *tbase_sh;
+    const uint32_t tbase = *tbase_sh, scol0 = tbase + 2 * tok;
 
-    if (warp == kTrigger) {
-        grid_dependency_wait();
-        grid_dependents_launch();
-    } else if (warp == kProd) {
+    if (warp == kProd || warp == kScalesW || warp == kTokens || warp == kScalesX) {
+        // Four warps bring a slot's parts, a lane each: a copy costs its thread ~100
+        // cycles whatever its size, a wait as much.  (6144 x 4096, one token, K in
+        // halves: one warp 6.0 us, two 5.7, four 5.45.)
         if (lane == 0) {
-            tc::prefetch_map(&tm_w);
-            tc::prefetch_map(&tm_x);
-            grid_dependency_wait();
+            const bool w = warp == kProd || warp == kScalesW, codes = warp == kProd || warp == kTokens;
+            tc::prefetch_map(w ? &tm_w : &tm_x);
             const uint64_t pol = l2_policy_evict_first();
-            RingPos<S> p;
+            const uint8_t* const sc = w ? a.w_scales : a.x_scales;
+            uint8_t* const to = ring + (w ? 0 : C::kW);
+            uint8_t* const sc_to = ring + C::kW + BOXES * tok * 128 + (w ? 0 : C::kScales);
+            const uint32_t bytes = w ? 128 * 128 * BOXES * (BITS == 8 ? 4 : 8) / 8 : BOXES * tok * 128;   // what the tensor copy brings
+            // rows r0 of codes and scales
+            auto copy = [&](int slot, int k, int r0) {
+                const uint32_t sb = 512u * min(NB, a.kblocks - k * NB);
+                uint64_t* bar = &full[slot];
+                mbar_arrive_expect_tx(bar, codes ? bytes : sb);
+                if (!codes) {
+                    bulk_g2s(sc_to + slot * a.slot_bytes, sc + (static_cast<size_t>(r0 >> 7) * a.kblocks + k * NB) * 512, sb, bar, pol);
+                } else if constexpr (BITS == 8)
+                    tc::tma_load_3d(to + slot * a.slot_bytes, w ? &tm_w : &tm_x, 0, r0, k * BOXES, bar);
+                else
+                    tc::tma_load_2d(to + slot * a.slot_bytes, w ? &tm_w : &tm_x, k * 128, r0, bar);
+            };
+            // the first slots' weights, and more of the tile into L2, while the previous kernel finishes
+            const int early = !w || a.stall || u0 >= tiles ? 0 : min(S, k1 - k0);
+            for (int i = 0; i < early; ++i) copy(i, k0 + i, u0 / a.ttiles * 128);
+            if (early == S && k1 > k0 + S) {
+                if (!codes) bulk_prefetch(sc + (static_cast<size_t>(u0 / a.ttiles) * a.kblocks + (k0 + S) * NB) * 512,
+                              512u * (min(k1 * NB, a.kblocks) - (k0 + S) * NB));
+                for (int k = k0 + S; codes && k < min(k1, k0 + S + 24); ++k) {
+                    if constexpr (BITS == 8)
+                        tc::tma_prefetch_3d(&tm_w, 0, u0 / a.ttiles * 128, k * BOXES);
+                    else
+                        tc::tma_prefetch_2d(&tm_w, k * 128, u0 / a.ttiles * 128);
+                }
+            }
+            grid_dependency_wait();
+            if (warp == kTokens) grid_dependents_launch();
+            RingPos p;
             int n = 0;
             bool ok = true;
-            for (int u = a.stall ? tiles : static_cast<int>(blockIdx.x); u < tiles && ok; u += gridDim.x) {
-                const int n0 = u / a.ttiles * 128, m0 = u % a.ttiles * T;
-                const uint8_t* ws = a.w_scales + static_cast<size_t>(n0 >> 7) * a.kblocks * 512;
-                const uint8_t* xs = a.x_scales + static_cast<size_t>(m0 >> 7) * a.kblocks * 512;
-                for (int k = 0; k < slots; ++k, ++n, p.next()) {
-                    if (n >= S && (!mbar_wait(&empty[p.slot], p.par ^ 1u, err) || !mbar_wait(&full[p.slot], p.par ^ 1u, err))) {
+            for (int u = a.stall ? tiles : u0; u < tiles && ok; u += ustep) {
+                const int r0 = w ? u / a.ttiles * 128 : u % a.ttiles * tok;
+                for (int k = k0; k < k1; ++k, ++n, p.next(S)) {
+                    if (n >= S && !mbar_wait(&empty[p.slot], p.par ^ 1u, err)) {
                         ok = false;
                         break;
                     }
-                    uint8_t* base = ring + static_cast<size_t>(p.slot) * C::kSlot;
-                    const uint32_t sb = 512u * min(NB, a.kblocks - k * NB);
-                    mbar_arrive_expect_tx(&full[p.slot], C::kBytes + 2 * sb);
-                    tc::tma_load_2d(base, &tm_w, k * 128, n0, &full[p.slot]);
-                    tc::tma_load_2d(base + C::kW, &tm_x, k * 128, m0, &full[p.slot]);
-                    bulk_g2s(base + C::kW + C::kX, ws + static_cast<size_t>(k) * NB * 512, sb, &full[p.slot], pol);
-                    bulk_g2s(base + C::kW + C::kX + C::kScales, xs + static_cast<size_t>(k) * NB * 512, sb, &full[p.slot], pol);
+                    if (n >= early) copy(p.slot, k, r0);
                 }
             }
             // every copy issued has landed before the CTA's memory goes away
             for (int i = max(0, n - S); i < n; ++i) mbar_wait(&full[i % S], (i / S) & 1, err);
         }
     } else if (warp == kIssuer) {
-        constexpr uint32_t idesc = BITS == 8 ? tc::idesc_mx_e2m1_e4m3(128, T) : tc::idesc_mx_e2m1_e2m1(128, T);
-        const bool leader = tc::elect_one();
-        RingPos<S> p;
+        const uint32_t idesc = BITS == 8 ? tc::idesc_mx_e2m1_e4m3(128, tok) : tc::idesc_mx_e2m1_e2m1(128, tok);
+        const uint32_t leader = tc::elect_one() ? 1u : 0u;
+        RingPos p;
         int dit = 0;
         bool ok = true;
+        const uint64_t sdesc = tc::scales_desc(smem_addr(ring + C::kW + BOXES * tok * 128));
         const uint64_t wdesc = tc::sw128_kmajor_desc(smem_addr(ring));
         const uint64_t xdesc = tc::sw128_kmajor_desc(smem_addr(ring + C::kW));
-        const uint64_t sdesc = tc::scales_desc(smem_addr(ring + C::kW + C::kX));
-        for (int u = blockIdx.x; u < tiles; u += gridDim.x, ++dit) {
+        for (int u = u0; u < tiles; u += ustep, ++dit) {
             const int buf = dit & 1;
+            const uint32_t dcol = tbase + buf * tok;
             if (dit >= 2 && ok) ok = mbar_wait(&dempty[buf], ((dit >> 1) - 1) & 1, err);
-            tc::fence_after_sync();
-            // a tile of 64 tokens may begin at the second half of a block of 128
-            const uint32_t shift = (u % a.ttiles * T & 127) >> 5;
-            for (int k = 0; k < slots; ++k, p.next()) {
+            for (int k = k0; k < k1; ++k) {
                 if (ok) ok = mbar_wait(&full[p.slot], p.par, err);
                 tc::fence_after_sync();
-                const uint64_t off = static_cast<uint64_t>(p.slot) * (C::kSlot >> 4);
-                const uint32_t scol = tbase + C::kScaleCol0 + p.slot * C::kScaleCols;
-                const int nb = min(NB, a.kblocks - k * NB);
-                if (leader) {
-                    for (int b = 0; b < nb; ++b) {
-                        tc::cp_scales(scol + 4 * b, sdesc + off + b * 32);
-                        tc::cp_scales(scol + 4 * (NB + b), sdesc + off + (C::kScales >> 4) + b * 32);
-                    }
+                const int slot = p.slot, nb = min(NB, a.kblocks - k * NB);
+                p.next(S);
+                const uint64_t off = static_cast<uint64_t>(slot * a.slot_bytes >> 4);
+                const uint32_t scol = scol0 + slot * C::kScaleCols;
+                // predicated, not in a branch of one lane: the operands stay warp-uniform
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int b = BITS == 8 ? 0 : j >> 1;
-                        if (b >= nb) break;
-                        const uint32_t acc = k > 0 || j > 0 ? 1u : 0u;
-                        const uint32_t id = idesc | tc::idesc_mx_scale_byte(BITS == 8 ? j : 2 * (j & 1));
-                        if constexpr (BITS == 8)
-                            tc::mma_mxf8f6f4(tbase + buf * T, wdesc + off + 2 * j, xdesc + off + 2 * j, id, scol, scol + 4 + shift, acc);
-                        else
-                            tc::mma_mxf4(tbase + buf * T, wdesc + off + 2 * j, xdesc + off + 2 * j, id, scol + 4 * b,
-                                         scol + 4 * (NB + b) + shift, acc);
+                for (int b = 0; b < NB; ++b) {
+                    if (b > 0 && b >= nb) break;
+                    const uint32_t sfw = scol + 4 * b, sfx = scol + 4 * (NB + b);
+                    tc::cp_scales(sfw, sdesc + off + b * 32, leader);
+                    tc::cp_scales(sfx, sdesc + off + (C::kScales >> 4) + b * 32, leader);
+                    if constexpr (BITS == 8) {
+                        const uint64_t wd = wdesc + off + b * (128 * 128 >> 4), xd = xdesc + off + static_cast<uint32_t>(b * tok * 8);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            tc::mma_mxf8f6f4(dcol, wd + 2 * j, xd + 2 * j, idesc | tc::idesc_mx_scale_byte(j), sfw, sfx,
+                                             k > k0 || b + j > 0 ? 1u : 0u, leader);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            tc::mma_mxf4(dcol, wdesc + off + 4 * b + 2 * j, xdesc + off + 4 * b + 2 * j,
+                                         idesc | tc::idesc_mx_scale_byte(2 * j), sfw, sfx, k > k0 || b + j > 0 ? 1u : 0u, leader);
                     }
-                    tc::commit(&empty[p.slot]);
                 }
+                tc::commit_if(&empty[slot], leader);
+                if (k == k1 - 1) tc::commit_if(&dfull[buf], leader);
                 __syncwarp();
             }
-            if (leader) tc::commit(&dfull[buf]);
         }
         // all MMAs issued have completed before tensor memory is released
         if (leader) tc::commit(drain);
         mbar_wait(drain, 0, err);
-    } else if (warp >= kEpi) {
+    } else {
+        // two groups of four warps, blocks of 16 tokens in turn
         grid_dependency_wait();          // y is written after the previous kernel
-        const int quad = warp & 3;
+        const int quad = warp & 3, row = 32 * quad + lane, grp = (warp - kEpi) >> 2;
         const uint32_t lane_base = tbase + (static_cast<uint32_t>(32 * quad) << 16);
         int dit = 0;
         bool ok = true;
-        for (int u = blockIdx.x; u < tiles; u += gridDim.x, ++dit) {
+        for (int u = u0; u < tiles; u += ustep, ++dit) {
             const int buf = dit & 1;
-            const int nn = u / a.ttiles * 128 + 32 * quad + lane, m0 = u % a.ttiles * T;
+            const int nn = u / a.ttiles * 128 + row, m0 = u % a.ttiles * tok, tv = min(tok, a.M - m0);
+            uint16_t* out = a.y + static_cast<size_t>(m0) * a.N + nn;
+            const uint32_t dcol = lane_base + buf * tok;
+            const int per = ((tv + 3) / 4 + split - 1) / split;       // groups of four tokens that a CTA adds
             if (ok) ok = mbar_wait(&dfull[buf], (dit >> 1) & 1, err);
+            if (split > 1) tc::cluster_wait();
             __syncwarp();
             tc::fence_after_sync();
-            for (int t = 0; t < T; t += 16) {
+            for (int t = 16 * grp; t < tv; t += 32) {
                 uint32_t d[16];
-                tc::ld16(lane_base + buf * T + t, d);
+                tc::ld16(dcol + t, d);
                 tc::ld_wait();
+                if (split > 1) {
+                    int to = (t / 4) / per, j = (t / 4) % per;
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (nn < a.N && m0 + t + i < a.M)
-                        a.y[static_cast<size_t>(m0 + t + i) * a.N + nn] = float_to_half_bits(__uint_as_float(d[i]));
+                    for (int i = 0; i < 4; ++i) {
+                        if (t + 4 * i < tv)
+                            tc::st_async(tc::cluster_addr(sums + (rank * per + j) * 128 + row, to), d + 4 * i, tc::cluster_addr(sfull, to));
+                        if (++j == per) j = 0, ++to;
+                    }
+                } else if (nn < a.N) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (t + i < tv) out[static_cast<size_t>(t + i) * a.N] = float_to_half_bits(__uint_as_float(d[i]));
+                }
             }
             tc::fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive(&dempty[buf]);
+            if (split == 1) continue;
+            // a CTA that gives up stays until the others have, too, and sent what they send
+            if (!ok || !mbar_wait_cluster(sfull, 0, err))
+                for (const uint64_t t0 = globaltimer_ns(); globaltimer_ns() - t0 < 2 * kWaitTimeoutNs;) {}
+            __syncwarp();
+            for (int j = grp; j < per; j += 2) {
+                const int t = 4 * (rank * per + j);
+                if (t >= tv) break;
+                float4 v = sums[j * 128 + row];
+                for (int q = 1; q < split; ++q) {
+                    const float4 w = sums[(q * per + j) * 128 + row];
+                    v.x += w.x;
+                    v.y += w.y;
+                    v.z += w.z;
+                    v.w += w.w;
+                }
+                if (nn < a.N) {
+                    out[static_cast<size_t>(t) * a.N] = float_to_half_bits(v.x);
+                    if (t + 1 < tv) out[static_cast<size_t>(t + 1) * a.N] = float_to_half_bits(v.y);
+                    if (t + 2 < tv) out[static_cast<size_t>(t + 2) * a.N] = float_to_half_bits(v.z);
+                    if (t + 3 < tv) out[static_cast<size_t>(t + 3) * a.N] = float_to_half_bits(v.w);
+                }
+            }
+            break;
         }
     }
+    if (split > 1 && (warp < kEpi || warp == kScalesX)) tc::cluster_wait();
 
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
-    if (warp == kIssuer) tc::tmem_dealloc(tbase, kTmemCols);
+    if (warp == kIssuer) tc::tmem_dealloc(tbase, a.tmem_cols);
 }
 
-template <int BITS, int T>
-int launch(const DeviceInfo* di, const CUtensorMap* tm, const Args& a, cudaStream_t stream)
+template <int BITS, int BOXES>
+bool set_attributes(const DeviceInfo* di)
 {
     static std::atomic<bool> ready[kMaxDevices];      // per device; setting the attribute twice is harmless
-    if (!ready[di->dev].load()) {
-        if (cudaFuncSetAttribute(mx_gemm_kernel<BITS, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<BITS, T>::kSmem) !=
-            cudaSuccess)
-            return WQ4_ERR_CUDA;
-        ready[di->dev].store(true);
-    }
+    if (ready[di->dev].load()) return true;
+    if (cudaFuncSetAttribute(mx_gemm_kernel<BITS, BOXES>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWhole) != cudaSuccess) return false;
+    ready[di->dev].store(true);
+    return true;
+}
+
+// Clusters of `split` CTAs that fit the device at once (cached per device).
+template <int BITS, int BOXES>
+int cluster_capacity(const DeviceInfo* di, int split, bool half)
+{
+    static std::atomic<int> cached[kMaxDevices][9][2];
+    if (split == 1) return half ? 2 * di->sm_count : di->sm_count;
+    if (const int n = cached[di->dev][split][half].load()) return n;
     cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = split;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(std::min(a.rtiles * a.ttiles, di->sm_count));
+    cfg.gridDim = dim3(split);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = Cfg<BITS, T>::kSmem;
-    cfg.stream = stream;
+    cfg.dynamicSmemBytes = half ? kHalf : kWhole;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, mx_gemm_kernel<BITS, T>, tm[0], tm[1], a) == cudaSuccess ? WQ4_OK : WQ4_ERR_CUDA;
+    int n = 0;
+    if (!set_attributes<BITS, BOXES>(di) || cudaOccupancyMaxActiveClusters(&n, mx_gemm_kernel<BITS, BOXES>, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        n = 0;
+    }
+    if (n > 0) cached[di->dev][split][half].store(n);
+    return n;
+}
+
+struct Plan {
+    int tok, split;
+    bool half, pair;
+};
+
+template <int BITS, int BOXES>
+int launch(const DeviceInfo* di, const CUtensorMap& w, const CUtensorMap& x, Args a, const Plan& pl, cudaStream_t stream)
+{
+    using C = Cfg<BITS, BOXES>;
+    if (!set_attributes<BITS, BOXES>(di)) return WQ4_ERR_CUDA;
+    const int64_t tiles = static_cast<int64_t>(a.rtiles) * a.ttiles;
+    a.tok = pl.tok;
+    a.split = pl.split;
+    a.slot_bytes = static_cast<int>(align_up(C::kW + BOXES * a.tok * 128 + 2 * C::kScales, 1024));
+    // sums: of groups of four tokens by 128 rows, a CTA's share from each
+    const int sums = a.split > 1 ? (a.tok / 4 + a.split - 1) / a.split * a.split * 128 * 16 : 0;
+    a.ring = kHeader + sums;
+    const int smem = pl.half ? kHalf : kWhole;
+    a.nslots = std::min((smem - a.ring) / a.slot_bytes, C::kMaxSlots);
+    a.tmem_cols = pl.half ? kTmemCols / 2 : kTmemCols;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = a.split;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(a.split > 1 ? tiles * a.split : std::min<int64_t>(tiles, pl.half ? 2 * di->sm_count : di->sm_count)));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.split > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, mx_gemm_kernel<BITS, BOXES>, w, x, a) == cudaSuccess ? WQ4_OK : WQ4_ERR_CUDA;
+}
+
+// Up to this many tokens two CTAs of an SM, by their tensor memory and shared memory.
+constexpr int kHalfTok = 80;
+
+// What a form takes, in us, with t = tokens of a tile / 128 and f = the share of its
+// CTAs that are busy: a + at t, beside k0 + k0t t (alone) .. + k1 + k1t t more (f = 1)
+// a slot, w a round after the first, and where s CTAs share a tile's K
+// st t + sf f + stf t f + ss (s - 2).
+struct Cost {
+    double a, at, k0, k0t, k1, k1t, w, st, sf, stf, ss;
+};
+
+// Fitted to 432 measurements (40 sizes of 1 to 4096 tokens, each form and split that
+// is possible, over copies of 400 MB): 3 to 7 % off on average; what it picks takes
+// 1.8 % more than the best on average, 18 % at most.  6144 x 4096 over one token:
+// whole 6.4 us, K in halves 5.5; 4096 x 14336 over 16 tokens 16.7 whole, 9.7 in
+// quarters; 512 tokens of 6144 x 4096 17.6 in single CTAs, 15.0 in pairs.
+constexpr Cost kCost[2][3] = {
+    // activations of 8 bits: two CTAs an SM, one, pairs
+    {{1.87, 1.16, 0.200, 0.088, 0.199, 0.188, 0.00, 0.63, 0.48, 5.98, 0.03},
+     {1.68, 0.93, 0.218, 0.184, 0.188, 0.000, 0.00, 3.18, 0.79, 0.92, 0.03},
+     {2.56, 1.63, 0.154, 0.047, 0.048, 0.005, 2.96, 0.00, 0.00, 0.00, 0.00}},
+    // of 4 bits
+    {{1.75, 1.30, 0.210, 0.042, 0.445, 0.450, 0.80, 0.76, 0.40, 4.66, 0.06},
+     {1.92, 0.81, 0.238, 0.000, 0.114, 0.000, 0.22, 2.25, 0.84, 1.56, 0.00},
+     {2.78, 1.57, 0.124, 0.060, 0.040, 0.032, 4.21, 0.00, 0.00, 0.00, 0.00}}};
+
+double estimate(const Cost& c, int tok, int slots, int64_t ctas, int cap, int s)
+{
+    const double t = tok / 128.0, f = std::min(1.0, static_cast<double>(ctas) / cap), n = (slots + s - 1) / s;
+    const double k0 = c.k0 + c.k0t * t, k1 = k0 + c.k1 + c.k1t * t;
+    const int64_t full = ctas / cap, rest = ctas % cap;
+    double us = c.a + c.at * t + n * (full * k1 + (rest ? k0 + (k1 - k0) * rest / cap : 0.0)) + c.w * (full - (rest ? 0 : 1));
+    if (s > 1) us += c.st * t + c.sf * f + c.stf * t * f + c.ss * (s - 2);
+    return us;
+}
+
+Plan pick(const DeviceInfo* di, int bits, int N, int M, int kblocks)
+{
+    const int tok = M > 112 ? 128 : (M + 15) / 16 * 16;
+    const int64_t tiles = (static_cast<int64_t>(N) + 127) / 128 * ((static_cast<int64_t>(M) + tok - 1) / tok);
+    Plan pl = {tok, 1, false, false};
+    double best = 1e300;
+    for (int half = tok <= kHalfTok ? 1 : 0; half >= 0; --half) {
+        const int slot = bits == 8 && half ? 1 : 2, slots = (kblocks + slot - 1) / slot;
+        for (int s = 1; s <= 8 && s <= slots; ++s) {
+            // a cluster's CTAs are on the GPU together: no more of them than fit
+            const int fit = s == 1      ? 0
+                            : bits == 4 ? cluster_capacity<4, 1>(di, s, half)
+                            : half      ? cluster_capacity<8, 1>(di, s, true)
+                                        : cluster_capacity<8, 2>(di, s, false);
+            if (s > 1 && tiles > fit) continue;
+            const double us = estimate(kCost[bits == 4][half ? 0 : 1], tok, slots, tiles * s, di->sm_count * (half ? 2 : 1), s);
+            if (us < best) best = us, pl.split = s, pl.half = half != 0;
+        }
+    }
+    if (M > 64) {
+        const int64_t pairs = (static_cast<int64_t>(N) + 255) / 256 * ((static_cast<int64_t>(M) + 255) / 256);
+        if (estimate(kCost[bits == 4][2], 256, bits == 8 ? kblocks : (kblocks + 1) / 2, pairs, di->sm_count / 2, 1) < best)
+            pl = {256, 1, false, true};
+    }
+    return pl;
 }
 
 // ------------------------------------------------------- pairs of CTAs --
@@ -283,8 +478,6 @@ struct PairCfg {
     static_assert(kSlots * kScaleCols <= kScaleSpace && kOver % 64 == 0, "tensor memory");
     static_assert(kSmem <= 227 * 1024, "shared memory");
 };
-
-constexpr int kPairThreads = 384;      // warps 4-11: two groups of four epilogue warps
 
 struct PairMaps {
     CUtensorMap w, x, ws, xs, y;
@@ -336,12 +529,12 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_gemm_pair_kernel(const __g
             tc::prefetch_map(&tm.ws);
             tc::prefetch_map(&tm.xs);
             grid_dependency_wait();
-            RingPos<S> p;
+            RingPos p;
             int n = 0;
             bool ok = true;
             for (int u = a.stall ? tiles : u0; u < tiles && ok; u += ustep) {
                 const int n0 = u / a.ttiles * 256 + 128 * rank, m0 = u % a.ttiles * T;
-                for (int k = 0; k < slots; ++k, ++n, p.next()) {
+                for (int k = 0; k < slots; ++k, ++n, p.next(S)) {
                     if (n >= S && !mbar_wait(&empty[p.slot], p.par ^ 1u, err)) {
                         ok = false;
                         break;
@@ -363,7 +556,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_gemm_pair_kernel(const __g
         if (rank == 0) {
             constexpr uint32_t idesc = BITS == 8 ? tc::idesc_mx_e2m1_e4m3(256, T) : tc::idesc_mx_e2m1_e2m1(256, T);
             const bool leader = tc::elect_one();
-            RingPos<S> p;
+            RingPos p;
             int dit = 0;
             bool ok = true;
             const uint64_t wdesc = tc::sw128_kmajor_desc(smem_addr(ring));
@@ -374,7 +567,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_gemm_pair_kernel(const __g
                 // the last tile's shared columns are read, and so all of the one before it
                 if (dit >= 1 && ok) ok = mbar_wait(dempty, (dit - 1) & 1, err);
                 tc::fence_after_sync();
-                for (int k = 0; k < slots; ++k, p.next()) {
+                for (int k = 0; k < slots; ++k, p.next(S)) {
                     if (ok) ok = mbar_wait(&full[p.slot], p.par, err);
                     tc::fence_after_sync();
                     const uint64_t off = static_cast<uint64_t>(p.slot) * (C::kSlot >> 4);
@@ -515,9 +708,10 @@ extern "C" int wq4_mx_gemm(const uint8_t* W, const uint8_t* W_scales, const uint
         return WQ4_ERR_INVALID;
     const DeviceInfo* di = current_device_info(nullptr);
     if (!di) return WQ4_ERR_CUDA;
-    const bool pair = M > 128 && static_cast<int64_t>((N - 1) / 256 + 1) * ((M - 1) / 256 + 1) >= di->sm_count / 2;
-    const int T = pair ? 256 : M <= 16 ? 16 : M <= 64 ? 64 : 128, rows = pair ? 256 : 128;
-    Args a;
+    const Plan pl = pick(di, bits, N, M, K / 128);
+    const bool pair = pl.pair;
+    const int T = pl.tok, rows = pair ? 256 : 128;
+    Args a = {};
     a.y = y;
     a.w_scales = W_scales;
     a.x_scales = x_scales;
@@ -535,9 +729,17 @@ extern "C" int wq4_mx_gemm(const uint8_t* W, const uint8_t* W_scales, const uint
     constexpr CUtensorMapDataType kBytes = CU_TENSOR_MAP_DATA_TYPE_UINT8, kWords = CU_TENSOR_MAP_DATA_TYPE_UINT32;
     constexpr CUtensorMapSwizzle kSwz = CU_TENSOR_MAP_SWIZZLE_128B, kPlain = CU_TENSOR_MAP_SWIZZLE_NONE;
     // activations of 8 bits: the weights' codes are spread on their way into shared memory
-    const bool w_ok = bits == 8 ? encode_tensor_map_2d(&tm.w, CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, W, k, N, wrow, 128, 128, kSwz)
-                                : encode_tensor_map_2d(&tm.w, kBytes, W, wrow, N, wrow, 128, 128, kSwz);
-    if (!w_ok || !encode_tensor_map_2d(&tm.x, kBytes, x, xrow, M, xrow, 128, T < 128 ? T : 128, kSwz)) return WQ4_ERR_CUDA;
+    constexpr CUtensorMapDataType kSpread = CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B;
+    const uint32_t box = T < 128 ? T : 128, boxes = pl.half ? 1 : 2;
+    const uint64_t n64 = static_cast<uint64_t>(N), m64 = static_cast<uint64_t>(M);
+    bool ok;
+    if (bits == 8 && !pair)
+        ok = encode_tensor_map_3d(&tm.w, kSpread, W, {128, n64, k / 128}, {wrow, 64}, {128, 128, boxes}, kSwz) &&
+             encode_tensor_map_3d(&tm.x, kBytes, x, {128, m64, k / 128}, {xrow, 128}, {128, box, boxes}, kSwz);
+    else
+        ok = encode_tensor_map_2d(&tm.w, bits == 8 ? kSpread : kBytes, W, bits == 8 ? k : wrow, n64, wrow, 128, 128, kSwz) &&
+             encode_tensor_map_2d(&tm.x, kBytes, x, xrow, m64, xrow, 128, box, kSwz);
+    if (!ok) return WQ4_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (pair) {
         const uint32_t sbox = bits == 8 ? 128 : 256;          // words: of one or two blocks of 128 K
@@ -550,7 +752,6 @@ extern "C" int wq4_mx_gemm(const uint8_t* W, const uint8_t* W_scales, const uint
             return WQ4_ERR_CUDA;
         return bits == 8 ? launch_pair<8>(di, tm, a, st) : launch_pair<4>(di, tm, a, st);
     }
-    const CUtensorMap tms[2] = {tm.w, tm.x};
-    if (bits == 8) return T == 16 ? launch<8, 16>(di, tms, a, st) : T == 64 ? launch<8, 64>(di, tms, a, st) : launch<8, 128>(di, tms, a, st);
-    return T == 16 ? launch<4, 16>(di, tms, a, st) : T == 64 ? launch<4, 64>(di, tms, a, st) : launch<4, 128>(di, tms, a, st);
+    if (bits == 4) return launch<4, 1>(di, tm.w, tm.x, a, pl, st);
+    return pl.half ? launch<8, 1>(di, tm.w, tm.x, a, pl, st) : launch<8, 2>(di, tm.w, tm.x, a, pl, st);
 }

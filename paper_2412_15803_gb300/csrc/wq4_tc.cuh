@@ -95,6 +95,16 @@ __device__ __forceinline__ void commit(uint64_t* bar)
                  : "memory");
 }
 
+// commit by the threads with `on`.
+__device__ __forceinline__ void commit_if(uint64_t* bar, uint32_t on)
+{
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_addr(bar)),
+        "r"(on)
+        : "memory");
+}
+
 // True in one lane of a converged warp.
 __device__ __forceinline__ bool elect_one()
 {
@@ -169,22 +179,22 @@ __host__ __device__ constexpr uint32_t idesc_mx_scale_byte(int byte)
 // D (+)= (A scaled by sfa) * (B scaled by sfb), A and B in shared memory (K-major,
 // 128-byte swizzle), the scales in tensor memory; issued by one thread.
 __device__ __forceinline__ void mma_mxf8f6f4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
-                                             uint32_t accumulate)
+                                             uint32_t accumulate, uint32_t on)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 q, %7, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(on)
         : "memory");
 }
 
 __device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
-                                         uint32_t accumulate)
+                                         uint32_t accumulate, uint32_t on)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 q, %7, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(on)
         : "memory");
 }
 
@@ -198,9 +208,11 @@ __device__ __forceinline__ uint64_t scales_desc(uint32_t saddr)
 // A block of scales, shared memory -> four columns of tensor memory (32 lanes,
 // repeated in each of the four quarters): column c, lane l is word c of row l.
 // Executed in order with the MMAs that this thread issues after it.
-__device__ __forceinline__ void cp_scales(uint32_t taddr, uint64_t desc)
+__device__ __forceinline__ void cp_scales(uint32_t taddr, uint64_t desc, uint32_t on)
 {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr), "l"(desc),
+                 "r"(on)
+                 : "memory");
 }
 
 // ------------------------------------------------- pairs of CTAs (cta_group::2) --
@@ -277,10 +289,21 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar)
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// Four words to another CTA's shared memory, counted as 16 bytes by a barrier there
+// (both cluster addresses).
+__device__ __forceinline__ void st_async(uint32_t addr, const uint32_t v[4], uint32_t bar)
+{
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(addr), "r"(v[0]),
+                 "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(bar)
+                 : "memory");
+}
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync_all()
 {
-    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    cluster_arrive();
+    cluster_wait();
 }
 
 // 32 consecutive columns of each lane.
