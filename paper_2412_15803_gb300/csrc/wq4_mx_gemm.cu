@@ -555,7 +555,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_gemm_pair_kernel(const __g
     } else if (warp == kIssuer) {
         if (rank == 0) {
             constexpr uint32_t idesc = BITS == 8 ? tc::idesc_mx_e2m1_e4m3(256, T) : tc::idesc_mx_e2m1_e2m1(256, T);
-            const bool leader = tc::elect_one();
+            const uint32_t leader = tc::elect_one() ? 1u : 0u;
             RingPos p;
             int dit = 0;
             bool ok = true;
@@ -573,34 +573,33 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_gemm_pair_kernel(const __g
                     const uint64_t off = static_cast<uint64_t>(p.slot) * (C::kSlot >> 4);
                     const uint32_t scol = tbase + C::kScaleCol0 + p.slot * C::kScaleCols;
                     const int nb = min(NB, a.kblocks - k * NB);
-                    if (leader) {
-                        // in tensor memory: the rows' scales of each 128 K, then the tokens' (two blocks of 128) of each
-                        for (int b = 0; b < nb; ++b) {
-                            tc::cp_scales_pair(scol + 4 * b, sdesc + off + b * 32);
-                            tc::cp_scales_pair(scol + 4 * NB + 8 * b, sdesc + off + (C::kScales >> 4) + b * 32);
-                            tc::cp_scales_pair(scol + 4 * NB + 8 * b + 4, sdesc + off + 2 * (C::kScales >> 4) + b * 32);
-                        }
+                    // in tensor memory: the rows' scales of each 128 K, then the tokens' (two blocks of 128) of each
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int b = BITS == 8 ? 0 : j >> 1;
-                            if (b >= nb) break;
-                            const uint32_t acc = k > 0 || j > 0 ? 1u : 0u;
-                            const uint32_t id = idesc | tc::idesc_mx_scale_byte(BITS == 8 ? j : 2 * (j & 1));
-                            if constexpr (BITS == 8)
-                                tc::mma_mxf8f6f4_pair(dcol, wdesc + off + 2 * j, xdesc + off + 2 * j, id, scol, scol + 4, acc);
-                            else
-                                tc::mma_mxf4_pair(dcol, wdesc + off + 2 * j, xdesc + off + 2 * j, id, scol + 4 * b,
-                                                  scol + 4 * NB + 8 * b, acc);
-                        }
-                        tc::commit_pair(&empty[p.slot]);
+                    for (int b = 0; b < NB; ++b) {
+                        if (b > 0 && b >= nb) break;
+                        tc::cp_scales_pair(scol + 4 * b, sdesc + off + b * 32, leader);
+                        tc::cp_scales_pair(scol + 4 * NB + 8 * b, sdesc + off + (C::kScales >> 4) + b * 32, leader);
+                        tc::cp_scales_pair(scol + 4 * NB + 8 * b + 4, sdesc + off + 2 * (C::kScales >> 4) + b * 32, leader);
                     }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int b = BITS == 8 ? 0 : j >> 1;
+                        if (b > 0 && b >= nb) break;
+                        const uint32_t acc = k > 0 || j > 0 ? 1u : 0u;
+                        const uint32_t id = idesc | tc::idesc_mx_scale_byte(BITS == 8 ? j : 2 * (j & 1));
+                        if constexpr (BITS == 8)
+                            tc::mma_mxf8f6f4_pair(dcol, wdesc + off + 2 * j, xdesc + off + 2 * j, id, scol, scol + 4, acc, leader);
+                        else
+                            tc::mma_mxf4_pair(dcol, wdesc + off + 2 * j, xdesc + off + 2 * j, id, scol + 4 * b,
+                                              scol + 4 * NB + 8 * b, acc, leader);
+                    }
+                    tc::commit_pair(&empty[p.slot], leader);
+                    if (k == slots - 1) tc::commit_pair(dfull, leader);
                     __syncwarp();
                 }
-                if (leader) tc::commit_pair(dfull);
-                __syncwarp();
             }
             // all MMAs issued have completed before tensor memory is released
-            if (leader) tc::commit_pair(drain);
+            tc::commit_pair(drain, leader);
             mbar_wait(drain, 0, err);
         }
     } else if (warp >= kEpi) {
@@ -619,18 +618,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_gemm_pair_kernel(const __g
             if (ok) ok = mbar_wait(dfull, dit & 1, err);
             __syncwarp();
             tc::fence_after_sync();
-#pragma unroll 1
-            for (int i = 0; i < 4; ++i) {
-                // blocks of 32 tokens, the shared columns' first, to the two groups in turn
-                const int blk = (((dit & 1) ? 0 : 8 - kOverBlocks) + 2 * i + grp) & 7;
-                uint32_t d[32];
-                tc::ld32(dcol + 32 * blk, d);
-                tc::ld_wait();
-                if (i == kOverBlocks / 2 - 1) {
-                    tc::fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) tc::mbar_arrive_cluster(dempty0);
-                }
+            // Blocks of 32 tokens, the shared columns' first, to the two groups in turn.
+            // Those go to registers before anything else: the next tile's MMAs wait.
+            const int first = ((dit & 1) ? 0 : 8 - kOverBlocks) + grp;
+            auto store = [&](int blk, const uint32_t d[32]) {
                 const int mb = m0 + 32 * blk;
                 if (a.bulk) {
                     uint16_t* st = stage + (nst & 1) * (C::kStage / 2);
@@ -651,6 +642,22 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_gemm_pair_kernel(const __g
                         if (n0 + row < a.N && mb + t < a.M)
                             a.y[static_cast<size_t>(mb + t) * a.N + n0 + row] = float_to_half_bits(__uint_as_float(d[t]));
                 }
+            };
+            uint32_t d[kOverBlocks / 2][32];
+#pragma unroll
+            for (int i = 0; i < kOverBlocks / 2; ++i) tc::ld32(dcol + 32 * ((first + 2 * i) & 7), d[i]);
+            tc::ld_wait();
+            tc::fence_before_sync();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive_cluster_relaxed(dempty0);
+#pragma unroll
+            for (int i = 0; i < kOverBlocks / 2; ++i) store((first + 2 * i) & 7, d[i]);
+#pragma unroll 1
+            for (int i = kOverBlocks / 2; i < 4; ++i) {
+                const int blk = (first + 2 * i) & 7;
+                tc::ld32(dcol + 32 * blk, d[0]);
+                tc::ld_wait();
+                store(blk, d[0]);
             }
         }
         if (warp % 4 == 0 && lane == 0) tc::bulk_wait<0>();
