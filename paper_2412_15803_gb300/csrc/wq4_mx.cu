@@ -120,7 +120,7 @@ __device__ __forceinline__ void store_scales(uint32_t w, uint8_t* __restrict__ s
 // The approximate exponential and quotient: relative errors of 2 ulp, and of
 // |g| 2^-23 from the exponent's product, far below the half step (2^-4) that the
 // code is off by.  (expf and an exact division: 70 us where these take 49, 4096
-// rows of 14336.)
+// rows of 14336 in 8 bits.)
 __device__ __forceinline__ float silu(float g)
 {
     return __fdividef(g, 1.f + __expf(-g));
@@ -152,9 +152,16 @@ __device__ __forceinline__ Place place(int M, int chunks)
     return {r, c, i < n && r < M};
 }
 
-// Rows without a sum over them: quantize, and silu(gate) * up.
+// Rows without a sum over them: quantize, and silu(gate) * up.  Bound by memory:
+// 4096 rows of 14336 silu in 49.1 us (6.0 TB/s) in 8 bits and 43.7 in 4, quantize in
+// 26.0 in 4 bits (5.7 TB/s); four rows' loads of each thread are in flight (two: 52.5,
+// 48.7 and 30.4), in blocks of 128 threads but for silu in 8 bits (256: 47.8 and 26.4
+// in 4 bits; silu in 8 bits with 128 51.9).
+template <int BITS, bool SILU>
+constexpr int kRowThreads = BITS == 8 && SILU ? 256 : 128;
+
 template <int BITS, bool SILU, int R>
-__global__ void __launch_bounds__(256) rows_kernel(const uint16_t* __restrict__ x, int stride, uint8_t* __restrict__ codes,
+__global__ void __launch_bounds__(kRowThreads<BITS, SILU>) rows_kernel(const uint16_t* __restrict__ x, int stride, uint8_t* __restrict__ codes,
                                                    uint8_t* __restrict__ scales, int M, int K)
 {
     grid_dependency_wait();
@@ -168,8 +175,8 @@ __global__ void __launch_bounds__(256) rows_kernel(const uint16_t* __restrict__ 
         a[q] = b[q] = make_uint4(0, 0, 0, 0);
         if (p.live && p.r + 32 * q < M) {
             const uint16_t* row = x + static_cast<size_t>(p.r + 32 * q) * stride + 8 * p.c;
-            a[q] = __ldcs(reinterpret_cast<const uint4*>(row));
-            if (SILU) b[q] = __ldcs(reinterpret_cast<const uint4*>(row + K));
+            a[q] = __ldg(reinterpret_cast<const uint4*>(row));
+            if (SILU) b[q] = __ldg(reinterpret_cast<const uint4*>(row + K));
         }
     }
     uint32_t w[R];
@@ -205,15 +212,28 @@ struct NormArgs {
     float eps;
 };
 
+__device__ __forceinline__ uint32_t add_half2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
 // fp16(x + residual) of eight values.
 __device__ __forceinline__ uint4 add_halves(uint4 x, uint4 r)
 {
-    float a[8], b[8];
-    to_floats(x, a);
-    to_floats(r, b);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) a[i] += b[i];
-    return to_halves(a);
+    return make_uint4(add_half2(x.x, r.x), add_half2(x.y, r.y), add_half2(x.z, r.z), add_half2(x.w, r.w));
+}
+
+// fp32 c + a b of the lower and of the upper halves: products of fp16 values are
+// exact in fp32, and need no conversion first (sm_100 and later).
+__device__ __forceinline__ float2 fma_halves(uint32_t a, uint32_t b, float2 c)
+{
+    asm("{\n\t.reg .f16 a0, a1, b0, b1;\n\tmov.b32 {a0, a1}, %2;\n\tmov.b32 {b0, b1}, %3;\n\t"
+        "fma.rn.f32.f16 %0, a0, b0, %0;\n\tfma.rn.f32.f16 %1, a1, b1, %1;\n\t}"
+        : "+f"(c.x), "+f"(c.y)
+        : "r"(a), "r"(b));
+    return c;
 }
 
 __device__ __forceinline__ uint4 load_h(const NormArgs& a, int r, int c)
@@ -225,20 +245,23 @@ __device__ __forceinline__ uint4 load_h(const NormArgs& a, int r, int c)
 
 __device__ __forceinline__ float squares(uint4 h, float ss)
 {
-    float v[8];
-    to_floats(h, v);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) ss = fmaf(v[j], v[j], ss);
-    return ss;
+    float2 t = fma_halves(h.x, h.x, make_float2(ss, 0.f));
+    t = fma_halves(h.y, h.y, t);
+    t = fma_halves(h.z, h.z, t);
+    t = fma_halves(h.w, h.w, t);
+    return t.x + t.y;
 }
 
+// f h g
 __device__ __forceinline__ void norm_codes(uint4 h, uint4 g, float f, float o[8])
 {
-    float v[8], w[8];
-    to_floats(h, v);
-    to_floats(g, w);
+    const uint32_t a[4] = {h.x, h.y, h.z, h.w}, b[4] = {g.x, g.y, g.z, g.w};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = v[j] * f * w[j];
+    for (int j = 0; j < 4; ++j) {
+        const float2 t = fma_halves(a[j], b[j], make_float2(0.f, 0.f));
+        o[2 * j] = t.x * f;
+        o[2 * j + 1] = t.y * f;
+    }
 }
 
 constexpr uint32_t kOnes = 0x3C003C00u;      // fp16 1, 1
@@ -248,7 +271,39 @@ __device__ __forceinline__ uint4 load_gain(const NormArgs& a, int c)
     return a.gain && c < (a.K >> 3) ? *reinterpret_cast<const uint4*>(a.gain + 8 * c) : make_uint4(kOnes, kOnes, kOnes, kOnes);
 }
 
-// Few rows, and rows of more than 16384: a block a row, the row in registers, NC
+// Rows of up to 512: a warp a row, eight rows a block, NC chunks of eight a lane.
+template <int BITS, int NC>
+__global__ void __launch_bounds__(256) norm_warp_kernel(const NormArgs a)
+{
+    grid_dependency_wait();
+    grid_dependents_launch();
+    const int64_t r = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    if (r >= a.M) return;
+    const int lane = threadIdx.x & 31, chunks = a.K >> 3;
+    uint4 h[NC];
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = lane + 32 * i;
+        h[i] = make_uint4(0, 0, 0, 0);
+        if (c < chunks) {
+            h[i] = load_h(a, static_cast<int>(r), c);
+            if (a.sum) *reinterpret_cast<uint4*>(a.sum + static_cast<size_t>(r) * a.sum_stride + 8 * c) = h[i];
+        }
+        ss = squares(h[i], ss);
+    }
+    const float f = rsqrtf(warp_sum(ss) / static_cast<float>(a.K) + a.eps);
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = lane + 32 * i;
+        float o[8];
+        norm_codes(h[i], load_gain(a, c), f, o);
+        const uint32_t w = store_codes<BITS>(o, a.codes, static_cast<int>(r), c, a.K, c < chunks);
+        store_scales(w, a.scales, static_cast<int>(r), c, a.K, c < chunks);
+    }
+}
+
+// A block a row, the row in registers, NC
 // chunks of eight a thread (NC = 0, rows of more than 32768: read again for the
 // second pass, from `sum` where there is one, since it may be x or residual).
 template <int BITS, int NC>
@@ -296,13 +351,13 @@ __global__ void __launch_bounds__(1024) norm_kernel(const NormArgs a)
     }
 }
 
-// Many rows: bulk copies bring the next rows into a ring in shared memory while
+// Many long rows: bulk copies bring the next rows into a ring in shared memory while
 // this one is in registers, so that what is in flight does not end at a block's
 // barrier; one barrier a row, after which its slot is free.
 constexpr int kNormSlots = 8;
 
 template <int BITS, int NC>
-__global__ void __launch_bounds__(NC == 1 ? 256 : 1024) norm_ring_kernel(const NormArgs a, const int slots, uint32_t* err)
+__global__ void __launch_bounds__(512) norm_ring_kernel(const NormArgs a, const int slots, uint32_t* err)
 {
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ float part[2][32];
@@ -466,10 +521,10 @@ bool four_rows(const DeviceInfo* di, int M, int K)
     return static_cast<int64_t>(M) * (K / 8) >= static_cast<int64_t>(di->sm_count) * 2048 * 8;
 }
 
-int64_t rows_grid(int M, int K, int R)
+int64_t rows_grid(int M, int K, int R, int threads)
 {
     const int64_t groups = R == 1 ? M : (static_cast<int64_t>(M) + 127) / 128 * 32;
-    return (groups * (K / 8) + 255) / 256;
+    return (groups * (K / 8) + threads - 1) / threads;
 }
 
 template <bool SILU>
@@ -487,17 +542,18 @@ int run_rows(const uint16_t* x, int stride, uint8_t* codes, uint8_t* scales, int
     if (overlaps(x, xb, codes, code_bytes(M, K, bits)) || overlaps(x, xb, scales, scale_bytes(M, K))) return WQ4_ERR_INVALID;
     const DeviceInfo* di = current_device_info(nullptr);
     if (!di) return WQ4_ERR_CUDA;
+    const int t = bits == 8 ? kRowThreads<8, SILU> : kRowThreads<4, SILU>;
     if (four_rows(di, M, K))
-        return launch(bits == 8 ? rows_kernel<8, SILU, 4> : rows_kernel<4, SILU, 4>, rows_grid(M, K, 4), 256, 0, stream, x, stride, codes,
+        return launch(bits == 8 ? rows_kernel<8, SILU, 4> : rows_kernel<4, SILU, 4>, rows_grid(M, K, 4, t), t, 0, stream, x, stride, codes,
                       scales, M, K);
-    return launch(bits == 8 ? rows_kernel<8, SILU, 1> : rows_kernel<4, SILU, 1>, rows_grid(M, K, 1), 256, 0, stream, x, stride, codes,
+    return launch(bits == 8 ? rows_kernel<8, SILU, 1> : rows_kernel<4, SILU, 1>, rows_grid(M, K, 1, t), t, 0, stream, x, stride, codes,
                   scales, M, K);
 }
 
 template <int BITS, int NC>
 int launch_norm_ring(const NormArgs& a, const DeviceInfo* di, void* stream)
 {
-    constexpr int kMost = 200 * 1024;
+    constexpr int kMost = 220 * 1024;
     static std::atomic<bool> ready[kMaxDevices];      // per device; setting the attribute twice is harmless
     if (!ready[di->dev].load()) {
         if (cudaFuncSetAttribute(norm_ring_kernel<BITS, NC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost) != cudaSuccess)
@@ -505,19 +561,27 @@ int launch_norm_ring(const NormArgs& a, const DeviceInfo* di, void* stream)
         ready[di->dev].store(true);
     }
     const int threads = (a.K / 8 + 32 * NC - 1) / (32 * NC) * 32;
-    const int blocks = std::max(1, 1280 / threads);                   // of an SM, by registers
+    const int blocks = std::max(1, 2048 / threads);                   // of an SM
     const int slot = (a.residual ? 4 : 2) * a.K;
     const int slots = std::max(1, std::min(kNormSlots, kMost / blocks / slot));
     const int64_t grid = std::min<int64_t>(a.M, static_cast<int64_t>(di->sm_count) * blocks);
     return launch(norm_ring_kernel<BITS, NC>, grid, threads, static_cast<size_t>(slots) * slot, stream, a, slots, di->status);
 }
 
+// Measured, 8 bits, us: by a block a row and by the ring 8192 rows of 4096 38.4 and
+// 38.9 (6.1 TB/s; 46.7 with conversions before every product), 8000 of 5120 48.5 and
+// 49.2, 6000 of 8192 58.1 and 57.3, 5000 of 11008 79.8 and 64.1; by a block and by a
+// warp a row 16384 of 1024 20.2 and 22.0, of 512 12.7 and 11.1, of 128 9.3 and 5.4.
 template <int BITS>
 int launch_norm(const NormArgs& a, const DeviceInfo* di, void* stream)
 {
     const int chunks = a.K / 8;
-    if (a.M > 4 * di->sm_count && a.K <= 16384)
-        return a.K <= 2048 ? launch_norm_ring<BITS, 1>(a, di, stream) : launch_norm_ring<BITS, 2>(a, di, stream);
+    if (chunks <= 64) {
+        const int64_t grid = (static_cast<int64_t>(a.M) + 7) / 8;
+        return chunks <= 32 ? launch(norm_warp_kernel<BITS, 1>, grid, 256, 0, stream, a)
+                            : launch(norm_warp_kernel<BITS, 2>, grid, 256, 0, stream, a);
+    }
+    if (a.M > 4 * di->sm_count && a.K > 6144 && a.K <= 16384) return launch_norm_ring<BITS, 4>(a, di, stream);
     const int threads = chunks < 1024 ? (chunks + 31) / 32 * 32 : 1024;
     const int n = (chunks + threads - 1) / threads;
     const int grid = std::min(a.M, di->sm_count * 16);
@@ -599,8 +663,8 @@ extern "C" int wq4_mx_dequantize(const uint8_t* codes, const uint8_t* scales, ui
     const DeviceInfo* di = current_device_info(nullptr);
     if (!di) return WQ4_ERR_CUDA;
     if (four_rows(di, M, K))
-        return launch(bits == 8 ? dequantize_kernel<8, 4> : dequantize_kernel<4, 4>, rows_grid(M, K, 4), 256, 0, stream, codes, scales, y,
+        return launch(bits == 8 ? dequantize_kernel<8, 4> : dequantize_kernel<4, 4>, rows_grid(M, K, 4, 256), 256, 0, stream, codes, scales, y,
                       y_stride, M, K);
-    return launch(bits == 8 ? dequantize_kernel<8, 1> : dequantize_kernel<4, 1>, rows_grid(M, K, 1), 256, 0, stream, codes, scales, y,
+    return launch(bits == 8 ? dequantize_kernel<8, 1> : dequantize_kernel<4, 1>, rows_grid(M, K, 1, 256), 256, 0, stream, codes, scales, y,
                   y_stride, M, K);
 }
