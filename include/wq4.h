@@ -205,14 +205,11 @@ int wq4_device_status(void* stream, int* flags_out);
  * fp16 rows 16-byte aligned with strides (in elements) that are multiples of
  * 8, y of wq4_mx_gemm 2-byte aligned; outputs overlap neither inputs nor each
  * other (buffers are compared from their first byte to their last).  bits is 4
- * or 8, M and N at least 1, N * K and M * K at most 2^41.  Launched with
+ * or 8, M and N at least 1, N * K and M * K at most 2^41 (wq4_mx_gemm refuses
+ * more than 2^30 tiles of 128 x 128 of y: WQ4_ERR_UNSUPPORTED).  Launched with
  * programmatic dependent launch; everything is read after the previous kernel in
- * `stream` has completed, but for wq4_mx_gemm's W and W_scales: it may copy them
- * while that kernel finishes, if that lets its dependents launch early, so such a
- * kernel must not write them.  (Of this library's, wq4_mx_norm and wq4_mx_silu
- * do; wq4_mx_quantize, which makes weights, does not.)  Deterministic.
- * WQ4_ERR_INVALID for sizes, null pointers and overlaps, WQ4_ERR_ALIGN,
- * WQ4_ERR_CUDA.
+ * `stream` has completed.  Deterministic.  WQ4_ERR_INVALID for sizes, null
+ * pointers and overlaps, WQ4_ERR_ALIGN, WQ4_ERR_CUDA.
  */
 
 /* Bytes of the scales of `rows` rows of K values; 0 for bad sizes. */

@@ -165,9 +165,7 @@ __global__ void __launch_bounds__(kRowThreads<BITS, SILU>) rows_kernel(const uin
                                                    uint8_t* __restrict__ scales, int M, int K)
 {
     grid_dependency_wait();
-    // wq4_mx_gemm copies its weights before the previous kernel is complete where
-    // that lets it begin early, and quantize writes weights
-    if (SILU) grid_dependents_launch();
+    grid_dependents_launch();
     const Place p = place<R>(M, K >> 3);
     uint4 a[R], b[R];
 #pragma unroll

@@ -162,18 +162,19 @@ __global__ void __launch_bounds__(kThreads, 2)
                 else
                     tc::tma_load_2d(to + slot * a.slot_bytes, w ? &tm_w : &tm_x, k * 128, r0, bar);
             };
-            // the first slots' weights, and more of the tile into L2, while the previous kernel finishes
-            const int early = !w || a.stall || u0 >= tiles ? 0 : min(S, k1 - k0);
-            for (int i = 0; i < early; ++i) copy(i, k0 + i, u0 / a.ttiles * 128);
-            if (early == S && k1 > k0 + S) {
-                if (!codes) bulk_prefetch(sc + (static_cast<size_t>(u0 / a.ttiles) * a.kblocks + (k0 + S) * NB) * 512,
-                              512u * (min(k1 * NB, a.kblocks) - (k0 + S) * NB));
-                for (int k = k0 + S; codes && k < min(k1, k0 + S + 24); ++k) {
-                    if constexpr (BITS == 8)
-                        tc::tma_prefetch_3d(&tm_w, 0, u0 / a.ttiles * 128, k * BOXES);
-                    else
-                        tc::tma_prefetch_2d(&tm_w, k * 128, u0 / a.ttiles * 128);
-                }
+            // The previous kernel may write the weights: the first tile's are fetched into
+            // L2 while it finishes and copied after it.
+            if (w && !a.stall && u0 < tiles) {
+                const int r0 = u0 / a.ttiles * 128, ke = min(k1, k0 + 32);
+                if (!codes)
+                    bulk_prefetch(sc + (static_cast<size_t>(r0 >> 7) * a.kblocks + k0 * NB) * 512, 512u * (min(ke * NB, a.kblocks) - k0 * NB));
+                else
+                    for (int k = k0; k < ke; ++k) {
+                        if constexpr (BITS == 8)
+                            tc::tma_prefetch_3d(&tm_w, 0, r0, k * BOXES);
+                        else
+                            tc::tma_prefetch_2d(&tm_w, k * 128, r0);
+                    }
             }
             grid_dependency_wait();
             if (warp == kTokens) grid_dependents_launch();
@@ -187,13 +188,14 @@ __global__ void __launch_bounds__(kThreads, 2)
                         ok = false;
                         break;
                     }
-                    if (n >= early) copy(p.slot, k, r0);
+                    copy(p.slot, k, r0);
                 }
             }
             // every copy issued has landed before the CTA's memory goes away
             for (int i = max(0, n - S); i < n; ++i) mbar_wait(&full[i % S], (i / S) & 1, err);
         }
     } else if (warp == kIssuer) {
+        grid_dependency_wait();          // its waits are bounded, the previous kernel's time is not
         const uint32_t idesc = BITS == 8 ? tc::idesc_mx_e2m1_e4m3(128, tok) : tc::idesc_mx_e2m1_e2m1(128, tok);
         const uint32_t leader = tc::elect_one() ? 1u : 0u;
         RingPos p;
@@ -554,6 +556,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_gemm_pair_kernel(const __g
         }
     } else if (warp == kIssuer) {
         if (rank == 0) {
+            grid_dependency_wait();      // its waits are bounded, the previous kernel's time is not
             constexpr uint32_t idesc = BITS == 8 ? tc::idesc_mx_e2m1_e4m3(256, T) : tc::idesc_mx_e2m1_e2m1(256, T);
             const uint32_t leader = tc::elect_one() ? 1u : 0u;
             RingPos p;
@@ -713,6 +716,7 @@ extern "C" int wq4_mx_gemm(const uint8_t* W, const uint8_t* W_scales, const uint
     if (overlaps(y, yb, W, wb) || overlaps(y, yb, W_scales, wq4_mx_scale_bytes(N, K)) || overlaps(y, yb, x, xb) ||
         overlaps(y, yb, x_scales, wq4_mx_scale_bytes(M, K)))
         return WQ4_ERR_INVALID;
+    if ((static_cast<int64_t>(N - 1) / 128 + 1) * (static_cast<int64_t>(M - 1) / 128 + 1) > (static_cast<int64_t>(1) << 30)) return WQ4_ERR_UNSUPPORTED;
     const DeviceInfo* di = current_device_info(nullptr);
     if (!di) return WQ4_ERR_CUDA;
     const Plan pl = pick(di, bits, N, M, K / 128);
@@ -730,7 +734,6 @@ extern "C" int wq4_mx_gemm(const uint8_t* W, const uint8_t* W_scales, const uint
     a.err = di->status;
     a.stall = test_copy_stall() == WQ4_STALL_MX ? 1 : 0;
     a.bulk = (N % 8) == 0 && aligned(y, 16) ? 1 : 0;
-    if (static_cast<int64_t>(a.rtiles) * a.ttiles > (static_cast<int64_t>(1) << 30)) return WQ4_ERR_INVALID;
     PairMaps tm;
     const uint64_t k = static_cast<uint64_t>(K), wrow = k / 2, xrow = k / 8 * bits, srow = k / 128 * 512;
     constexpr CUtensorMapDataType kBytes = CU_TENSOR_MAP_DATA_TYPE_UINT8, kWords = CU_TENSOR_MAP_DATA_TYPE_UINT32;

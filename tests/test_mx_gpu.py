@@ -9,6 +9,8 @@ ulp, a quotient and two products): a code is then the nearest of a value within 
 exact one.  Products are exact and their sums in fp32: K / 32 additions of at most 2^-22
 of sum |w x| each, under 2^-12 of it to K = 16384, and one rounding to fp16.
 """
+import time
+
 import numpy as np
 import pytest
 import torch
@@ -16,6 +18,7 @@ import torch
 import oracle
 from oracle import mx
 from paper_2412_15803_gb300 import wq4
+from test_dependent_launch_gpu import late_copy  # noqa: F401  (a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -191,35 +194,273 @@ def test_gemm(M, N, K, bits):
     check_product(gemm(W, ws, x, xs, M, N, K, bits), W, ws, x, xs, bits)
 
 
+def sampled(N, rng, n=400):
+    """Weight rows whose outputs are checked: the edges of the first, some and the last tiles, others at random."""
+    if N <= n:
+        return np.arange(N)
+    edges = np.concatenate([np.arange(0, 3), np.arange(125, 131), np.arange(253, 259), np.arange(N - 300, N)])
+    return np.unique(np.concatenate([edges, rng.integers(0, N, n - 315)]))
+
+
+def check_any(M, N, K, bits):
+    """Every output finite and repeated to the bit, sampled rows against the oracle."""
+    rng = np.random.default_rng(M * N + K)
+    W, ws = any_operand(rng, N, K, 4)
+    x, xs = any_operand(rng, M, K, bits)
+    xs -= 6 if bits == 8 else 0
+    y = gemm(W, ws, x, xs, M, N, K, bits)
+    assert np.all((y & 0x7C00) != 0x7C00)
+    n = sampled(N, rng)
+    check_product(y[:, n], W[n], ws[n], x, xs, bits)
+    assert np.array_equal(gemm(W, ws, x, xs, M, N, K, bits, 0x00), y)
+
+
 # pairs of blocks: tiles of 256 rows by 256 tokens, one and several a pair, ragged in each direction, rows that a
 # tensor copy can write and rows that it cannot
-PAIRS = [(129, 19464, 128), (200, 20003, 384), (513, 6600, 1280), (256, 40000, 256), (1000, 9728, 640), (700, 25001, 128), (2000, 5128, 2176)]
-
-
 @pytest.mark.parametrize("bits", [8, 4])
-@pytest.mark.parametrize("M,N,K", PAIRS)
+@pytest.mark.parametrize("M,N,K", [(200, 30003, 384), (513, 6600, 1280), (1000, 9728, 640), (1500, 10001, 128), (2000, 5128, 2176),
+                                   (1030, 40000, 256)])
 def test_gemm_pairs(M, N, K, bits):
-    rng = np.random.default_rng(M * N + K)
-    W, ws = any_operand(rng, N, K, 4)
-    x, xs = any_operand(rng, M, K, bits)
-    xs -= 6 if bits == 8 else 0
-    y = gemm(W, ws, x, xs, M, N, K, bits)
-    check_product(y, W, ws, x, xs, bits)
-    assert np.array_equal(gemm(W, ws, x, xs, M, N, K, bits, 0x00), y)
+    check_any(M, N, K, bits)
 
 
-# K split over a cluster, one tile a cluster and several; tokens in tiles of every size
-SPLITS = [(1, 40000, 1024), (3, 20001, 1152), (16, 29000, 640), (20, 6144, 4096), (40, 12000, 896), (77, 5003, 2176), (100, 9000, 1024),
-          (128, 8200, 3200), (150, 3000, 4096), (270, 2100, 2304)]
+# K split over a cluster, one or two blocks an SM; tokens in tiles of every size
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("M,N,K", [(1, 6144, 4096), (3, 2001, 8192), (16, 4096, 14336), (20, 6144, 4096), (40, 300, 14208), (77, 5003, 2176),
+                                   (100, 1000, 8064), (128, 4100, 14336), (150, 1003, 4096), (270, 1100, 14336), (90, 200, 1152), (1, 40000, 1024)])
+def test_gemm_split(M, N, K, bits):
+    check_any(M, N, K, bits)
 
 
 @pytest.mark.parametrize("bits", [8, 4])
-@pytest.mark.parametrize("M,N,K", SPLITS)
-def test_gemm_split(M, N, K, bits):
-    rng = np.random.default_rng(M * N + K)
+def test_gemm_over_drawn_sizes(bits):
+    """Sizes spread by their logarithm over what the call is for."""
+    rng = np.random.default_rng(bits)
+    for _ in range(12):
+        K = 128 * int(np.exp(rng.uniform(0, np.log(112))) + 0.5)
+        M, N = (int(np.exp(rng.uniform(0, np.log(hi))) + 0.5) for hi in (2000, 20000))
+        if M * N * K < 1.5e10:
+            check_any(M, N, K, bits)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("M,N,K", [(5, 400, 512), (100, 300, 2048), (600, 9728, 256)])
+def test_gemm_scales_and_codes_that_are_not_numbers(M, N, K, bits):
+    """A NaN of one token or weight row is that token's or row's alone; scales from 2^-127 to 2^127."""
+    rng = np.random.default_rng(5)
     W, ws = any_operand(rng, N, K, 4)
     x, xs = any_operand(rng, M, K, bits)
     xs -= 6 if bits == 8 else 0
-    y = gemm(W, ws, x, xs, M, N, K, bits)
-    check_product(y, W, ws, x, xs, bits)
-    assert np.array_equal(gemm(W, ws, x, xs, M, N, K, bits, 0x00), y)
+    ref = gemm(W, ws, x, xs, M, N, K, bits)
+    ws2, xs2, x2 = ws.copy(), xs.copy(), x.copy()
+    ws2[7, 1], xs2[3, K // 32 - 1] = 255, 255
+    bad = [3]
+    if bits == 8:
+        x2[M - 1, 40] = 0x7F
+        bad.append(M - 1)
+    y = gemm(W, ws2, x2, xs2, M, N, K, bits)
+    nan = (y & 0x7FFF) > 0x7C00
+    assert np.all(nan[:, 7]) and np.all(nan[bad])
+    keep = np.delete(np.arange(M), bad)
+    cols = np.delete(np.arange(N), 7)
+    assert np.array_equal(y[np.ix_(keep, cols)], ref[np.ix_(keep, cols)])
+    # far exponents that cancel: the same products
+    far = gemm(W, (ws.astype(int) - 120).astype(np.uint8), x, (xs.astype(int) + 120).astype(np.uint8), M, N, K, bits)
+    assert np.array_equal(far, ref)
+
+
+# ------------------------------------------------------------- a run of them --
+
+class Layer:
+    """A decoder layer's projections and what stands between, in microscaled form: tokens x [M][H], residual h."""
+
+    def __init__(self, M, bits, seed, H=512, F=1152, nq=768):
+        rng = np.random.default_rng(seed)
+        self.M, self.bits, self.H, self.F, self.nq = M, bits, H, F, nq
+        self.host = [(rng.standard_normal(s) * s[1] ** -0.5).astype(np.float16) for s in ((nq, H), (H, H), (2 * F, H), (H, F))]
+        self.mats = []
+        for w in self.host:
+            N, K = w.shape
+            c, s = torch.zeros((N, K // 2), dtype=torch.uint8, device="cuda"), torch.zeros(wq4.wq4_mx_scale_bytes(N, K), dtype=torch.uint8, device="cuda")
+            wq4.wq4_mx_quantize(dev(w), K, c, s, N, K, 4)
+            self.mats.append((c, s))
+        self.gains = [(1 + 0.3 * rng.standard_normal(H)).astype(np.float16) for _ in range(2)]
+        self.dgains = [dev(g) for g in self.gains]
+        self.x0, self.h0 = rng.standard_normal((M, H)).astype(np.float16), (2 * rng.standard_normal((M, H))).astype(np.float16)
+        self.x, self.h = dev(self.x0), dev(self.h0)
+        half = lambda n: torch.zeros((M, n), dtype=torch.int16, device="cuda")
+        self.qkv, self.o, self.gu, self.y = half(nq), half(H), half(2 * F), half(H)
+        self.held = [(torch.zeros((M, n * bits // 8), dtype=torch.uint8, device="cuda"),
+                      torch.zeros(wq4.wq4_mx_scale_bytes(M, n), dtype=torch.uint8, device="cuda")) for n in (H, H, H, F)]
+
+    def calls(self):
+        M, H, F, nq, b = self.M, self.H, self.F, self.nq, self.bits
+        (wq, sq), (wo, so), (wg, sg), (wd, sd) = self.mats
+        (c0, s0), (c1, s1), (c2, s2), (c3, s3) = self.held
+        return [lambda: wq4.wq4_mx_norm(self.x, H, self.h, H, self.dgains[0], 1e-5, self.h, H, c0, s0, M, H, b),
+                lambda: wq4.wq4_mx_gemm(wq, sq, c0, s0, self.qkv, nq, H, M, b),
+                lambda: wq4.wq4_mx_quantize(self.qkv, nq, c1, s1, M, H, b),
+                lambda: wq4.wq4_mx_gemm(wo, so, c1, s1, self.o, H, H, M, b),
+                lambda: wq4.wq4_mx_norm(self.o, H, self.h, H, self.dgains[1], 1e-5, self.h, H, c2, s2, M, H, b),
+                lambda: wq4.wq4_mx_gemm(wg, sg, c2, s2, self.gu, 2 * F, H, M, b),
+                lambda: wq4.wq4_mx_silu(self.gu, 2 * F, c3, s3, M, F, b),
+                lambda: wq4.wq4_mx_gemm(wd, sd, c3, s3, self.y, H, F, M, b)]
+
+    def run(self, sync=False):
+        for c in self.calls():
+            c()
+            if sync:
+                torch.cuda.synchronize()
+
+    def state(self):
+        torch.cuda.synchronize()
+        return [t.clone() for t in (self.h, self.qkv, self.o, self.gu, self.y, *(t for p in self.held for t in p))]
+
+    def reset(self):
+        self.x.copy_(dev(self.x0))
+        self.h.copy_(dev(self.h0))
+        torch.cuda.synchronize()
+
+
+def same(a, b):
+    return all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("M", [1, 5, 150])
+def test_layer_stage_by_stage(M, bits):
+    """Each stage on the GPU's own input to it."""
+    L = Layer(M, bits, 3)
+    L.run()
+    h1, qkv, o, gu, y, *held = [t.cpu().numpy() for t in L.state()]
+    codes = [(held[2 * i], held[2 * i + 1][mx.scale_index(M, n)]) for i, n in enumerate((L.H, L.H, L.H, L.F))]
+    f16 = lambda a: a.view(np.float16)
+    hmid, v = mx.norm(L.x0, L.h0, L.gains[0], 1e-5)
+    assert not mx.wrong_groups(*codes[0], v, bits, 2.0 ** -18).any()
+    assert np.array_equal(codes[1][0], mx.quantize(f16(qkv)[:, :L.H].astype(np.float64), bits)[0])
+    h, v = mx.norm(f16(o), hmid, L.gains[1], 1e-5)
+    assert np.array_equal(f16(h1), h) and not mx.wrong_groups(*codes[2], v, bits, 2.0 ** -18).any()
+    delta = (8 + 1.2 * np.abs(f16(gu)[:, :L.F].astype(np.float64))) * 2.0 ** -23
+    assert not mx.wrong_groups(*codes[3], mx.silu(f16(gu)), bits, delta, 2.0 ** -100).any()
+    for i, out in enumerate((qkv, o, gu, y)):
+        N, K = L.host[i].shape
+        wc, ws = L.mats[i][0].cpu().numpy(), L.mats[i][1].cpu().numpy()[mx.scale_index(N, K)]
+        c_ref, s_ref = mx.quantize(L.host[i].astype(np.float64), 4)
+        assert np.array_equal(wc, c_ref) and np.array_equal(ws, s_ref)
+        check_product(out.view(np.uint16), wc, ws, *codes[i], bits)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("M", [1, 40, 600])
+def test_layer_back_to_back(late_copy, M, bits):  # noqa: F811
+    """Nothing waited for between the calls, the first input written late by a kernel that lets its dependents launch."""
+    L = Layer(M, bits, 4, H=1024, F=2048, nq=1536)
+    L.run(sync=True)
+    want = L.state()
+    for _ in range(4):
+        L.reset()
+        src = L.x.clone()
+        L.x.zero_()
+        torch.cuda.synchronize()
+        late_copy(L.x, src, 100_000)
+        L.run()
+        assert same(L.state(), want)
+    assert wq4.wq4_device_status() == 0
+
+
+# one size of each form of the product: two blocks an SM, K split, one block an SM, pairs
+@pytest.mark.parametrize("M,N,K", [(1, 20000, 512), (1, 2048, 4096), (100, 2048, 1024), (1000, 9728, 512)])
+@pytest.mark.parametrize("bits", [8, 4])
+def test_gemm_reads_weights_that_a_running_kernel_writes(late_copy, M, N, K, bits):  # noqa: F811
+    rng = np.random.default_rng(6)
+    W, ws = (dev(a) for a in any_operand(rng, N, K, 4))
+    x, xs = (dev(a) for a in any_operand(rng, M, K, bits))
+    ws, xs = (dev(mx.tiled(a.cpu().numpy(), K)) for a in (ws, xs))
+    y = torch.zeros((M, N), dtype=torch.int16, device="cuda")
+    wq4.wq4_mx_gemm(W, ws, x, xs, y, N, K, M, bits)
+    torch.cuda.synchronize()
+    ref = y.clone()
+    for t in (W, ws, x, xs):
+        src = t.clone()
+        t.zero_()
+        y.zero_()
+        torch.cuda.synchronize()
+        late_copy(t, src)
+        wq4.wq4_mx_gemm(W, ws, x, xs, y, N, K, M, bits)
+        torch.cuda.synchronize()
+        assert torch.equal(y, ref)
+
+
+@pytest.mark.parametrize("M", [1, 200])
+def test_layer_in_a_graph(M):
+    """Captured, and replayed with other inputs in the same buffers."""
+    L, other = Layer(M, 8, 7), Layer(M, 8, 8)
+    L.run()                                    # attributes are set outside the capture
+    g = torch.cuda.CUDAGraph()
+    L.reset()
+    with torch.cuda.graph(g):
+        L.run()
+    L.reset()
+    g.replay()
+    got = L.state()
+    L.reset()
+    L.run()
+    assert same(got, L.state())
+    for (c, s), (c2, s2) in zip(L.mats, other.mats):
+        c.copy_(c2)
+        s.copy_(s2)
+    for a, b in zip(L.dgains, other.dgains):
+        a.copy_(b)
+    L.x.copy_(other.x)
+    L.h.copy_(other.h)
+    g.replay()
+    got = L.state()
+    other.run()
+    assert same(got, other.state())
+
+
+def test_layers_on_two_streams_at_once():
+    a, b = Layer(30, 8, 9), Layer(300, 4, 10)
+    a.run()
+    b.run()
+    want = [a.state(), b.state()]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        a.reset()
+        b.reset()
+        for ca, cb in zip(a.calls(), b.calls()):
+            with torch.cuda.stream(streams[0]):
+                ca()
+            with torch.cuda.stream(streams[1]):
+                cb()
+        assert same(a.state(), want[0]) and same(b.state(), want[1])
+    assert wq4.wq4_device_status() == 0
+
+
+# every form of the product, one tile a block and several
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("M,N,K", [(1, 6144, 4096), (3, 60000, 512), (100, 2048, 1024), (200, 1024, 4096), (1500, 28672, 512)])
+def test_gemm_without_its_copies_ends(M, N, K, bits):
+    """The waits for copies that never come run out, are flagged, and the next call is clean."""
+    rng = np.random.default_rng(11)
+    W, ws = any_operand(rng, N, K, 4)
+    x, xs = any_operand(rng, M, K, bits)
+    args = [dev(W), dev(mx.tiled(ws, K)), dev(x), dev(mx.tiled(xs, K)), torch.zeros((M, N), dtype=torch.int16, device="cuda"), N, K, M, bits]
+    wq4.wq4_mx_gemm(*args)
+    torch.cuda.synchronize()
+    ref = args[4].clone()
+    assert wq4.wq4_device_status() == 0
+    try:
+        wq4.wq4_test_copy_stall(4)
+        t0 = time.perf_counter()
+        wq4.wq4_mx_gemm(*args)
+        torch.cuda.synchronize()
+        took = time.perf_counter() - t0
+        flags = wq4.wq4_device_status()
+    finally:
+        wq4.wq4_test_copy_stall()
+    assert flags == 1 and 0.4 < took < 4.0
+    args[4].zero_()
+    wq4.wq4_mx_gemm(*args)
+    torch.cuda.synchronize()
+    assert wq4.wq4_device_status() == 0 and torch.equal(args[4], ref)
