@@ -392,26 +392,26 @@ constexpr int kHalfTok = 80;
 
 // What a form takes, in us, with t = tokens of a tile / 128 and f = the share of its
 // CTAs that are busy: a + at t, beside k0 + k0t t (alone) .. + k1 + k1t t more (f = 1)
-// a slot, w a round after the first, and where s CTAs share a tile's K
-// st t + sf f + stf t f + ss (s - 2).
+// a slot, w a round after the first; where s CTAs share a tile's K st t + sf f +
+// stf t f + ss (s - 2); where an SM has two CTAs kd a slot and d more.
 struct Cost {
-    double a, at, k0, k0t, k1, k1t, w, st, sf, stf, ss;
+    double a, at, k0, k0t, k1, k1t, w, st, sf, stf, ss, kd, d;
 };
 
-// Fitted to 432 measurements (40 sizes of 1 to 4096 tokens, each form and split that
-// is possible, over copies of 400 MB): 3 to 7 % off on average; what it picks takes
-// 1.8 % more than the best on average, 18 % at most.  6144 x 4096 over one token:
-// whole 6.4 us, K in halves 5.5; 4096 x 14336 over 16 tokens 16.7 whole, 9.7 in
-// quarters; 512 tokens of 6144 x 4096 17.6 in single CTAs, 15.0 in pairs.
+// Fitted to 426 measurements (78 sizes of 1 to 4096 tokens, each form and split that
+// is possible, over copies of 400 MB), those near the best of a size above all: what
+// it picks takes 1.5 % more than the best on average, 15 % at most.  6144 x 4096 over
+// one token: whole 6.6 us, K in thirds 5.4; 4096 x 14336 over 16 tokens 17.0 whole,
+// 9.9 in sixths; 512 tokens of 6144 x 4096 17.6 in single CTAs, 14.0 in pairs.
 constexpr Cost kCost[2][3] = {
     // activations of 8 bits: two CTAs an SM, one, pairs
-    {{1.87, 1.16, 0.200, 0.088, 0.199, 0.188, 0.00, 0.63, 0.48, 5.98, 0.03},
-     {1.68, 0.93, 0.218, 0.184, 0.188, 0.000, 0.00, 3.18, 0.79, 0.92, 0.03},
-     {2.56, 1.63, 0.154, 0.047, 0.048, 0.005, 2.96, 0.00, 0.00, 0.00, 0.00}},
+    {{1.854, 0.916, 0.182, 0.136, 0.206, 0.131, 0.000, 1.897, 0.000, 2.660, 0.029, 0.022, 0.683},
+     {1.900, 0.633, 0.209, 0.172, 0.221, 0.026, 0.000, 2.317, 0.636, 2.287, 0.058, 0.000, 0.000},
+     {2.306, 1.440, 0.138, 0.052, 0.044, 0.003, 2.683, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000}},
     // of 4 bits
-    {{1.75, 1.30, 0.210, 0.042, 0.445, 0.450, 0.80, 0.76, 0.40, 4.66, 0.06},
-     {1.92, 0.81, 0.238, 0.000, 0.114, 0.000, 0.22, 2.25, 0.84, 1.56, 0.00},
-     {2.78, 1.57, 0.124, 0.060, 0.040, 0.032, 4.21, 0.00, 0.00, 0.00, 0.00}}};
+    {{1.776, 1.186, 0.184, 0.165, 0.385, 0.049, 2.436, 2.008, 0.000, 2.251, 0.063, 0.148, 0.434},
+     {1.813, 1.197, 0.224, 0.000, 0.144, 0.000, 0.095, 1.360, 1.000, 2.008, 0.036, 0.000, 0.000},
+     {2.365, 1.324, 0.101, 0.073, 0.037, 0.022, 3.658, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000}}};
 
 double estimate(const Cost& c, int tok, int slots, int64_t ctas, int cap, int s)
 {
@@ -419,6 +419,7 @@ double estimate(const Cost& c, int tok, int slots, int64_t ctas, int cap, int s)
     const double k0 = c.k0 + c.k0t * t, k1 = k0 + c.k1 + c.k1t * t;
     const int64_t full = ctas / cap, rest = ctas % cap;
     double us = c.a + c.at * t + n * (full * k1 + (rest ? k0 + (k1 - k0) * rest / cap : 0.0)) + c.w * (full - (rest ? 0 : 1));
+    if (2 * ctas > cap) us += n * c.kd + c.d;
     if (s > 1) us += c.st * t + c.sf * f + c.stf * t * f + c.ss * (s - 2);
     return us;
 }
