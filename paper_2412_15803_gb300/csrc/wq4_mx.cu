@@ -24,43 +24,42 @@ namespace {
 
 constexpr unsigned kAll = 0xffffffffu;
 
+// Two fp32 values an instruction.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<uint64_t&>(d))
+        : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+    return d;
+}
+
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<uint64_t&>(d))
+        : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+    return d;
+}
+
 // Eight fp16 values of a 16-byte load.
-__device__ __forceinline__ void to_floats(uint4 q, float v[8])
+__device__ __forceinline__ void to_floats(uint4 q, float2 v[4])
 {
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-        v[2 * i] = f.x;
-        v[2 * i + 1] = f.y;
-    }
+    for (int i = 0; i < 4; ++i) v[i] = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
 }
 
-__device__ __forceinline__ uint4 to_halves(const float v[8])
+__device__ __forceinline__ uint4 to_halves(const float2 v[4])
 {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+        const __half2 h = __floats2half2_rn(v[i].x, v[i].y);
         w[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// (b, a) as two e4m3 codes, a in the lower byte.
-__device__ __forceinline__ uint32_t e4m3x2(float a, float b)
-{
-    uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
-    return r;
-}
-
-// (b, a) as two e2m1 codes, a in the lower nibble.
-__device__ __forceinline__ uint32_t e2m1x2(float a, float b)
-{
-    uint16_t r;
-    asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u16.u8 %0, t;\n\t}" : "=h"(r) : "f"(b), "f"(a));
-    return r;
 }
 
 // Where the scales of row r's columns [128 kb, 128 kb + 128) lie.
@@ -69,47 +68,125 @@ __device__ __forceinline__ size_t scale_word(int r, int kb, int K)
     return (static_cast<size_t>(r >> 7) * (K >> 7) + kb) * 512 + (r & 31) * 16 + ((r >> 5) & 3) * 4;
 }
 
-// |a| and |b|: the larger, NaN if either is.
-__device__ __forceinline__ float max_abs(float a, float b)
+// The largest magnitude of three, NaN if one is.
+__device__ __forceinline__ float max_abs(float a, float b, float c)
 {
     float d;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(fabsf(a)), "f"(fabsf(b)));
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
 
-// Codes of the eight values that each lane has of columns [8 c, 8 c + 8) of row
-// r, and the word of scales of its 128 columns (in every lane); all lanes of a
-// warp, 16 in turn with 16 consecutive c.  Lanes without `live` store nothing.
+// The scale byte of a group whose largest magnitude has the bits mb.
 template <int BITS>
-__device__ __forceinline__ uint32_t store_codes(const float v[8], uint8_t* __restrict__ codes, int r, int c, int K, bool live)
+__device__ __forceinline__ uint32_t scale_of(uint32_t mb)
 {
-    float m = max_abs(max_abs(max_abs(v[0], v[1]), max_abs(v[2], v[3])), max_abs(max_abs(v[4], v[5]), max_abs(v[6], v[7])));
-    m = max_abs(m, __shfl_xor_sync(kAll, m, 1));
-    m = max_abs(m, __shfl_xor_sync(kAll, m, 2));
-    const uint32_t mb = __float_as_uint(m);
     constexpr int kTop = BITS == 8 ? 8 : 2;                       // top = 1.75 * 2^8, 1.5 * 2^2
     constexpr uint32_t kUp = BITS == 8 ? 0x1FFFFFu : 0x3FFFFFu;   // carries into the exponent where 1 + f is over that
-    const bool bad = mb >= 0x7F800000u;
-    int e = static_cast<int>((mb + kUp) >> 23) - 127 - kTop;
-    e = mb == 0 ? 0 : max(e, -127);
-    const float inv = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-    float q[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = v[i] * inv;
-    if constexpr (BITS == 8) {
-        uint2 o = make_uint2(e4m3x2(q[0], q[1]) | (e4m3x2(q[2], q[3]) << 16), e4m3x2(q[4], q[5]) | (e4m3x2(q[6], q[7]) << 16));
-        if (bad) o = make_uint2(0, 0);
-        if (live) *reinterpret_cast<uint2*>(codes + static_cast<size_t>(r) * K + 8 * c) = o;
-    } else {
-        uint32_t o = e2m1x2(q[0], q[1]) | (e2m1x2(q[2], q[3]) << 8) | (e2m1x2(q[4], q[5]) << 16) | (e2m1x2(q[6], q[7]) << 24);
-        if (bad) o = 0;
-        if (live) *reinterpret_cast<uint32_t*>(codes + static_cast<size_t>(r) * (K >> 1) + 4 * c) = o;
-    }
-    // group j's byte at place j of the word of 128 columns
-    uint32_t w = static_cast<uint32_t>(bad ? 255 : e + 127) << (8 * ((c >> 2) & 3));
+    const int e = max(static_cast<int>((mb + kUp) >> 23) - kTop, 0);
+    return mb == 0 ? 127u : mb >= 0x7F800000u ? 255u : static_cast<uint32_t>(e);
+}
+
+// Codes of columns [8 c, 8 c + 8) of row r, zeros where the group's scale is NaN.
+template <int BITS>
+__device__ __forceinline__ void put_codes(uint2 o, uint32_t byte, uint8_t* __restrict__ codes, int r, int c, int K, bool live)
+{
+    if (byte == 255u) o = make_uint2(0, 0);
+    if (!live) return;
+    if constexpr (BITS == 8)
+        *reinterpret_cast<uint2*>(codes + static_cast<size_t>(r) * K + 8 * c) = o;
+    else
+        *reinterpret_cast<uint32_t*>(codes + static_cast<size_t>(r) * (K >> 1) + 4 * c) = o.x;
+}
+
+// The word of scales of a lane's 128 columns, group j's byte at place j (in each of
+// its 16 lanes).
+__device__ __forceinline__ uint32_t scale_bytes_of(uint32_t byte, int c)
+{
+    uint32_t w = byte << (8 * ((c >> 2) & 3));
     w |= __shfl_xor_sync(kAll, w, 4);
     w |= __shfl_xor_sync(kAll, w, 8);
     return w;
+}
+
+// Codes of the eight values that each lane has of columns [8 c, 8 c + 8) of row
+// r, and the word of scales of its 128 columns; all lanes of a warp, 16 in turn
+// with 16 consecutive c.  Lanes without `live` store nothing.
+template <int BITS>
+__device__ __forceinline__ uint32_t store_codes(const float2 v[4], uint8_t* __restrict__ codes, int r, int c, int K, bool live)
+{
+    float m = max_abs(max_abs(v[0].x, v[0].y, v[1].x), max_abs(v[1].y, v[2].x, v[2].y), max_abs(v[3].x, v[3].y, 0.f));
+    m = max_abs(m, __shfl_xor_sync(kAll, m, 1), 0.f);
+    m = max_abs(m, __shfl_xor_sync(kAll, m, 2), 0.f);
+    const uint32_t byte = scale_of<BITS>(__float_as_uint(m));
+    const float inv = __uint_as_float((254u - byte) << 23);       // (a NaN scale's codes are not used)
+    float2 q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = mul2(v[i], make_float2(inv, inv));
+    uint2 o = make_uint2(0, 0);
+    if constexpr (BITS == 8) {
+        asm("{\n\t.reg .b16 a, b, c, d;\n\t"
+            "cvt.rn.satfinite.e4m3x2.f32 a, %3, %2;\n\tcvt.rn.satfinite.e4m3x2.f32 b, %5, %4;\n\t"
+            "cvt.rn.satfinite.e4m3x2.f32 c, %7, %6;\n\tcvt.rn.satfinite.e4m3x2.f32 d, %9, %8;\n\t"
+            "mov.b32 %0, {a, b};\n\tmov.b32 %1, {c, d};\n\t}"
+            : "=r"(o.x), "=r"(o.y)
+            : "f"(q[0].x), "f"(q[0].y), "f"(q[1].x), "f"(q[1].y), "f"(q[2].x), "f"(q[2].y), "f"(q[3].x), "f"(q[3].y));
+    } else {
+        asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+            "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+            "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+            "mov.b32 %0, {a, b, c, d};\n\t}"
+            : "=r"(o.x)
+            : "f"(q[0].x), "f"(q[0].y), "f"(q[1].x), "f"(q[1].y), "f"(q[2].x), "f"(q[2].y), "f"(q[3].x), "f"(q[3].y));
+    }
+    put_codes<BITS>(o, byte, codes, r, c, K, live);
+    return scale_bytes_of(byte, c);
+}
+
+// The same for fp16 values as they were loaded.  Magnitudes are compared as
+// integers (NaN is over all numbers), and where 2^-e is a normal fp16 number the
+// values are scaled in fp16: exactly, but for those that become smaller than 2^-14,
+// whose codes are 0 either way.
+template <int BITS>
+__device__ __forceinline__ uint32_t store_codes(uint4 x, uint8_t* __restrict__ codes, int r, int c, int K, bool live)
+{
+    auto max2 = [](uint32_t a, uint32_t b) {
+        uint32_t d;
+        asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+        return d;
+    };
+    constexpr uint32_t kAbs = 0x7FFF7FFFu;
+    uint32_t m = max2(max2(x.x & kAbs, x.y & kAbs), max2(x.z & kAbs, x.w & kAbs));
+    m = max2(m, __shfl_xor_sync(kAll, m, 1));
+    m = max2(m, __shfl_xor_sync(kAll, m, 2));
+    const uint32_t byte = scale_of<BITS>(__float_as_uint(half_bits_to_float(static_cast<uint16_t>(max(m & 0xFFFFu, m >> 16)))));
+    const bool normal = byte >= 127u - 15u;       // 2^-e at most 2^15 (and at least 2^-14: e is 14 at most)
+    uint2 o = make_uint2(0, 0);
+    if (__all_sync(kAll, normal)) {
+        const uint32_t inv = (127u + 15u - min(byte, 127u + 14u)) << 10;
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        uint32_t h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(h[i]) : "r"(w[i]), "r"(inv | (inv << 16)));
+        if constexpr (BITS == 8)
+            asm("{\n\t.reg .b16 a, b, c, d;\n\t"
+                "cvt.rn.satfinite.e4m3x2.f16x2 a, %2;\n\tcvt.rn.satfinite.e4m3x2.f16x2 b, %3;\n\t"
+                "cvt.rn.satfinite.e4m3x2.f16x2 c, %4;\n\tcvt.rn.satfinite.e4m3x2.f16x2 d, %5;\n\t"
+                "mov.b32 %0, {a, b};\n\tmov.b32 %1, {c, d};\n\t}"
+                : "=r"(o.x), "=r"(o.y)
+                : "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]));
+        else
+            asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+                "cvt.rn.satfinite.e2m1x2.f16x2 a, %1;\n\tcvt.rn.satfinite.e2m1x2.f16x2 b, %2;\n\t"
+                "cvt.rn.satfinite.e2m1x2.f16x2 c, %3;\n\tcvt.rn.satfinite.e2m1x2.f16x2 d, %4;\n\t"
+                "mov.b32 %0, {a, b, c, d};\n\t}"
+                : "=r"(o.x)
+                : "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]));
+        put_codes<BITS>(o, byte, codes, r, c, K, live);
+        return scale_bytes_of(byte, c);
+    }
+    float2 v[4];
+    to_floats(x, v);
+    return store_codes<BITS>(v, codes, r, c, K, live);
 }
 
 __device__ __forceinline__ void store_scales(uint32_t w, uint8_t* __restrict__ scales, int r, int c, int K, bool live)
@@ -117,13 +194,21 @@ __device__ __forceinline__ void store_scales(uint32_t w, uint8_t* __restrict__ s
     if (live && (c & 15) == 0) *reinterpret_cast<uint32_t*>(scales + scale_word(r, c >> 4, K)) = w;
 }
 
-// The approximate exponential and quotient: relative errors of 2 ulp, and of
-// |g| 2^-23 from the exponent's product, far below the half step (2^-4) that the
-// code is off by.  (expf and an exact division: 70 us where these take 49, 4096
-// rows of 14336 in 8 bits.)
-__device__ __forceinline__ float silu(float g)
+// silu(g) u = g u / (1 + 2^(-g log2 e)) of two values, with the approximate
+// exponential and reciprocal: relative errors of 2^-22 and 2^-23, and of |g| 2^-23
+// from the exponent's product, far below the half step (2^-4) that the code is off
+// by.  Under g = -87 the reciprocal is 0.  (expf and exact quotients: 70 us where
+// these take 46, 4096 rows of 14336 in 8 bits.)
+__device__ __forceinline__ float2 silu_times(float2 g, float2 u)
 {
-    return __fdividef(g, 1.f + __expf(-g));
+    const float2 t = mul2(g, make_float2(-1.44269504f, -1.44269504f));
+    float2 e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(t.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(t.y));
+    e = add2(e, make_float2(1.f, 1.f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(e.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(e.y));
+    return mul2(mul2(g, u), r);
 }
 
 // A lane's place in a call on rows: eight columns, and rows r, r + 32, r + 64 and
@@ -180,15 +265,17 @@ __global__ void __launch_bounds__(kRowThreads<BITS, SILU>) rows_kernel(const uin
     uint32_t w[R];
 #pragma unroll
     for (int q = 0; q < R; ++q) {
-        float v[8];
-        to_floats(a[q], v);
+        const bool live = p.live && p.r + 32 * q < M;
         if constexpr (SILU) {
-            float u[8];
+            float2 v[4], u[4];
+            to_floats(a[q], v);
             to_floats(b[q], u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = silu(v[i]) * u[i];
+            for (int i = 0; i < 4; ++i) v[i] = silu_times(v[i], u[i]);
+            w[q] = store_codes<BITS>(v, codes, p.r + 32 * q, p.c, K, live);
+        } else {
+            w[q] = store_codes<BITS>(a[q], codes, p.r + 32 * q, p.c, K, live);
         }
-        w[q] = store_codes<BITS>(v, codes, p.r + 32 * q, p.c, K, p.live && p.r + 32 * q < M);
     }
     if (R == 4 && p.r + 96 < M) {
         if (p.live && (p.c & 15) == 0)
@@ -251,15 +338,11 @@ __device__ __forceinline__ float squares(uint4 h, float ss)
 }
 
 // f h g
-__device__ __forceinline__ void norm_codes(uint4 h, uint4 g, float f, float o[8])
+__device__ __forceinline__ void norm_codes(uint4 h, uint4 g, float f, float2 o[4])
 {
     const uint32_t a[4] = {h.x, h.y, h.z, h.w}, b[4] = {g.x, g.y, g.z, g.w};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float2 t = fma_halves(a[j], b[j], make_float2(0.f, 0.f));
-        o[2 * j] = t.x * f;
-        o[2 * j + 1] = t.y * f;
-    }
+    for (int j = 0; j < 4; ++j) o[j] = mul2(fma_halves(a[j], b[j], make_float2(0.f, 0.f)), make_float2(f, f));
 }
 
 constexpr uint32_t kOnes = 0x3C003C00u;      // fp16 1, 1
@@ -294,7 +377,7 @@ __global__ void __launch_bounds__(256) norm_warp_kernel(const NormArgs a)
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
         const int c = lane + 32 * i;
-        float o[8];
+        float2 o[4];
         norm_codes(h[i], load_gain(a, c), f, o);
         const uint32_t w = store_codes<BITS>(o, a.codes, static_cast<int>(r), c, a.K, c < chunks);
         store_scales(w, a.scales, static_cast<int>(r), c, a.K, c < chunks);
@@ -341,7 +424,7 @@ __global__ void __launch_bounds__(1024) norm_kernel(const NormArgs a)
                 v = make_uint4(0, 0, 0, 0);
                 if (live) v = a.sum ? *reinterpret_cast<const uint4*>(a.sum + static_cast<size_t>(r) * a.sum_stride + 8 * c) : load_h(a, r, c);
             }
-            float o[8];
+            float2 o[4];
             norm_codes(v, load_gain(a, c), f, o);
             const uint32_t w = store_codes<BITS>(o, a.codes, r, c, a.K, live);
             store_scales(w, a.scales, r, c, a.K, live);
@@ -411,7 +494,7 @@ __global__ void __launch_bounds__(512) norm_ring_kernel(const NormArgs a, const 
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             const int c = t + i * nt;
-            float o[8];
+            float2 o[4];
             norm_codes(h[i], g[i], f, o);
             const uint32_t w = store_codes<BITS>(o, a.codes, static_cast<int>(r), c, a.K, c < chunks);
             store_scales(w, a.scales, static_cast<int>(r), c, a.K, c < chunks);
@@ -458,10 +541,10 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restri
                 asm("{\n\t.reg .b8 t, u;\n\tmov.b16 {t, u}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(h[i]) : "h"(c2));
             }
         }
-        float v[8];
+        float2 v[4];
         to_floats(make_uint4(h[0], h[1], h[2], h[3]), v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= s;
+        for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], make_float2(s, s));
         *reinterpret_cast<uint4*>(y + static_cast<size_t>(p.r + 32 * q) * stride + 8 * p.c) = to_halves(v);
     }
 }
