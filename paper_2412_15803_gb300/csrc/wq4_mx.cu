@@ -238,10 +238,11 @@ __device__ __forceinline__ Place place(int M, int chunks)
 }
 
 // Rows without a sum over them: quantize, and silu(gate) * up.  Bound by memory:
-// 4096 rows of 14336 silu in 49.1 us (6.0 TB/s) in 8 bits and 43.7 in 4, quantize in
-// 26.0 in 4 bits (5.7 TB/s); four rows' loads of each thread are in flight (two: 52.5,
-// 48.7 and 30.4), in blocks of 128 threads but for silu in 8 bits (256: 47.8 and 26.4
-// in 4 bits; silu in 8 bits with 128 51.9).
+// 4096 rows of 14336 silu in 45.2 us (6.5 TB/s) in 8 bits and 41.6 in 4, quantize in
+// 25.5 in 4 bits (5.8 TB/s).  Before two values an instruction they were bound by
+// issue (49.1, 43.7 and 26.0 at 0.72 of it).  Four rows' loads of each thread are in
+// flight (two, then: 52.5, 48.7 and 30.4), in blocks of 128 threads but for silu in 8
+// bits (256: 42.5 and 25.8 in 4 bits; silu in 8 bits with 128 50.9).
 template <int BITS, bool SILU>
 constexpr int kRowThreads = BITS == 8 && SILU ? 256 : 128;
 
@@ -650,9 +651,11 @@ int launch_norm_ring(const NormArgs& a, const DeviceInfo* di, void* stream)
 }
 
 // Measured, 8 bits, us: by a block a row and by the ring 8192 rows of 4096 38.4 and
-// 38.9 (6.1 TB/s; 46.7 with conversions before every product), 8000 of 5120 48.5 and
-// 49.2, 6000 of 8192 58.1 and 57.3, 5000 of 11008 79.8 and 64.1; by a block and by a
-// warp a row 16384 of 1024 20.2 and 22.0, of 512 12.7 and 11.1, of 128 9.3 and 5.4.
+// 38.9, 8000 of 5120 48.5 and 49.2, 6000 of 8192 58.1 and 57.3, 5000 of 11008 79.8 and
+// 64.1; by a block and by a warp a row 16384 of 1024 20.2 and 22.0, of 512 12.7 and
+// 11.1, of 128 9.3 and 5.4.  (8192 of 4096: 38.0 with packed products, 6.2 TB/s; 46.7
+// with conversions before every product.)  Bound by memory, then by the barrier
+// between a row's two halves (0.61 of the issue rate).
 template <int BITS>
 int launch_norm(const NormArgs& a, const DeviceInfo* di, void* stream)
 {

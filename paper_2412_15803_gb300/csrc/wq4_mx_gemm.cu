@@ -12,6 +12,20 @@
 // lie in memory (256 K in a 128-byte row).  Scales come in the order in which
 // the tensor cores read them, 512 bytes for 128 rows by 128 K, and go from
 // shared memory to tensor memory by tcgen05.cp, in order with the MMAs.
+//
+// What bounds it, by the number of tokens:
+// - one to some: a slot's fixed cost, not its bytes.  A copy costs the thread that
+//   issues it ~100 cycles, a wait that is over ~110, the issuer's 128 K ~480 (wait,
+//   fence, 2 copies of scales, 4 MMAs, commit), a launch that follows another ~2.5 us
+//   from the previous kernel's end to the first MMA, sums over a cluster 1 us.  So few
+//   rows are shared by many CTAs (K split over a cluster, two CTAs an SM) and four
+//   warps issue copies.  6144 x 4096 over one token 5.5-5.9 us (floor 2.0 at the copy
+//   rate), 128256 x 4096 over one token in 4 bits 44.5 (0.93 of the copy rate).
+// - a prompt: the power limit.  28672 x 4096 over 2048 tokens in 8 bits 146-150 us
+//   (3.2 PFLOP/s) with the SMs at 1.66 GHz, 117 at 2.07 GHz when all codes are zero;
+//   over 8192 in 4 bits 281-285 (6.8 PFLOP/s; zeros 246).
+// Tried and slower: a warp of its own for the copies of scales to tensor memory
+// (6.25 -> 6.7 us), one lane's waits with a shuffle (7.35), test_wait for try_wait (6.6).
 #include "wq4.h"
 #include "wq4_device.cuh"
 #include "wq4_host.h"
@@ -27,8 +41,8 @@ namespace wq4 {
 namespace {
 
 // Warps: 0, 2, 3 and 12 the copies (in pairs of CTAs 0; 2 lets the next kernel
-// launch), 1 the MMA issuer, 4-11 the
-// epilogue (a warp reads the quarter of tensor memory that its number says).
+// launch), 1 the MMA issuer, 4-11 the epilogue (a warp reads the quarter of tensor
+// memory that its number says).
 constexpr int kThreads = 416, kPairThreads = 384;
 constexpr int kProd = 0, kIssuer = 1, kTrigger = 2, kScalesW = 2, kTokens = 3, kEpi = 4, kScalesX = 12;
 constexpr int kHeader = 1024;
@@ -139,8 +153,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     const uint32_t tbase = *tbase_sh, scol0 = tbase + 2 * tok;
 
     if (warp == kProd || warp == kScalesW || warp == kTokens || warp == kScalesX) {
-        // Four warps bring a slot's parts, a lane each: a copy costs its thread ~100
-        // cycles whatever its size, a wait as much.  (6144 x 4096, one token, K in
+        // Four warps bring a slot's parts, a lane each.  (6144 x 4096, one token, K in
         // halves: one warp 6.0 us, two 5.7, four 5.45.)
         if (lane == 0) {
             const bool w = warp == kProd || warp == kScalesW, codes = warp == kProd || warp == kTokens;
@@ -458,7 +471,11 @@ Plan pick(const DeviceInfo* di, int bits, int N, int M, int kblocks)
 // the tokens, 34 KB a slot where two CTAs of their own would take 50.
 // Tensor memory holds two accumulators that share kOver columns, and the scales
 // of each slot: the epilogue takes the shared columns first, and the other
-// accumulator's MMAs begin when it has them.
+// accumulator's MMAs begin when it has them.  (8192 tokens of 28672 x 4096 in 4 bits:
+// 492 us by CTAs of their own with 128 x 128 tiles, 319 in pairs, 311 with predicated
+// MMAs, 299 with the shared columns read first, 281 with a relaxed arrival.)  In the
+// steady state 128 K of 8-bit activations take 512 cycles, the MMA rate; 256 K of
+// 4-bit ones ~655, the 35 KB of a slot from L2.
 template <int BITS>
 struct PairCfg {
     static constexpr int T = 256;

@@ -1,9 +1,10 @@
 // wq4_tc.cuh -- tensor-core (tcgen05) and TMA tensor-copy building blocks
 // for sm_103a: tensor-memory allocation, register <-> tensor-memory moves,
 // the kind::f16 MMA with its A operand in tensor memory and B in shared
-// memory (128-byte swizzled, K-major), commits to mbarriers, and 2-D and
-// 3-D tensor copies.  All inline PTX: the GEMM uses all of it, the batched GEMV,
-// the stages and the attention the tensor copies.
+// memory (128-byte swizzled, K-major), the block-scaled MMAs with their scales,
+// in one CTA and in pairs, commits to mbarriers, and 2-D and 3-D tensor copies.
+// All inline PTX: the GEMMs use all of it, the batched GEMV, the stages and the
+// attention the tensor copies.
 #pragma once
 
 #include <cstdint>

@@ -232,6 +232,21 @@ def test_gemm_split(M, N, K, bits):
     check_any(M, N, K, bits)
 
 
+@pytest.mark.parametrize("M,N,K", [(3, 264, 256), (600, 9728, 256)])
+def test_gemm_into_odd_addresses(M, N, K):
+    """y two bytes behind a multiple of 16: no tensor copy can write it, and what lies around it stays."""
+    rng = np.random.default_rng(12)
+    W, ws = any_operand(rng, N, K, 4)
+    x, xs = any_operand(rng, M, K, 8)
+    xs -= 6
+    ref = gemm(W, ws, x, xs, M, N, K, 8)
+    buf = torch.full((M * N + 20,), 0x1234, dtype=torch.int16, device="cuda")
+    wq4.wq4_mx_gemm(dev(W), dev(mx.tiled(ws, K)), dev(x), dev(mx.tiled(xs, K)), buf[9:], N, K, M, 8)
+    torch.cuda.synchronize()
+    out = buf.cpu().numpy().view(np.uint16)
+    assert np.array_equal(out[9:9 + M * N].reshape(M, N), ref) and np.all(out[:9] == 0x1234) and np.all(out[9 + M * N:] == 0x1234)
+
+
 @pytest.mark.parametrize("bits", [8, 4])
 def test_gemm_over_drawn_sizes(bits):
     """Sizes spread by their logarithm over what the call is for."""
