@@ -19,11 +19,12 @@
 //   fence, 2 copies of scales, 4 MMAs, commit), a launch that follows another ~2.5 us
 //   from the previous kernel's end to the first MMA, sums over a cluster 1 us.  So few
 //   rows are shared by many CTAs (K split over a cluster, two CTAs an SM) and four
-//   warps issue copies.  6144 x 4096 over one token 5.5-5.9 us (floor 2.0 at the copy
-//   rate), 128256 x 4096 over one token in 4 bits 44.5 (0.93 of the copy rate).
+//   warps issue copies.  6144 x 4096 over one token 5.8 us (floor 2.0 at the copy
+//   rate), 4096 x 14336 over 16 tokens 9.1 (4.7), 128256 x 4096 over one token in 4
+//   bits 45 (41).
 // - a prompt: the power limit.  28672 x 4096 over 2048 tokens in 8 bits 146-150 us
 //   (3.2 PFLOP/s) with the SMs at 1.66 GHz, 117 at 2.07 GHz when all codes are zero;
-//   over 8192 in 4 bits 281-285 (6.8 PFLOP/s; zeros 246).
+//   over 8192 in 4 bits 281-287 (6.8 PFLOP/s; zeros 246).
 // Tried and slower: a warp of its own for the copies of scales to tensor memory
 // (6.25 -> 6.7 us), one lane's waits with a shuffle (7.35), test_wait for try_wait (6.6).
 #include "wq4.h"
@@ -61,6 +62,7 @@ struct Args {
     uint32_t* err;
     int stall;               // test hook: leaves the copies out
     int bulk;                // y's rows can be written by tensor copies
+    int prefetch;            // fetch weights into L2 early
 };
 
 // A ring position: slot and parity of the n-th use of a ring of S slots.
@@ -154,7 +156,7 @@ __global__ void __launch_bounds__(kThreads, 2)
 
     if (warp == kProd || warp == kScalesW || warp == kTokens || warp == kScalesX) {
         // Four warps bring a slot's parts, a lane each.  (6144 x 4096, one token, K in
-        // halves: one warp 6.0 us, two 5.7, four 5.45.)
+        // halves, weights copied early: one warp 6.0 us, two 5.7, four 5.45.)
         if (lane == 0) {
             const bool w = warp == kProd || warp == kScalesW, codes = warp == kProd || warp == kTokens;
             tc::prefetch_map(w ? &tm_w : &tm_x);
@@ -175,9 +177,9 @@ __global__ void __launch_bounds__(kThreads, 2)
                 else
                     tc::tma_load_2d(to + slot * a.slot_bytes, w ? &tm_w : &tm_x, k * 128, r0, bar);
             };
-            // The previous kernel may write the weights: the first tile's are fetched into
-            // L2 while it finishes and copied after it.
-            if (w && !a.stall && u0 < tiles) {
+            // The previous kernel may write the weights: a small matrix's are fetched into L2
+            // while it finishes and copied after it.
+            if (w && a.prefetch && u0 < tiles) {
                 const int r0 = u0 / a.ttiles * 128, ke = min(k1, k0 + 32);
                 if (!codes)
                     bulk_prefetch(sc + (static_cast<size_t>(r0 >> 7) * a.kblocks + k0 * NB) * 512, 512u * (min(ke * NB, a.kblocks) - k0 * NB));
@@ -405,26 +407,26 @@ constexpr int kHalfTok = 80;
 
 // What a form takes, in us, with t = tokens of a tile / 128 and f = the share of its
 // CTAs that are busy: a + at t, beside k0 + k0t t (alone) .. + k1 + k1t t more (f = 1)
-// a slot, w a round after the first; where s CTAs share a tile's K st t + sf f +
+// a slot, w a round after the first; where s CTAs share a tile's K s0 + st t + sf f +
 // stf t f + ss (s - 2); where an SM has two CTAs kd a slot and d more.
 struct Cost {
-    double a, at, k0, k0t, k1, k1t, w, st, sf, stf, ss, kd, d;
+    double a, at, k0, k0t, k1, k1t, w, s0, st, sf, stf, ss, kd, d;
 };
 
 // Fitted to 426 measurements (78 sizes of 1 to 4096 tokens, each form and split that
 // is possible, over copies of 400 MB), those near the best of a size above all: what
-// it picks takes 1.5 % more than the best on average, 15 % at most.  6144 x 4096 over
-// one token: whole 6.6 us, K in thirds 5.4; 4096 x 14336 over 16 tokens 17.0 whole,
-// 9.9 in sixths; 512 tokens of 6144 x 4096 17.6 in single CTAs, 14.0 in pairs.
+// it picks takes 1.1 % more than the best on average, 15 % at most.  6144 x 4096 over
+// one token: whole 6.9 us, K in halves 5.8; 4096 x 14336 over 16 tokens 17.0 whole,
+// 9.1 in quarters; 512 tokens of 6144 x 4096 18.3 in single CTAs, 14.3 in pairs.
 constexpr Cost kCost[2][3] = {
     // activations of 8 bits: two CTAs an SM, one, pairs
-    {{1.854, 0.916, 0.182, 0.136, 0.206, 0.131, 0.000, 1.897, 0.000, 2.660, 0.029, 0.022, 0.683},
-     {1.900, 0.633, 0.209, 0.172, 0.221, 0.026, 0.000, 2.317, 0.636, 2.287, 0.058, 0.000, 0.000},
-     {2.306, 1.440, 0.138, 0.052, 0.044, 0.003, 2.683, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000}},
+    {{1.873, 0.000, 0.175, 0.218, 0.166, 0.060, 0.000, 0.276, 1.115, 0.001, 5.904, 0.000, 0.000, 0.933},
+     {1.843, 1.192, 0.222, 0.151, 0.175, 0.037, 0.000, 0.000, 2.210, 0.779, 1.566, 0.041, 0.000, 0.000},
+     {2.454, 1.425, 0.096, 0.074, 0.034, 0.009, 2.787, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000}},
     // of 4 bits
-    {{1.776, 1.186, 0.184, 0.165, 0.385, 0.049, 2.436, 2.008, 0.000, 2.251, 0.063, 0.148, 0.434},
-     {1.813, 1.197, 0.224, 0.000, 0.144, 0.000, 0.095, 1.360, 1.000, 2.008, 0.036, 0.000, 0.000},
-     {2.365, 1.324, 0.101, 0.073, 0.037, 0.022, 3.658, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000}}};
+    {{2.159, 0.000, 0.159, 0.230, 0.516, 0.000, 0.156, 0.025, 0.433, 0.000, 5.838, 0.000, 0.000, 0.987},
+     {1.946, 1.114, 0.213, 0.000, 0.142, 0.000, 0.693, 0.000, 1.445, 0.886, 2.076, 0.023, 0.000, 0.000},
+     {1.823, 1.618, 0.103, 0.069, 0.042, 0.026, 3.449, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000}}};
 
 double estimate(const Cost& c, int tok, int slots, int64_t ctas, int cap, int s)
 {
@@ -433,9 +435,15 @@ double estimate(const Cost& c, int tok, int slots, int64_t ctas, int cap, int s)
     const int64_t full = ctas / cap, rest = ctas % cap;
     double us = c.a + c.at * t + n * (full * k1 + (rest ? k0 + (k1 - k0) * rest / cap : 0.0)) + c.w * (full - (rest ? 0 : 1));
     if (2 * ctas > cap) us += n * c.kd + c.d;
-    if (s > 1) us += c.st * t + c.sf * f + c.stf * t * f + c.ss * (s - 2);
+    if (s > 1) us += c.s0 + c.st * t + c.sf * f + c.stf * t * f + c.ss * (s - 2);
     return us;
 }
+
+// Up to this many weights a call fetches them into L2 while the previous kernel
+// finishes: 5003 x 2176 over 77 tokens 5.8 us where without it 6.3.  Larger ones take
+// bandwidth from that kernel and hold up their own copies (4096 x 14336 over 16 tokens
+// 10.2 us with and 9.1 without, a decoder layer of one token 46.0 and 42.2).
+constexpr int64_t kPrefetchWeights = 16 << 20;
 
 Plan pick(const DeviceInfo* di, int bits, int N, int M, int kblocks)
 {
@@ -752,6 +760,7 @@ extern "C" int wq4_mx_gemm(const uint8_t* W, const uint8_t* W_scales, const uint
     a.err = di->status;
     a.stall = test_copy_stall() == WQ4_STALL_MX ? 1 : 0;
     a.bulk = (N % 8) == 0 && aligned(y, 16) ? 1 : 0;
+    a.prefetch = !a.stall && static_cast<int64_t>(N) * K <= kPrefetchWeights ? 1 : 0;
     PairMaps tm;
     const uint64_t k = static_cast<uint64_t>(K), wrow = k / 2, xrow = k / 8 * bits, srow = k / 128 * 512;
     constexpr CUtensorMapDataType kBytes = CU_TENSOR_MAP_DATA_TYPE_UINT8, kWords = CU_TENSOR_MAP_DATA_TYPE_UINT32;

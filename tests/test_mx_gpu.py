@@ -383,6 +383,27 @@ def test_layer_back_to_back(late_copy, M, bits):  # noqa: F811
     assert wq4.wq4_device_status() == 0
 
 
+# forms whose blocks of one call and of the next are resident together, and the others
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("M,N,K", [(1, 6144, 4096), (16, 4096, 14336), (1, 20000, 512), (77, 5003, 2176), (1000, 9728, 512)])
+def test_products_back_to_back(M, N, K, bits):
+    rng = np.random.default_rng(13)
+    calls, want = [], []
+    for _ in range(3):
+        W, ws = any_operand(rng, N, K, 4)
+        x, xs = any_operand(rng, M, K, bits)
+        xs -= 6 if bits == 8 else 0
+        want.append(gemm(W, ws, x, xs, M, N, K, bits))
+        calls.append([dev(W), dev(mx.tiled(ws, K)), dev(x), dev(mx.tiled(xs, K)), torch.zeros((M, N), dtype=torch.int16, device="cuda"), N, K, M, bits])
+    for _ in range(20):
+        for c in calls:
+            wq4.wq4_mx_gemm(*c)
+    torch.cuda.synchronize()
+    for c, w in zip(calls, want):
+        assert np.array_equal(c[4].cpu().numpy().view(np.uint16), w)
+    assert wq4.wq4_device_status() == 0
+
+
 # one size of each form of the product: two blocks an SM, K split, one block an SM, pairs
 @pytest.mark.parametrize("M,N,K", [(1, 20000, 512), (1, 2048, 4096), (100, 2048, 1024), (1000, 9728, 512)])
 @pytest.mark.parametrize("bits", [8, 4])
