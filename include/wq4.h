@@ -155,9 +155,8 @@ int wq4_test_gemv_path(int path);
 enum wq4_stall {
     WQ4_STALL_NONE = 0,
     WQ4_STALL_GEMM_X = 1,     /* wq4_gemm (17 tokens and more): the activations */
-    WQ4_STALL_GEMM_W = 2,     /* ... : the weights and scales */
-    WQ4_STALL_ATTN = 3,       /* the attention calls of wq4_attn.h: the keys and values (and a prompt's queries) */
-    WQ4_STALL_MX = 4          /* wq4_mx_gemm: weights, activations and their scales */
+    WQ4_STALL_GEMM_W = 2,     /* ... : the weights and scales; wq4_mx_gemm: all it copies */
+    WQ4_STALL_ATTN = 3        /* the attention calls of wq4_attn.h: the keys and values (and a prompt's queries) */
 };
 int wq4_test_copy_stall(int stall);
 

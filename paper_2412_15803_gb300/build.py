@@ -23,7 +23,8 @@ LIB = os.path.join(BUILD, "libwq4.so")
 
 SOURCES = ["wq4_gemv.cu", "wq4_bgemv.cu", "wq4_chain.cu", "wq4_synth.cu", "wq4_stage.cu", "wq4_attn.cu", "wq4_gemm.cu",
            "wq4_prompt.cu", "wq4_pool.cu", "wq4_mx.cu", "wq4_mx_gemm.cu"]
-HEADERS = ["wq4_device.cuh", "wq4_host.h", "wq4_items.cuh", "wq4_tc.cuh", "wq4_stage_host.h", "wq4_tiles.cuh", "wq4_seen.h", "wq4_cache.h"]
+HEADERS = ["wq4_device.cuh", "wq4_host.h", "wq4_items.cuh", "wq4_tc.cuh", "wq4_stage_host.h", "wq4_tiles.cuh", "wq4_seen.h", "wq4_cache.h",
+           "wq4_mx.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

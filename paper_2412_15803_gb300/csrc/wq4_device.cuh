@@ -100,34 +100,6 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, uint32
     }
 }
 
-// mbar_wait for a barrier on which other CTAs of the cluster arrive, after writes
-// to this CTA's shared memory that the caller reads.
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_addr(bar)), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-
-__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, uint32_t* err)
-{
-    if (mbar_try_wait_cluster(bar, parity)) return true;
-    const uint64_t t0 = globaltimer_ns();
-    for (;;) {
-        if (mbar_try_wait_cluster(bar, parity)) return true;
-        if (globaltimer_ns() - t0 > kWaitTimeoutNs) {
-            atomicOr(err, kErrPipeTimeout);
-            return false;
-        }
-    }
-}
-
 // ------------------------------------------------------------ bulk copy --
 
 // L2 policy for data read exactly once per token (the weights): evict first,
@@ -149,12 +121,6 @@ __device__ __forceinline__ void bulk_g2s(void* dst, const void* src, uint32_t by
         " [%0], [%1], %2, [%3], %4;" ::"r"(smem_addr(dst)),
         "l"(src), "r"(bytes), "r"(smem_addr(bar)), "l"(policy)
         : "memory");
-}
-
-// Contiguous bytes into L2 only; src 16-byte aligned, bytes a multiple of 16.
-__device__ __forceinline__ void bulk_prefetch(const void* src, uint32_t bytes)
-{
-    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
 }
 
 // Programmatic dependent launch: wait for the previous grid of the stream

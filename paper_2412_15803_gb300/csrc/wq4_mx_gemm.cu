@@ -22,7 +22,7 @@
 //   warps issue copies.  6144 x 4096 over one token 5.8 us (floor 2.0 at the copy
 //   rate), 4096 x 14336 over 16 tokens 9.1 (4.7), 128256 x 4096 over one token in 4
 //   bits 45 (41).
-// - a prompt: the power limit.  28672 x 4096 over 2048 tokens in 8 bits 146-150 us
+// - a prompt: the power limit.  28672 x 4096 over 2048 tokens in 8 bits 146-153 us
 //   (3.2 PFLOP/s) with the SMs at 1.66 GHz, 117 at 2.07 GHz when all codes are zero;
 //   over 8192 in 4 bits 281-287 (6.8 PFLOP/s; zeros 246).
 // Tried and slower: a warp of its own for the copies of scales to tensor memory
@@ -30,6 +30,7 @@
 #include "wq4.h"
 #include "wq4_device.cuh"
 #include "wq4_host.h"
+#include "wq4_mx.cuh"
 #include "wq4_tc.cuh"
 
 #include <cuda.h>
@@ -758,7 +759,7 @@ extern "C" int wq4_mx_gemm(const uint8_t* W, const uint8_t* W_scales, const uint
     a.rtiles = (N - 1) / rows + 1;
     a.ttiles = (M - 1) / T + 1;
     a.err = di->status;
-    a.stall = test_copy_stall() == WQ4_STALL_MX ? 1 : 0;
+    a.stall = test_copy_stall() == WQ4_STALL_GEMM_W ? 1 : 0;
     a.bulk = (N % 8) == 0 && aligned(y, 16) ? 1 : 0;
     a.prefetch = !a.stall && static_cast<int64_t>(N) * K <= kPrefetchWeights ? 1 : 0;
     PairMaps tm;

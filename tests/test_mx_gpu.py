@@ -487,7 +487,7 @@ def test_gemm_without_its_copies_ends(M, N, K, bits):
     ref = args[4].clone()
     assert wq4.wq4_device_status() == 0
     try:
-        wq4.wq4_test_copy_stall(4)
+        wq4.wq4_test_copy_stall(2)
         t0 = time.perf_counter()
         wq4.wq4_mx_gemm(*args)
         torch.cuda.synchronize()
