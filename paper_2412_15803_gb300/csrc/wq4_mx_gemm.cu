@@ -367,6 +367,43 @@ int cluster_capacity(const DeviceInfo* di, int split, bool half)
     return n;
 }
 
+// Up to this many tokens two CTAs of an SM, by their tensor memory and shared memory.
+constexpr int kHalfTok = 80;
+
+template <int BITS, int BOXES>
+constexpr int slot_bytes(int tok)
+{
+    return (Cfg<BITS, BOXES>::kW + BOXES * tok * 128 + 2 * Cfg<BITS, BOXES>::kScales + 1023) / 1024 * 1024;
+}
+
+// Behind the header and the cluster's sums: of groups of four tokens by 128 rows, a
+// CTA's share from each.
+constexpr int ring_at(int tok, int split)
+{
+    return kHeader + (split > 1 ? (tok / 4 + split - 1) / split * split * 128 * 16 : 0);
+}
+
+template <int BITS, int BOXES>
+constexpr int ring_slots(int tok, int split, bool half)
+{
+    const int n = ((half ? kHalf : kWhole) - ring_at(tok, split)) / slot_bytes<BITS, BOXES>(tok);
+    return n < Cfg<BITS, BOXES>::kMaxSlots ? n : Cfg<BITS, BOXES>::kMaxSlots;
+}
+
+// Every tile and split has two slots at least, and its accumulators and scales lie in
+// its tensor memory.  (Slots of two boxes are those of one CTA an SM.)
+template <int BITS, int BOXES>
+constexpr bool fits()
+{
+    for (int tok = 16; tok <= 128; tok += 16)
+        for (int split = 1; split <= 8; ++split)
+            for (int half = 0; half <= (BOXES == 1 && tok <= kHalfTok ? 1 : 0); ++half) {
+                const int n = ring_slots<BITS, BOXES>(tok, split, half != 0);
+                if (n < 2 || 2 * tok + n * Cfg<BITS, BOXES>::kScaleCols > kTmemCols / (half ? 2 : 1)) return false;
+            }
+    return true;
+}
+
 struct Plan {
     int tok, split;
     bool half, pair;
@@ -378,14 +415,14 @@ int launch(const DeviceInfo* di, const CUtensorMap& w, const CUtensorMap& x, Arg
     using C = Cfg<BITS, BOXES>;
     if (!set_attributes<BITS, BOXES>(di)) return WQ4_ERR_CUDA;
     const int64_t tiles = static_cast<int64_t>(a.rtiles) * a.ttiles;
+    constexpr bool kFits = fits<BITS, BOXES>();
+    static_assert(kFits, "rings of two slots and more, tensor memory");
+    const int smem = pl.half ? kHalf : kWhole;
     a.tok = pl.tok;
     a.split = pl.split;
-    a.slot_bytes = static_cast<int>(align_up(C::kW + BOXES * a.tok * 128 + 2 * C::kScales, 1024));
-    // sums: of groups of four tokens by 128 rows, a CTA's share from each
-    const int sums = a.split > 1 ? (a.tok / 4 + a.split - 1) / a.split * a.split * 128 * 16 : 0;
-    a.ring = kHeader + sums;
-    const int smem = pl.half ? kHalf : kWhole;
-    a.nslots = std::min((smem - a.ring) / a.slot_bytes, C::kMaxSlots);
+    a.slot_bytes = slot_bytes<BITS, BOXES>(pl.tok);
+    a.ring = ring_at(pl.tok, pl.split);
+    a.nslots = ring_slots<BITS, BOXES>(pl.tok, pl.split, pl.half);
     a.tmem_cols = pl.half ? kTmemCols / 2 : kTmemCols;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -402,9 +439,6 @@ int launch(const DeviceInfo* di, const CUtensorMap& w, const CUtensorMap& x, Arg
     cfg.numAttrs = a.split > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, mx_gemm_kernel<BITS, BOXES>, w, x, a) == cudaSuccess ? WQ4_OK : WQ4_ERR_CUDA;
 }
-
-// Up to this many tokens two CTAs of an SM, by their tensor memory and shared memory.
-constexpr int kHalfTok = 80;
 
 // What a form takes, in us, with t = tokens of a tile / 128 and f = the share of its
 // CTAs that are busy: a + at t, beside k0 + k0t t (alone) .. + k1 + k1t t more (f = 1)
