@@ -442,33 +442,38 @@ int launch(const DeviceInfo* di, const CUtensorMap& w, const CUtensorMap& x, Arg
 
 // What a form takes, in us, with t = tokens of a tile / 128 and f = the share of its
 // CTAs that are busy: a + at t, beside k0 + k0t t (alone) .. + k1 + k1t t more (f = 1)
-// a slot, w a round after the first; where s CTAs share a tile's K s0 + st t + sf f +
+// a slot; each round after the first waits for w, or for as long as the round
+// before writes (e t, for rows that 16 bytes do not divide eo t) past its own slots;
+// such rows o t at the end; where s CTAs share a tile's K s0 + st t + sf f +
 // stf t f + ss (s - 2); where an SM has two CTAs kd a slot and d more.
 struct Cost {
-    double a, at, k0, k0t, k1, k1t, w, s0, st, sf, stf, ss, kd, d;
+    double a, at, k0, k0t, k1, k1t, w, e, eo, o, s0, st, sf, stf, ss, kd, d;
 };
 
-// Fitted to 426 measurements (78 sizes of 1 to 4096 tokens, each form and split that
+// Fitted to 806 measurements (194 sizes of 1 to 8192 tokens, each form and split that
 // is possible, over copies of 400 MB), those near the best of a size above all: what
-// it picks takes 1.1 % more than the best on average, 15 % at most.  6144 x 4096 over
+// it picks takes 0.6 % more than the best on average, 16 % at most.  6144 x 4096 over
 // one token: whole 6.9 us, K in halves 5.8; 4096 x 14336 over 16 tokens 17.0 whole,
-// 9.1 in quarters; 512 tokens of 6144 x 4096 18.3 in single CTAs, 14.3 in pairs.
+// 9.1 in quarters; 512 tokens of 6144 x 4096 18.3 in single CTAs, 14.3 in pairs.  Over
+// a short K the writing decides: 16384 x 512 over 4000 tokens 46.5 in single CTAs,
+// 35.6 in pairs; of 16385 rows 53.8 and 69.8.
 constexpr Cost kCost[2][3] = {
     // activations of 8 bits: two CTAs an SM, one, pairs
-    {{1.873, 0.000, 0.175, 0.218, 0.166, 0.060, 0.000, 0.276, 1.115, 0.001, 5.904, 0.000, 0.000, 0.933},
-     {1.843, 1.192, 0.222, 0.151, 0.175, 0.037, 0.000, 0.000, 2.210, 0.779, 1.566, 0.041, 0.000, 0.000},
-     {2.454, 1.425, 0.096, 0.074, 0.034, 0.009, 2.787, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000}},
+    {{1.873, 0.000, 0.175, 0.218, 0.166, 0.060, 0.000, 1.798, 1.859, 0.110, 0.276, 1.115, 0.001, 5.904, 0.000, 0.000, 0.933},
+     {1.843, 1.192, 0.222, 0.151, 0.175, 0.037, 0.000, 1.798, 1.859, 0.110, 0.000, 2.210, 0.779, 1.566, 0.041, 0.000, 0.000},
+     {2.084, 1.530, 0.107, 0.069, 0.038, 0.015, 0.698, 1.132, 2.384, 1.784, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000}},
     // of 4 bits
-    {{2.159, 0.000, 0.159, 0.230, 0.516, 0.000, 0.156, 0.025, 0.433, 0.000, 5.838, 0.000, 0.000, 0.987},
-     {1.946, 1.114, 0.213, 0.000, 0.142, 0.000, 0.693, 0.000, 1.445, 0.886, 2.076, 0.023, 0.000, 0.000},
-     {1.823, 1.618, 0.103, 0.069, 0.042, 0.026, 3.449, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000}}};
+    {{2.159, 0.000, 0.159, 0.230, 0.516, 0.000, 0.156, 1.921, 1.921, 0.126, 0.025, 0.433, 0.000, 5.838, 0.000, 0.000, 0.987},
+     {1.946, 1.114, 0.213, 0.000, 0.142, 0.000, 0.693, 1.921, 1.921, 0.126, 0.000, 1.445, 0.886, 2.076, 0.023, 0.000, 0.000},
+     {2.675, 1.212, 0.126, 0.055, 0.074, 0.018, 0.832, 0.902, 2.464, 1.859, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000}}};
 
-double estimate(const Cost& c, int tok, int slots, int64_t ctas, int cap, int s)
+double estimate(const Cost& c, int tok, int slots, int64_t ctas, int cap, int s, bool whole_rows)
 {
     const double t = tok / 128.0, f = std::min(1.0, static_cast<double>(ctas) / cap), n = (slots + s - 1) / s;
     const double k0 = c.k0 + c.k0t * t, k1 = k0 + c.k1 + c.k1t * t;
-    const int64_t full = ctas / cap, rest = ctas % cap;
-    double us = c.a + c.at * t + n * (full * k1 + (rest ? k0 + (k1 - k0) * rest / cap : 0.0)) + c.w * (full - (rest ? 0 : 1));
+    const int64_t full = ctas / cap, rest = ctas % cap, more = std::max<int64_t>(0, full - (rest ? 0 : 1));
+    double us = c.a + c.at * t + n * (full * k1 + (rest ? k0 + (k1 - k0) * rest / cap : 0.0));
+    us += more * std::max(c.w, (whole_rows ? c.e : c.eo) * t - n * k1) + (whole_rows ? 0.0 : c.o * t);
     if (2 * ctas > cap) us += n * c.kd + c.d;
     if (s > 1) us += c.s0 + c.st * t + c.sf * f + c.stf * t * f + c.ss * (s - 2);
     return us;
@@ -495,13 +500,13 @@ Plan pick(const DeviceInfo* di, int bits, int N, int M, int kblocks)
                             : half      ? cluster_capacity<8, 1>(di, s, true)
                                         : cluster_capacity<8, 2>(di, s, false);
             if (s > 1 && tiles > fit) continue;
-            const double us = estimate(kCost[bits == 4][half ? 0 : 1], tok, slots, tiles * s, di->sm_count * (half ? 2 : 1), s);
+            const double us = estimate(kCost[bits == 4][half ? 0 : 1], tok, slots, tiles * s, di->sm_count * (half ? 2 : 1), s, N % 8 == 0);
             if (us < best) best = us, pl.split = s, pl.half = half != 0;
         }
     }
     if (M > 64) {
         const int64_t pairs = (static_cast<int64_t>(N) + 255) / 256 * ((static_cast<int64_t>(M) + 255) / 256);
-        if (estimate(kCost[bits == 4][2], 256, bits == 8 ? kblocks : (kblocks + 1) / 2, pairs, di->sm_count / 2, 1) < best)
+        if (estimate(kCost[bits == 4][2], 256, bits == 8 ? kblocks : (kblocks + 1) / 2, pairs, di->sm_count / 2, 1, N % 8 == 0) < best)
             pl = {256, 1, false, true};
     }
     return pl;
