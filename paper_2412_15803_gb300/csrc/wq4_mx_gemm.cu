@@ -450,9 +450,9 @@ struct Cost {
     double a, at, k0, k0t, k1, k1t, w, e, eo, o, s0, st, sf, stf, ss, kd, d;
 };
 
-// Fitted to 806 measurements (194 sizes of 1 to 8192 tokens, each form and split that
+// Fitted to 854 measurements (218 sizes of 1 to 8192 tokens, each form and split that
 // is possible, over copies of 400 MB), those near the best of a size above all: what
-// it picks takes 0.6 % more than the best on average, 16 % at most.  6144 x 4096 over
+// it picks takes 0.5 % more than the best on average, 16 % at most.  6144 x 4096 over
 // one token: whole 6.9 us, K in halves 5.8; 4096 x 14336 over 16 tokens 17.0 whole,
 // 9.1 in quarters; 512 tokens of 6144 x 4096 18.3 in single CTAs, 14.3 in pairs.  Over
 // a short K the writing decides: 16384 x 512 over 4000 tokens 46.5 in single CTAs,
@@ -460,7 +460,7 @@ struct Cost {
 constexpr Cost kCost[2][3] = {
     // activations of 8 bits: two CTAs an SM, one, pairs
     {{1.873, 0.000, 0.175, 0.218, 0.166, 0.060, 0.000, 1.798, 1.859, 0.110, 0.276, 1.115, 0.001, 5.904, 0.000, 0.000, 0.933},
-     {1.843, 1.192, 0.222, 0.151, 0.175, 0.037, 0.000, 1.798, 1.859, 0.110, 0.000, 2.210, 0.779, 1.566, 0.041, 0.000, 0.000},
+     {1.843, 1.192, 0.222, 0.151, 0.160, 0.052, 0.000, 1.798, 1.859, 0.110, 0.000, 2.210, 0.779, 1.566, 0.041, 0.000, 0.000},
      {2.084, 1.530, 0.107, 0.069, 0.038, 0.015, 0.698, 1.132, 2.384, 1.784, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000, 0.000}},
     // of 4 bits
     {{2.159, 0.000, 0.159, 0.230, 0.516, 0.000, 0.156, 1.921, 1.921, 0.126, 0.025, 0.433, 0.000, 5.838, 0.000, 0.000, 0.987},
