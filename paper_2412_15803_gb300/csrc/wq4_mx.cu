@@ -9,6 +9,11 @@
 // 16-byte load is coalesced over a warp and the four scale bytes of 128
 // columns, which lie side by side in the layout that the tensor cores read,
 // leave as one word of 16 lanes.
+//
+// No load goes through the read-only path, and no pointer says that it has no
+// aliases: the kernel before, which a launch here may overlap, may still be writing
+// what is read after the wait for it, and nothing keeps a load of memory that is said
+// not to change behind that wait.
 #include "wq4.h"
 #include "wq4_device.cuh"
 #include "wq4_host.h"
@@ -62,6 +67,14 @@ __device__ __forceinline__ uint4 to_halves(const float2 v[4])
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Sixteen bytes, in the order of the program.
+__device__ __forceinline__ uint4 load16(const uint16_t* p)
+{
+    uint4 v;
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+
 // Where the scales of row r's columns [128 kb, 128 kb + 128) lie.
 __device__ __forceinline__ size_t scale_word(int r, int kb, int K)
 {
@@ -88,7 +101,7 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t mb)
 
 // Codes of columns [8 c, 8 c + 8) of row r, zeros where the group's scale is NaN.
 template <int BITS>
-__device__ __forceinline__ void put_codes(uint2 o, uint32_t byte, uint8_t* __restrict__ codes, int r, int c, int K, bool live)
+__device__ __forceinline__ void put_codes(uint2 o, uint32_t byte, uint8_t* codes, int r, int c, int K, bool live)
 {
     if (byte == 255u) o = make_uint2(0, 0);
     if (!live) return;
@@ -112,7 +125,7 @@ __device__ __forceinline__ uint32_t scale_bytes_of(uint32_t byte, int c)
 // r, and the word of scales of its 128 columns; all lanes of a warp, 16 in turn
 // with 16 consecutive c.  Lanes without `live` store nothing.
 template <int BITS>
-__device__ __forceinline__ uint32_t store_codes(const float2 v[4], uint8_t* __restrict__ codes, int r, int c, int K, bool live)
+__device__ __forceinline__ uint32_t store_codes(const float2 v[4], uint8_t* codes, int r, int c, int K, bool live)
 {
     float m = max_abs(max_abs(v[0].x, v[0].y, v[1].x), max_abs(v[1].y, v[2].x, v[2].y), max_abs(v[3].x, v[3].y, 0.f));
     m = max_abs(m, __shfl_xor_sync(kAll, m, 1), 0.f);
@@ -147,7 +160,7 @@ __device__ __forceinline__ uint32_t store_codes(const float2 v[4], uint8_t* __re
 // values are scaled in fp16: exactly, but for those that become smaller than 2^-14,
 // whose codes are 0 either way.
 template <int BITS>
-__device__ __forceinline__ uint32_t store_codes(uint4 x, uint8_t* __restrict__ codes, int r, int c, int K, bool live)
+__device__ __forceinline__ uint32_t store_codes(uint4 x, uint8_t* codes, int r, int c, int K, bool live)
 {
     auto max2 = [](uint32_t a, uint32_t b) {
         uint32_t d;
@@ -189,7 +202,7 @@ __device__ __forceinline__ uint32_t store_codes(uint4 x, uint8_t* __restrict__ c
     return store_codes<BITS>(v, codes, r, c, K, live);
 }
 
-__device__ __forceinline__ void store_scales(uint32_t w, uint8_t* __restrict__ scales, int r, int c, int K, bool live)
+__device__ __forceinline__ void store_scales(uint32_t w, uint8_t* scales, int r, int c, int K, bool live)
 {
     if (live && (c & 15) == 0) *reinterpret_cast<uint32_t*>(scales + scale_word(r, c >> 4, K)) = w;
 }
@@ -238,45 +251,57 @@ __device__ __forceinline__ Place place(int M, int chunks)
 }
 
 // Rows without a sum over them: quantize, and silu(gate) * up.  Bound by memory:
-// 4096 rows of 14336 silu in 45.2 us (6.5 TB/s) in 8 bits and 41.6 in 4, quantize in
-// 25.5 in 4 bits (5.8 TB/s).  Before two values an instruction they were bound by
-// issue (49.1, 43.7 and 26.0 at 0.72 of it).  Four rows' loads of each thread are in
-// flight (two, then: 52.5, 48.7 and 30.4), in blocks of 128 threads but for silu in 8
-// bits (256: 42.5 and 25.8 in 4 bits; silu in 8 bits with 128 50.9).
+// 4096 rows of 14336 silu in 44.0 us (6.7 TB/s) in 8 bits and 40.6 in 4, quantize in
+// 25.6 in 4 bits (5.8 TB/s).  Before two values an instruction they were bound by
+// issue (49.1, 43.7 and 26.0 at 0.72 of it).  Four rows a thread (two, then: 52.5, 48.7
+// and 30.4), in blocks of 128 threads but for silu in 8 bits (256: 42.5 and 25.8 in 4
+// bits, then; silu in 8 bits with 128 50.9).  Quantize has all four rows' loads in
+// flight, silu two rows': the next one's loads go out behind a row's stores (all four
+// 47.8 and 44.6, three 44.6 and 42.6; loads that the compiler may move 44.1 and 44.0).
 template <int BITS, bool SILU>
 constexpr int kRowThreads = BITS == 8 && SILU ? 256 : 128;
 
+template <int BITS, int R>
+__device__ __forceinline__ void silu_rows(const Place& p, const uint16_t* x, int stride, uint8_t* codes, int M, int K, uint32_t w[R])
+{
+    uint4 a[R], b[R];
+    auto load = [&](int q) {          // behind the last row, that one again
+        const uint16_t* row = x + static_cast<size_t>(min(p.r + 32 * q, M - 1)) * stride + 8 * p.c;
+        a[q] = load16(row);
+        b[q] = load16(row + K);
+    };
+#pragma unroll
+    for (int q = 0; q < min(R, 2); ++q) load(q);
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+        float2 v[4], u[4];
+        to_floats(a[q], v);
+        to_floats(b[q], u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = silu_times(v[i], u[i]);
+        w[q] = store_codes<BITS>(v, codes, p.r + 32 * q, p.c, K, p.live && p.r + 32 * q < M);
+        if (q + 2 < R) load(q + 2);
+    }
+}
+
 template <int BITS, bool SILU, int R>
-__global__ void __launch_bounds__(kRowThreads<BITS, SILU>) rows_kernel(const uint16_t* __restrict__ x, int stride, uint8_t* __restrict__ codes,
-                                                   uint8_t* __restrict__ scales, int M, int K)
+__global__ void __launch_bounds__(kRowThreads<BITS, SILU>) rows_kernel(const uint16_t* x, int stride, uint8_t* codes, uint8_t* scales, int M, int K)
 {
     grid_dependency_wait();
     grid_dependents_launch();
     const Place p = place<R>(M, K >> 3);
-    uint4 a[R], b[R];
-#pragma unroll
-    for (int q = 0; q < R; ++q) {
-        a[q] = b[q] = make_uint4(0, 0, 0, 0);
-        if (p.live && p.r + 32 * q < M) {
-            const uint16_t* row = x + static_cast<size_t>(p.r + 32 * q) * stride + 8 * p.c;
-            a[q] = __ldg(reinterpret_cast<const uint4*>(row));
-            if (SILU) b[q] = __ldg(reinterpret_cast<const uint4*>(row + K));
-        }
-    }
     uint32_t w[R];
+    if constexpr (SILU) {
+        silu_rows<BITS, R>(p, x, stride, codes, M, K, w);
+    } else {
+        uint4 a[R];
 #pragma unroll
-    for (int q = 0; q < R; ++q) {
-        const bool live = p.live && p.r + 32 * q < M;
-        if constexpr (SILU) {
-            float2 v[4], u[4];
-            to_floats(a[q], v);
-            to_floats(b[q], u);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = silu_times(v[i], u[i]);
-            w[q] = store_codes<BITS>(v, codes, p.r + 32 * q, p.c, K, live);
-        } else {
-            w[q] = store_codes<BITS>(a[q], codes, p.r + 32 * q, p.c, K, live);
+        for (int q = 0; q < R; ++q) {
+            a[q] = make_uint4(0, 0, 0, 0);
+            if (p.live && p.r + 32 * q < M) a[q] = load16(x + static_cast<size_t>(p.r + 32 * q) * stride + 8 * p.c);
         }
+#pragma unroll
+        for (int q = 0; q < R; ++q) w[q] = store_codes<BITS>(a[q], codes, p.r + 32 * q, p.c, K, p.live && p.r + 32 * q < M);
     }
     if (R == 4 && p.r + 96 < M) {
         if (p.live && (p.c & 15) == 0)
@@ -508,8 +533,8 @@ __global__ void __launch_bounds__(512) norm_ring_kernel(const NormArgs a, const 
 }
 
 template <int BITS, int R>
-__global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
-                                                         uint16_t* __restrict__ y, int stride, int M, int K)
+__global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* codes, const uint8_t* scales,
+                                                         uint16_t* y, int stride, int M, int K)
 {
     grid_dependency_wait();
     grid_dependents_launch();
@@ -522,9 +547,9 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restri
         const int r = min(p.r + 32 * q, M - 1);
         sb[q] = scales[scale_word(r, p.c >> 4, K) + ((p.c >> 2) & 3)];
         if constexpr (BITS == 8)
-            code[q] = __ldcs(reinterpret_cast<const uint2*>(codes + static_cast<size_t>(r) * K + 8 * p.c));
+            code[q] = *reinterpret_cast<const uint2*>(codes + static_cast<size_t>(r) * K + 8 * p.c);
         else
-            code[q].x = __ldcs(reinterpret_cast<const uint32_t*>(codes + static_cast<size_t>(r) * (K >> 1) + 4 * p.c));
+            code[q].x = *reinterpret_cast<const uint32_t*>(codes + static_cast<size_t>(r) * (K >> 1) + 4 * p.c);
     }
 #pragma unroll
     for (int q = 0; q < R; ++q) {
