@@ -619,6 +619,13 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_gemm_pair_kernel(const __g
             // every copy issued, the other CTA's too, has landed before the memory goes away
             if (rank == 0)
                 for (int i = max(0, n - S); i < n; ++i) mbar_wait(&full[i % S], (i / S) & 1, err);
+            // and so has every arrival on this CTA's barriers by the commits of the pair's
+            // MMAs (those on dfull the epilogue has waited for): that CTA 0 has them on its
+            // own says nothing of CTA 1's.  Where the waits before gave up, the issuer's
+            // may only be giving up now: drain has twice the time.
+            if (ok)
+                for (int i = max(0, n - S); i < n; ++i) mbar_wait(&empty[i % S], (i / S) & 1, err);
+            if (!mbar_wait(drain, 0, err)) mbar_wait(drain, 0, err);
         }
     } else if (warp == kIssuer) {
         if (rank == 0) {
