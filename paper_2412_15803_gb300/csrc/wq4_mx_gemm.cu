@@ -341,12 +341,11 @@ bool set_attributes(const DeviceInfo* di)
     return true;
 }
 
-// Clusters of `split` CTAs that fit the device at once (cached per device).
+// Clusters of `split` CTAs, two or more, that fit the device at once (cached per device).
 template <int BITS, int BOXES>
 int cluster_capacity(const DeviceInfo* di, int split, bool half)
 {
     static std::atomic<int> cached[kMaxDevices][9][2];
-    if (split == 1) return half ? 2 * di->sm_count : di->sm_count;
     if (const int n = cached[di->dev][split][half].load()) return n;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -485,7 +484,8 @@ double estimate(const Cost& c, int tok, int slots, int64_t ctas, int cap, int s,
 // 10.2 us with and 9.1 without, a decoder layer of one token 46.0 and 42.2).
 constexpr int64_t kPrefetchWeights = 16 << 20;
 
-Plan pick(const DeviceInfo* di, int bits, int N, int M, int kblocks)
+// whole_rows: 16 bytes divide y's address and rows.
+Plan pick(const DeviceInfo* di, int bits, int N, int M, int kblocks, bool whole_rows)
 {
     const int tok = M > 112 ? 128 : (M + 15) / 16 * 16;
     const int64_t tiles = (static_cast<int64_t>(N) + 127) / 128 * ((static_cast<int64_t>(M) + tok - 1) / tok);
@@ -500,13 +500,13 @@ Plan pick(const DeviceInfo* di, int bits, int N, int M, int kblocks)
                             : half      ? cluster_capacity<8, 1>(di, s, true)
                                         : cluster_capacity<8, 2>(di, s, false);
             if (s > 1 && tiles > fit) continue;
-            const double us = estimate(kCost[bits == 4][half ? 0 : 1], tok, slots, tiles * s, di->sm_count * (half ? 2 : 1), s, N % 8 == 0);
+            const double us = estimate(kCost[bits == 4][half ? 0 : 1], tok, slots, tiles * s, di->sm_count * (half ? 2 : 1), s, whole_rows);
             if (us < best) best = us, pl.split = s, pl.half = half != 0;
         }
     }
     if (M > 64) {
         const int64_t pairs = (static_cast<int64_t>(N) + 255) / 256 * ((static_cast<int64_t>(M) + 255) / 256);
-        if (estimate(kCost[bits == 4][2], 256, bits == 8 ? kblocks : (kblocks + 1) / 2, pairs, di->sm_count / 2, 1, N % 8 == 0) < best)
+        if (estimate(kCost[bits == 4][2], 256, bits == 8 ? kblocks : (kblocks + 1) / 2, pairs, di->sm_count / 2, 1, whole_rows) < best)
             pl = {256, 1, false, true};
     }
     return pl;
@@ -792,7 +792,8 @@ extern "C" int wq4_mx_gemm(const uint8_t* W, const uint8_t* W_scales, const uint
     if ((static_cast<int64_t>(N - 1) / 128 + 1) * (static_cast<int64_t>(M - 1) / 128 + 1) > (static_cast<int64_t>(1) << 30)) return WQ4_ERR_UNSUPPORTED;
     const DeviceInfo* di = current_device_info(nullptr);
     if (!di) return WQ4_ERR_CUDA;
-    const Plan pl = pick(di, bits, N, M, K / 128);
+    const bool bulk = (N % 8) == 0 && aligned(y, 16);
+    const Plan pl = pick(di, bits, N, M, K / 128, bulk);
     const bool pair = pl.pair;
     const int T = pl.tok, rows = pair ? 256 : 128;
     Args a = {};
@@ -806,7 +807,7 @@ extern "C" int wq4_mx_gemm(const uint8_t* W, const uint8_t* W_scales, const uint
     a.ttiles = (M - 1) / T + 1;
     a.err = di->status;
     a.stall = test_copy_stall() == WQ4_STALL_GEMM_W ? 1 : 0;
-    a.bulk = (N % 8) == 0 && aligned(y, 16) ? 1 : 0;
+    a.bulk = bulk ? 1 : 0;
     a.prefetch = !a.stall && static_cast<int64_t>(N) * K <= kPrefetchWeights ? 1 : 0;
     PairMaps tm;
     const uint64_t k = static_cast<uint64_t>(K), wrow = k / 2, xrow = k / 8 * bits, srow = k / 128 * 512;

@@ -1,0 +1,45 @@
+"""Which form of the microscaled product a call takes, and how the norm's launches fill the SMs.
+
+Run without a GPU over a stand-in for the CUDA runtime (fake_cudart.c), which tells the kernel,
+the grid and the shared memory of the last launch.
+"""
+import os
+import subprocess
+import sys
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+HEAD = r"""
+import ctypes, sys
+fake = ctypes.CDLL(sys.argv[1])
+fake.fake_last_shape.restype = ctypes.c_size_t
+from paper_2412_15803_gb300 import wq4
+L = wq4.load(build_if_missing=False)
+A = 1 << 40
+
+def product(M, N, K, bits, off=0):
+    '(kernel, grid, shared memory)'
+    assert L.wq4_mx_gemm(A, 4 * A, 8 * A, 16 * A, 32 * A + off, N, K, M, bits, None) == 0
+    s = fake.fake_last_shape()
+    return fake.fake_last_kernel(), s >> 32, s & 0xffffffff
+"""
+
+
+def run(fake_cudart, child):
+    env = dict(os.environ, LD_PRELOAD=fake_cudart, PYTHONPATH=os.path.dirname(HERE))
+    r = subprocess.run([sys.executable, "-c", HEAD + child, fake_cudart], env=env, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+
+
+def test_rows_that_tensor_copies_cannot_write_by_address(fake_cudart):
+    """y off a multiple of 16 bytes costs what rows that 16 bytes do not divide cost: the same form for both."""
+    run(fake_cudart, r"""
+other = 0
+for bits in (8, 4):
+    for M, N, K in ((4000, 16384, 512), (600, 9728, 256), (2048, 28672, 4096), (730, 71064, 256), (1500, 10000, 128), (3, 264, 256),
+                    (300, 30000, 384), (8192, 28672, 4096)):
+        odd = product(M, N - 1, K, bits)[0]
+        assert product(M, N, K, bits, 2)[0] == product(M, N, K, bits, 8)[0] == odd, (bits, M, N, K)
+        other += product(M, N, K, bits)[0] != odd
+assert other >= 3       # sizes where it decides
+""")
