@@ -3,11 +3,13 @@
 The writer lets its dependents launch at its start and writes late; before it the buffers
 hold something else, so that a call which reads before the writer is through shows.
 """
+import numpy as np
 import pytest
 import torch
 
 from paper_2412_15803_gb300 import wq4
 from test_dependent_launch_gpu import late_copy  # noqa: F401  (a fixture)
+from test_mx_gpu import Layer, same
 
 pytestmark = pytest.mark.gpu
 
@@ -74,3 +76,23 @@ def test_norm(late_copy, M, K, bits):  # noqa: F811
     x, r, g, (c, s) = rows(M, K, 4), rows(M, K, 5), rows(1, K, 6), held(M, K, bits)
     h = torch.zeros((M, K), dtype=torch.int16, device="cuda")
     check_late(late_copy, [x, r, g], [h, c, s], lambda: wq4.wq4_mx_norm(x, K, r, K, g, 1e-5, h, K, c, s, M, K, bits))
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("M", [1, 40, 600])
+def test_layer_back_to_back_into_cleared_buffers(late_copy, M, bits):  # noqa: F811
+    """Nothing of the run before is left for a call that reads too early."""
+    L = Layer(M, bits, 4, H=1024, F=2048, nq=1536)
+    L.run(sync=True)
+    want = L.state()
+    for _ in range(4):
+        L.reset()
+        for t in (L.qkv, L.o, L.gu, L.y, *(t for p in L.held for t in p)):
+            t.zero_()
+        src = L.x.clone()
+        L.x.zero_()
+        torch.cuda.synchronize()
+        late_copy(L.x, src, 100_000)
+        L.run()
+        assert same(L.state(), want)
+    assert all(np.any(t.cpu().numpy()) for t in want)
+    assert wq4.wq4_device_status() == 0
