@@ -160,6 +160,17 @@ enum wq4_stall {
 };
 int wq4_test_copy_stall(int stall);
 
+/*
+ * Test hook: which form wq4_mx_gemm takes, for every later call in this process
+ * (no counterpart in the paper).  0 (the default) picks by an estimate of each
+ * form's time; 1 two blocks an SM (up to 80 tokens), 2 one, 3 pairs of blocks;
+ * with 1 and 2, `split` blocks share a tile's K (1 to 8; 0: by the estimate).  A
+ * call that the form does not take (more tokens, or a K of fewer slots) returns
+ * WQ4_ERR_UNSUPPORTED.  Results agree within
+ * the tolerance.  WQ4_ERR_INVALID for other values.
+ */
+int wq4_test_mx_form(int form, int split);
+
 /* Static, human-readable text of a status code. */
 const char* wq4_status_string(int status);
 

@@ -484,27 +484,35 @@ double estimate(const Cost& c, int tok, int slots, int64_t ctas, int cap, int s,
 // 10.2 us with and 9.1 without, a decoder layer of one token 46.0 and 42.2).
 constexpr int64_t kPrefetchWeights = 16 << 20;
 
-// whole_rows: 16 bytes divide y's address and rows.
+// The form that calls take (wq4_test_mx_form): 0 the estimate's choice, 1 two CTAs an
+// SM, 2 one, 3 pairs, and times 16 the CTAs that share a tile's K (0: the estimate's).
+std::atomic<int> g_form{0};
+
+// whole_rows: 16 bytes divide y's address and rows.  A split of 0: the form that a test
+// has set does not take the call.
 Plan pick(const DeviceInfo* di, int bits, int N, int M, int kblocks, bool whole_rows)
 {
     const int tok = M > 112 ? 128 : (M + 15) / 16 * 16;
     const int64_t tiles = (static_cast<int64_t>(N) + 127) / 128 * ((static_cast<int64_t>(M) + tok - 1) / tok);
-    Plan pl = {tok, 1, false, false};
+    const int set = g_form.load(), form = set % 16, cut = set / 16;
+    Plan pl = {tok, 0, false, false};
     double best = 1e300;
     for (int half = tok <= kHalfTok ? 1 : 0; half >= 0; --half) {
+        if (form && form != (half ? 1 : 2)) continue;
         const int slot = bits == 8 && half ? 1 : 2, slots = (kblocks + slot - 1) / slot;
         for (int s = 1; s <= 8 && s <= slots; ++s) {
-            // a cluster's CTAs are on the GPU together: no more of them than fit
+            if (cut && s != cut) continue;
+            // no more clusters than are on the GPU at once (a split that a test has set: in turns)
             const int fit = s == 1      ? 0
                             : bits == 4 ? cluster_capacity<4, 1>(di, s, half)
                             : half      ? cluster_capacity<8, 1>(di, s, true)
                                         : cluster_capacity<8, 2>(di, s, false);
-            if (s > 1 && tiles > fit) continue;
+            if (s > 1 && (fit < 1 || tiles > (cut ? INT32_MAX / s : fit))) continue;
             const double us = estimate(kCost[bits == 4][half ? 0 : 1], tok, slots, tiles * s, di->sm_count * (half ? 2 : 1), s, whole_rows);
             if (us < best) best = us, pl.split = s, pl.half = half != 0;
         }
     }
-    if (M > 64) {
+    if (form ? form == 3 : M > 64) {
         const int64_t pairs = (static_cast<int64_t>(N) + 255) / 256 * ((static_cast<int64_t>(M) + 255) / 256);
         if (estimate(kCost[bits == 4][2], 256, bits == 8 ? kblocks : (kblocks + 1) / 2, pairs, di->sm_count / 2, 1, whole_rows) < best)
             pl = {256, 1, false, true};
@@ -794,6 +802,7 @@ extern "C" int wq4_mx_gemm(const uint8_t* W, const uint8_t* W_scales, const uint
     if (!di) return WQ4_ERR_CUDA;
     const bool bulk = (N % 8) == 0 && aligned(y, 16);
     const Plan pl = pick(di, bits, N, M, K / 128, bulk);
+    if (pl.split == 0) return WQ4_ERR_UNSUPPORTED;
     const bool pair = pl.pair;
     const int T = pl.tok, rows = pair ? 256 : 128;
     Args a = {};
@@ -839,4 +848,11 @@ extern "C" int wq4_mx_gemm(const uint8_t* W, const uint8_t* W_scales, const uint
     }
     if (bits == 4) return launch<4, 1>(di, tm.w, tm.x, a, pl, st);
     return pl.half ? launch<8, 1>(di, tm.w, tm.x, a, pl, st) : launch<8, 2>(di, tm.w, tm.x, a, pl, st);
+}
+
+extern "C" int wq4_test_mx_form(int form, int split)
+{
+    if (form < 0 || form > 3 || split < 0 || split > 8 || (split > 0 && form != 1 && form != 2)) return WQ4_ERR_INVALID;
+    g_form.store(16 * split + form);
+    return WQ4_OK;
 }

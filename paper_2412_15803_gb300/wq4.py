@@ -114,6 +114,7 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
     L.wq4_test_chain_waits.argtypes = [_U64, _I]
     L.wq4_test_gemv_path.argtypes = [_I]
     L.wq4_test_copy_stall.argtypes = [_I]
+    L.wq4_test_mx_form.argtypes = [_I, _I]
     L.wq4_decode_step_workspace_bytes.argtypes = [ctypes.POINTER(wq4_layer_table)]
     L.wq4_decode_step_workspace_bytes.restype = _SZ
     L.wq4_decode_step.argtypes = [ctypes.POINTER(wq4_layer_table), ctypes.POINTER(wq4_decode_attn), _P, _P, _P]
@@ -151,7 +152,7 @@ EXPORTED = ["wq4_gemv", "wq4_gemm", "wq4_unpack_debug", "wq4_pack_host", "wq4_st
             "wq4_device_status", "wq4_chain_workspace_bytes", "wq4_decode_chain",
             "wq4_decode_chain_host", "wq4_decode_chain_noalloc", "wq4_chain_plan_destroy", "wq4_chain_path",
             "wq4_chain_trace_offsets",
-            "wq4_test_chain_waits", "wq4_test_gemv_path", "wq4_test_copy_stall",
+            "wq4_test_chain_waits", "wq4_test_gemv_path", "wq4_test_copy_stall", "wq4_test_mx_form",
             "wq4_decode_step_workspace_bytes", "wq4_decode_step", "wq4_decode_step_host",
             "wq4_mx_scale_bytes", "wq4_mx_gemm", "wq4_mx_norm", "wq4_mx_silu", "wq4_mx_quantize", "wq4_mx_dequantize",
             "wq4_synth_codes", "wq4_synth_scales", "wq4_synth_sum4",
@@ -318,6 +319,11 @@ def wq4_test_gemv_path(path: int) -> None:
 def wq4_test_copy_stall(stall: int = 0) -> None:
     """Test hook: the copies that later launches leave out (WQ4_STALL_* of wq4.h)."""
     _check("wq4_test_copy_stall", load().wq4_test_copy_stall(stall))
+
+
+def wq4_test_mx_form(form: int = 0, split: int = 0) -> None:
+    """Test hook: the form of wq4_mx_gemm, 0 by size, 1 two blocks an SM, 2 one, 3 pairs, and how many share a tile's K."""
+    _check("wq4_test_mx_form", load().wq4_test_mx_form(form, split))
 
 
 def wq4_test_chain_waits(wait_limit_ns: int, stall_stage: int = -1) -> None:

@@ -43,3 +43,33 @@ for bits in (8, 4):
         other += product(M, N, K, bits)[0] != odd
 assert other >= 3       # sizes where it decides
 """)
+
+
+def test_form_hook(fake_cudart):
+    """Each form by its blocks' shared memory and its grid; what it does not take is refused."""
+    run(fake_cudart, r"""
+HALF, WHOLE = 113 * 1024, 227 * 1024
+f = L.wq4_test_mx_form
+refused = lambda *a: L.wq4_mx_gemm(A, 4 * A, 8 * A, 16 * A, 32 * A, a[1], a[2], a[0], a[3], None) == wq4.WQ4_ERR_UNSUPPORTED
+sizes = [(1, 1, 128, 8), (1, 6144, 4096, 8), (77, 5003, 2176, 4), (300, 640, 14336, 8), (2048, 28672, 4096, 4)]
+before = [product(*c) for c in sizes]
+pairs = {}
+for M, N, K, bits in ((1, 1, 128, 8), (33, 1003, 2176, 8), (80, 1003, 2176, 4), (300, 640, 14336, 8), (2048, 28672, 4096, 4)):
+    tiles = -(-N // 128) * -(-M // min(128, -(-M // 16) * 16))
+    for form, smem in ((1, HALF), (2, WHOLE)):
+        for split in range(9):
+            assert f(form, split) == 0
+            slots = -(-K // (128 if bits == 8 and form == 1 else 256))
+            if (form == 1 and M > 80) or split > slots:
+                assert refused(M, N, K, bits), (M, N, K, bits, form, split)
+            else:
+                k, grid, s = product(M, N, K, bits)
+                assert s == smem and (split == 0 or grid == (min(tiles, 304 if form == 1 else 152) if split == 1 else tiles * split))
+    assert f(3, 0) == 0
+    k, grid, s = product(M, N, K, bits)
+    assert s not in (HALF, WHOLE) and grid == 2 * min(76, -(-N // 256) * -(-M // 256))
+    assert pairs.setdefault(bits, k) == k
+for bad in ((-1, 0), (4, 0), (0, 1), (3, 2), (1, 9), (2, -1)):
+    assert f(*bad) == wq4.WQ4_ERR_INVALID
+assert f(0, 0) == 0 and [product(*c) for c in sizes] == before
+""")
