@@ -229,8 +229,10 @@ size_t wq4_mx_scale_bytes(int rows, int K);
  * y[m][n] = fp16( sum_k x(m,k) * w(n,k) ), m < M, n < N, with microscaled
  * weights of 4 bits (W, W_scales: N rows) and activations of `bits` bits (x,
  * x_scales: M rows), on the tensor cores: products are exact, sums in fp32.
- * Accuracy: |y - y_ref| <= 2^-12 * sum_k |w*x| + ulp16(|y_ref|); a sum beyond
- * fp16's range comes back as an infinity.  y is fp16 [M][N].
+ * Accuracy: |y - y_ref| <= max(2^-12, K * 2^-27) * sum_k |w*x| + ulp16(|y_ref|)
+ * (the two are the same at K = 32768; K / 32 additions of at most 2^-22 of the sum
+ * each).  A sum beyond fp16's range comes back as an infinity; where sum_k |w*x| is
+ * beyond fp32's, y may be an infinity or NaN.  y is fp16 [M][N].
  */
 int wq4_mx_gemm(const uint8_t* W, const uint8_t* W_scales, const uint8_t* x, const uint8_t* x_scales, uint16_t* y,
                 int N, int K, int M, int bits, void* stream);
