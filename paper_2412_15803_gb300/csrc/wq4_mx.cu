@@ -458,46 +458,45 @@ __global__ void __launch_bounds__(1024) norm_kernel(const NormArgs a)
     }
 }
 
-// Many long rows: bulk copies bring the next rows into a ring in shared memory while
-// this one is in registers, so that what is in flight does not end at a block's
-// barrier; one barrier a row, after which its slot is free.
-constexpr int kNormSlots = 8;
+constexpr int kCopyMost = 16384;      // columns: four chunks for each of 512 threads
 
+// Many long rows: a bulk copy brings a block's next row (and the residual's) into shared
+// memory while this one is in registers, so that what is in flight does not end at a
+// block's barrier; one barrier a row, after which the buffer is free.  (Two to six rows
+// in shared memory: no gain at any width from 6272 to 16384.)
 template <int BITS, int NC>
-__global__ void __launch_bounds__(512) norm_ring_kernel(const NormArgs a, const int slots, uint32_t* err)
+__global__ void __launch_bounds__(512) norm_copy_kernel(const NormArgs a, uint32_t* err)
 {
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ float part[2][32];
-    __shared__ __align__(8) uint64_t full[kNormSlots];
+    __shared__ __align__(8) uint64_t full;
     const int nt = static_cast<int>(blockDim.x), chunks = a.K >> 3, t = static_cast<int>(threadIdx.x);
-    const uint32_t row_bytes = 2 * a.K, slot_bytes = a.residual ? 2 * row_bytes : row_bytes;
+    const uint32_t row_bytes = 2 * a.K;
     const int step = static_cast<int>(gridDim.x);
     uint64_t pol = 0;
-    auto fetch = [&](int slot, int r) {
-        uint8_t* dst = smem + slot * slot_bytes;
-        mbar_arrive_expect_tx(&full[slot], slot_bytes);
-        bulk_g2s(dst, a.x + static_cast<size_t>(r) * a.x_stride, row_bytes, &full[slot], pol);
-        if (a.residual) bulk_g2s(dst + row_bytes, a.residual + static_cast<size_t>(r) * a.residual_stride, row_bytes, &full[slot], pol);
+    auto fetch = [&](int64_t r) {
+        mbar_arrive_expect_tx(&full, a.residual ? 2 * row_bytes : row_bytes);
+        bulk_g2s(smem, a.x + static_cast<size_t>(r) * a.x_stride, row_bytes, &full, pol);
+        if (a.residual) bulk_g2s(smem + row_bytes, a.residual + static_cast<size_t>(r) * a.residual_stride, row_bytes, &full, pol);
     };
     if (t == 0) {
-        for (int i = 0; i < slots; ++i) mbar_init(&full[i], 1);
+        mbar_init(&full, 1);
         mbar_fence_init();
     }
     grid_dependency_wait();
     grid_dependents_launch();
     if (t == 0) {
         pol = l2_policy_evict_first();
-        for (int i = 0; i < slots && blockIdx.x + static_cast<int64_t>(i) * step < a.M; ++i) fetch(i, blockIdx.x + i * step);
+        fetch(blockIdx.x);
     }
     uint4 g[NC];
 #pragma unroll
     for (int i = 0; i < NC; ++i) g[i] = load_gain(a, t + i * nt);
-    __syncthreads();                 // the barriers are there
-    int slot = 0, buf = 0;
+    __syncthreads();                 // the barrier is there
+    const uint4* const xs = reinterpret_cast<const uint4*>(smem);
     uint32_t par = 0;
-    for (int64_t r = blockIdx.x; r < a.M; r += step, buf ^= 1) {
-        mbar_wait(&full[slot], par, err);
-        const uint4* xs = reinterpret_cast<const uint4*>(smem + slot * slot_bytes);
+    for (int64_t r = blockIdx.x; r < a.M; r += step, par ^= 1u) {
+        mbar_wait(&full, par, err);
         uint4 h[NC];
         float ss = 0.f;
 #pragma unroll
@@ -512,10 +511,10 @@ __global__ void __launch_bounds__(512) norm_ring_kernel(const NormArgs a, const 
             ss = squares(h[i], ss);
         }
         ss = warp_sum(ss);
-        if ((t & 31) == 0) part[buf][t >> 5] = ss;
+        if ((t & 31) == 0) part[par][t >> 5] = ss;
         __syncthreads();
-        if (t == 0 && r + static_cast<int64_t>(slots) * step < a.M) fetch(slot, static_cast<int>(r + static_cast<int64_t>(slots) * step));
-        ss = warp_sum((t & 31) < (nt >> 5) ? part[buf][t & 31] : 0.f);
+        if (t == 0 && r + step < a.M) fetch(r + step);
+        ss = warp_sum((t & 31) < (nt >> 5) ? part[par][t & 31] : 0.f);
         const float f = rsqrtf(ss / static_cast<float>(a.K) + a.eps);
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
@@ -524,10 +523,6 @@ __global__ void __launch_bounds__(512) norm_ring_kernel(const NormArgs a, const 
             norm_codes(h[i], g[i], f, o);
             const uint32_t w = store_codes<BITS>(o, a.codes, static_cast<int>(r), c, a.K, c < chunks);
             store_scales(w, a.scales, static_cast<int>(r), c, a.K, c < chunks);
-        }
-        if (++slot == slots) {
-            slot = 0;
-            par ^= 1u;
         }
     }
 }
@@ -657,25 +652,27 @@ int run_rows(const uint16_t* x, int stride, uint8_t* codes, uint8_t* scales, int
                   scales, M, K);
 }
 
+// Blocks of an SM: two to five are resident at a time (56 or 64 registers a thread), the
+// others begin as those end, so that no SM is left with one row more than the next.
+// With a residual and without, us, 64 Mi values of 8192 / 16384 columns: as many as are
+// resident 77.6 / 78.6 and 40.5 / 40.0, 2048 threads' worth 77.9 / 78.7 and 39.8 / 40.8,
+// 16 75.6 / 74.3 and 40.5 / 46.1; in 4 bits with a residual 71.7 / 72.1 as many as are
+// resident, 69.9 / 69.1 16.
 template <int BITS, int NC>
-int launch_norm_ring(const NormArgs& a, const DeviceInfo* di, void* stream)
+int launch_norm_copy(const NormArgs& a, const DeviceInfo* di, void* stream)
 {
-    constexpr int kMost = 220 * 1024;
     static std::atomic<bool> ready[kMaxDevices];      // per device; setting the attribute twice is harmless
     if (!ready[di->dev].load()) {
-        if (cudaFuncSetAttribute(norm_ring_kernel<BITS, NC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost) != cudaSuccess)
+        if (cudaFuncSetAttribute(norm_copy_kernel<BITS, NC>, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * kCopyMost) != cudaSuccess)
             return WQ4_ERR_CUDA;
         ready[di->dev].store(true);
     }
     const int threads = (a.K / 8 + 32 * NC - 1) / (32 * NC) * 32;
-    const int blocks = std::max(1, 2048 / threads);                   // of an SM
-    const int slot = (a.residual ? 4 : 2) * a.K;
-    const int slots = std::max(1, std::min(kNormSlots, kMost / blocks / slot));
-    const int64_t grid = std::min<int64_t>(a.M, static_cast<int64_t>(di->sm_count) * blocks);
-    return launch(norm_ring_kernel<BITS, NC>, grid, threads, static_cast<size_t>(slots) * slot, stream, a, slots, di->status);
+    const int64_t grid = std::min<int64_t>(a.M, static_cast<int64_t>(di->sm_count) * (a.residual ? 16 : 2048 / threads));
+    return launch(norm_copy_kernel<BITS, NC>, grid, threads, static_cast<size_t>(a.residual ? 4 : 2) * a.K, stream, a, di->status);
 }
 
-// Measured, 8 bits, us: by a block a row and by the ring 8192 rows of 4096 38.4 and
+// Measured, 8 bits, us: by a block a row and by copies 8192 rows of 4096 38.4 and
 // 38.9, 8000 of 5120 48.5 and 49.2, 6000 of 8192 58.1 and 57.3, 5000 of 11008 79.8 and
 // 64.1; by a block and by a warp a row 16384 of 1024 20.2 and 22.0, of 512 12.7 and
 // 11.1, of 128 9.3 and 5.4.  (8192 of 4096: 38.0 with packed products, 6.2 TB/s; 46.7
@@ -690,7 +687,7 @@ int launch_norm(const NormArgs& a, const DeviceInfo* di, void* stream)
         return chunks <= 32 ? launch(norm_warp_kernel<BITS, 1>, grid, 256, 0, stream, a)
                             : launch(norm_warp_kernel<BITS, 2>, grid, 256, 0, stream, a);
     }
-    if (a.M > 4 * di->sm_count && a.K > 6144 && a.K <= 16384) return launch_norm_ring<BITS, 4>(a, di, stream);
+    if (a.M > 4 * di->sm_count && a.K > 6144 && a.K <= kCopyMost) return launch_norm_copy<BITS, 4>(a, di, stream);
     const int threads = chunks < 1024 ? (chunks + 31) / 32 * 32 : 1024;
     const int n = (chunks + threads - 1) / threads;
     const int grid = std::min(a.M, di->sm_count * 16);

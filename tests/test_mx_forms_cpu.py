@@ -73,3 +73,15 @@ for bad in ((-1, 0), (4, 0), (0, 1), (3, 2), (1, 9), (2, -1)):
     assert f(*bad) == wq4.WQ4_ERR_INVALID
 assert f(0, 0) == 0 and [product(*c) for c in sizes] == before
 """)
+
+
+def test_norm_of_many_long_rows(fake_cudart):
+    """A block holds one row of each input in shared memory, whatever the width: more were of no use, and mostly not there."""
+    run(fake_cudart, r"""
+for K in range(6272, 16385, 128):
+    for residual in (4 * A, None):
+        for bits in (8, 4):
+            assert L.wq4_mx_norm(A, K, residual, K, 128 * A, 1e-5, None, 0, 16 * A, 64 * A, 8000, K, bits, None) == 0
+            s = fake.fake_last_shape()
+            assert s & 0xffffffff == (4 if residual else 2) * K and 152 <= s >> 32 <= 8000
+""")
