@@ -216,7 +216,7 @@ int wq4_device_status(void* stream, int* flags_out);
  * 8, y of wq4_mx_gemm 2-byte aligned; outputs overlap neither inputs nor each
  * other (buffers are compared from their first byte to their last).  bits is 4
  * or 8, M and N at least 1, N * K and M * K at most 2^41 (wq4_mx_gemm refuses
- * more than 2^30 tiles of 128 x 128 of y: WQ4_ERR_UNSUPPORTED).  Launched with
+ * more than 2^30 tiles of 128 x 128 of y and K above 2^24: WQ4_ERR_UNSUPPORTED).  Launched with
  * programmatic dependent launch; everything is read after the previous kernel in
  * `stream` has completed.  Deterministic.  WQ4_ERR_INVALID for sizes, null
  * pointers and overlaps, WQ4_ERR_ALIGN, WQ4_ERR_CUDA.

@@ -211,7 +211,7 @@ __device__ __forceinline__ void store_scales(uint32_t w, uint8_t* scales, int r,
 // exponential and reciprocal: relative errors of 2^-22 and 2^-23, and of |g| 2^-23
 // from the exponent's product, far below the half step (2^-4) that the code is off
 // by.  Under g = -87 the reciprocal is 0.  (expf and exact quotients: 70 us where
-// these take 46, 4096 rows of 14336 in 8 bits.)
+// these take 44, 4096 rows of 14336 in 8 bits.)
 __device__ __forceinline__ float2 silu_times(float2 g, float2 u)
 {
     const float2 t = mul2(g, make_float2(-1.44269504f, -1.44269504f));

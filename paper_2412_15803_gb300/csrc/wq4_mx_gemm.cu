@@ -21,7 +21,7 @@
 //   rows are shared by many CTAs (K split over a cluster, two CTAs an SM) and four
 //   warps issue copies.  6144 x 4096 over one token 5.8 us (floor 2.0 at the copy
 //   rate), 4096 x 14336 over 16 tokens 9.1 (4.7), 128256 x 4096 over one token in 4
-//   bits 45 (41).
+//   bits 43.5 (41).
 // - a prompt: the power limit.  28672 x 4096 over 2048 tokens in 8 bits 146-153 us
 //   (3.2 PFLOP/s) with the SMs at 1.66 GHz, 117 at 2.07 GHz when all codes are zero;
 //   over 8192 in 4 bits 281-287 (6.8 PFLOP/s; zeros 246).
@@ -402,6 +402,11 @@ constexpr bool fits()
             }
     return true;
 }
+
+// A tile's sum must end within the limit of the epilogue's wait for it, 0.5 s: at ~0.25
+// us for 128 K, 33 ms here in a CTA that has a tile to itself; 2^31 would take that long
+// in a cluster of eight.  (The error that K / 32 additions may add is 2^-3 of the sum.)
+constexpr int kMostK = 1 << 24;
 
 struct Plan {
     int tok, split;
@@ -798,6 +803,7 @@ extern "C" int wq4_mx_gemm(const uint8_t* W, const uint8_t* W_scales, const uint
         overlaps(y, yb, x_scales, wq4_mx_scale_bytes(M, K)))
         return WQ4_ERR_INVALID;
     if ((static_cast<int64_t>(N - 1) / 128 + 1) * (static_cast<int64_t>(M - 1) / 128 + 1) > (static_cast<int64_t>(1) << 30)) return WQ4_ERR_UNSUPPORTED;
+    if (K > kMostK) return WQ4_ERR_UNSUPPORTED;
     const DeviceInfo* di = current_device_info(nullptr);
     if (!di) return WQ4_ERR_CUDA;
     const bool bulk = (N % 8) == 0 && aligned(y, 16);

@@ -85,3 +85,14 @@ for K in range(6272, 16385, 128):
             s = fake.fake_last_shape()
             assert s & 0xffffffff == (4 if residual else 2) * K and 152 <= s >> 32 <= 8000
 """)
+
+
+def test_longest_sums(fake_cudart):
+    """A tile's sum ends well within the limit of a wait for it, and its error stays below the sum: K to 2^24."""
+    run(fake_cudart, r"""
+for bits in (8, 4):
+    for M, N in ((1, 1), (1, 128), (256, 256)):
+        product(M, N, 1 << 24, bits)
+        for K in ((1 << 24) + 128, (1 << 31) - 128):
+            assert L.wq4_mx_gemm(A, 4 * A, 8 * A, 16 * A, 32 * A, N, K, M, bits, None) == wq4.WQ4_ERR_UNSUPPORTED
+""")

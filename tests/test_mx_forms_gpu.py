@@ -154,6 +154,28 @@ def test_long_sums_of_one_sign(form, split, M, N, bits):
     assert np.all(err <= max(2.0 ** -12, K * 2.0 ** -27) * A + oracle.ulp16_array(ref))
 
 
+@pytest.mark.parametrize("form,split", [(0, 0), (HALF, 1), (WHOLE, 1), (PAIRS, 0)])
+def test_the_longest_sum(form, split):
+    """K of 2^24 in one block or pair: no wait runs out.  Every product is 1/2, -1/2 or 0 and the sum below 2^23, so exact."""
+    K, M, N = 1 << 24, 2, 3
+    W = torch.zeros((N, K // 2), dtype=torch.uint8, device="cuda")          # 1 (0x2) and -1 (0xA) at some k
+    at = torch.from_numpy(np.random.default_rng(3).permutation(K // 2)[:20000]).cuda()
+    for n in range(N):
+        W[n, at[:5000 + 4000 * n]] = 0x02
+        W[n, at[15000:15000 + 1000 * n]] = 0xA0
+    ws = torch.full((wq4.wq4_mx_scale_bytes(N, K),), 127, dtype=torch.uint8, device="cuda")
+    x = torch.full((M, K), 0x38, dtype=torch.uint8, device="cuda")          # 1
+    x[1, ::2] = 0xB8                                                        # -1 and 1 in turn
+    xs = torch.full((wq4.wq4_mx_scale_bytes(M, K),), 126, dtype=torch.uint8, device="cuda")
+    y = torch.zeros((M, N), dtype=torch.float16, device="cuda")
+    with form_of(form, split):
+        wq4.wq4_mx_gemm(W, ws, x, xs, y, N, K, M, 8)
+        torch.cuda.synchronize()
+    assert wq4.wq4_device_status() == 0
+    lower, upper = np.array([5000, 9000, 13000]), np.array([0, 1000, 2000])
+    assert np.array_equal(y.cpu().numpy(), np.stack([lower - upper, -lower - upper]).astype(np.float64) / 2)
+
+
 @pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("form,split,M,N,K", FORMS)
 def test_operands_written_late(late_copy, form, split, M, N, K, bits):  # noqa: F811
